@@ -1,0 +1,429 @@
+"""The operators around the expert layer in training, and the cases that their speed is measured on.
+
+Four operators, which a training step of a token model with expert layers runs one after the other:
+
+  lookup, lookup_grad   token embeddings: rows of a table by token, scaled; the gradient of the table (every row of it)
+  norm, norm_grad       layer norm of the tokens; gradients of its input, its weight and its bias
+  product, product_grad_input, product_grad_weight
+                        products of stacked token rows with their experts' matrices: the layer, optionally ReLU, its rows
+                        gathered from the tokens; the gradient of its rows, optionally through the ReLU below; the gradient
+                        of the matrices
+  clip                  the norm of all gradients together, and the gradients scaled down to a largest norm
+
+Token ids and expert loads follow Zipf's law, as words and routers do; some ids are the -1 of padding and some experts have
+no rows.  Widths are those of the benchmark configurations' expert layers (512 -> 1024 with 256 experts and two uses of a
+token, 1024 -> 2048 with 1024 experts and four), or drawn around them.
+"""
+from __future__ import annotations
+
+import math
+
+import numpy as np
+import torch
+
+own = False                # False: the operators' plain forms; True: the framework's entry points
+
+DTYPE = {"bf16": torch.bfloat16, "f32": torch.float32}
+EPS = 1e-5
+
+
+# ------------------------------------------------------------------------------------------ the cases
+def _lookup(name, T, V, d, dtype="bf16", grad=False, grad_dtype="f32", pad=0.0):
+    return dict(name=name, kind="lookup_grad" if grad else "lookup", T=T, V=V, d=d, dtype=dtype, grad_dtype=grad_dtype, pad=pad)
+
+
+def _norm(name, T, d, dtype="bf16", grad=False):
+    return dict(name=name, kind="norm_grad" if grad else "norm", T=T, d=d, dtype=dtype)
+
+
+def _product(name, kind, T, k, K, N, E, zipf, empty=0.0, fused=True, grad_dtype="f32"):
+    return dict(name=name, kind=kind, T=T, k=k, K=K, N=N, E=E, zipf=zipf, empty=empty, fused=fused, grad_dtype=grad_dtype)
+
+
+def _clip(name, tensors, elements, dtype="f32", scale=1.0):
+    return dict(name=name, kind="clip", tensors=tensors, elements=elements, dtype=dtype, scale=scale)
+
+
+def listed():
+    return [
+        # one step of generation for a few sequences: the new tokens' embeddings
+        _lookup("lookup_37", 37, 32000, 512),
+        # a small training batch in full precision, a table with an odd number of rows, a few of them padding
+        _lookup("lookup_grad_4095_f32", 4095, 20011, 512, dtype="f32", grad=True, pad=0.05),
+        # the large layer's batch: the embedding's gradient, into the fp32 sum that an optimiser keeps
+        _lookup("lookup_grad_65536", 65536, 50021, 1024, grad=True, pad=0.01),
+        # the norm ahead of the layer for the same few tokens
+        _norm("norm_37", 37, 512),
+        # a batch of odd sizes in full precision, backward
+        _norm("norm_grad_4097x777_f32", 4097, 777, dtype="f32", grad=True),
+        # the large layer's batch, backward
+        _norm("norm_grad_65536x1024", 65536, 1024, grad=True),
+        # generation: the first expert layer of the small configuration, most experts idle
+        _product("product_74", "product", 37, 2, 512, 1024, 256, 1.1),
+        # the small configuration's training batch: the gradient of the hidden rows through the ReLU
+        _product("product_grad_input_8192", "product_grad_input", 4096, 2, 1024, 512, 256, 1.1),
+        # crowded experts: the first layer forward, rows gathered from the tokens
+        _product("product_65536", "product", 16384, 4, 1024, 2048, 64, 0.6, empty=0.05),
+        # ... and the gradient of that layer's matrices
+        _product("product_grad_weight_65536", "product_grad_weight", 16384, 4, 1024, 2048, 64, 0.6, empty=0.05),
+        # the program-tree engine's gradients: some forty functions' tensors, from biases to 3x3 convolutions
+        _clip("clip_240", 240, 14_000_000),
+        # expert layers' gradients: few tensors, gigabytes
+        _clip("clip_12_bf16", 12, 1_000_000_000, dtype="bf16", scale=1e-3),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return min(hi, max(lo, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def _width(rng, lo, hi):
+    """Mostly a multiple of 64, sometimes of 8, sometimes anything."""
+    n, form = _log_int(rng, lo, hi), rng.random()
+    unit = 64 if form < 0.6 else 8 if form < 0.8 else 1
+    return max(unit, n // unit * unit)
+
+
+def draw(rng):
+    kind = rng.choice(["lookup", "lookup_grad", "norm", "norm_grad", "product", "product", "product_grad_input",
+                       "product_grad_weight", "clip"])
+    dtype = rng.choice(["bf16", "bf16", "f32"])
+    while True:
+        if kind in ("lookup", "lookup_grad"):
+            case = dict(kind=kind, T=_log_int(rng, 1, 65536), V=_log_int(rng, 40, 200000), d=_width(rng, 64, 2048), dtype=dtype,
+                        grad_dtype=rng.choice(["f32", "f32", "bf16"]) if dtype == "bf16" else "f32", pad=rng.choice([0.0, 0.02, 0.3]))
+            fits = case["V"] * case["d"] <= 50021 * 1024 and case["T"] * case["d"] <= 65536 * 1024
+        elif kind in ("norm", "norm_grad"):
+            case = dict(kind=kind, T=_log_int(rng, 1, 65536), d=_width(rng, 64, 8192), dtype=dtype)
+            fits = case["T"] * case["d"] <= 65536 * 1024 // (2 if dtype == "f32" else 1)
+        elif kind == "clip":
+            case = dict(kind=kind, tensors=_log_int(rng, 1, 1000), elements=_log_int(rng, 10_000, 400_000_000), dtype=dtype,
+                        scale=rng.choice([1.0, 1e-3, 1e-6]))
+            fits = case["elements"] >= 4 * case["tensors"]
+        else:
+            E = _log_int(rng, 1, 1024)
+            case = dict(kind=kind, T=_log_int(rng, 1, 16384), k=min(E, rng.choice([1, 2, 2, 4, 4])), K=_width(rng, 64, 2048), N=_width(rng, 64, 2048),
+                        E=E, zipf=round(rng.uniform(0.4, 1.2), 2), empty=rng.choice([0.0, 0.05]) if E >= 64 else 0.0,
+                        fused=rng.random() < 0.6, grad_dtype=rng.choice(["f32", "bf16"]))
+            fits = (case["T"] * case["k"] * case["K"] * case["N"] <= 65536 * 1024 * 2048 and
+                    E * case["K"] * case["N"] <= 256 * 1024 * 2048)
+        if fits:
+            return case
+
+
+# ------------------------------------------------------------------------------------------ inputs
+def _generators(seed):
+    return np.random.Generator(np.random.Philox(key=[seed, 29])), torch.Generator("cuda").manual_seed(seed * 1000003 + 29)
+
+
+def _normal(g, *shape, dtype, std=1.0):
+    out = torch.empty(shape, dtype=dtype, device="cuda")
+    flat, step = out.view(-1), 1 << 28
+    for i in range(0, flat.numel(), step):
+        part = flat[i:i + step]
+        part.copy_(torch.randn(part.numel(), generator=g, device="cuda").mul_(std))
+    return out
+
+
+def _zipf(r, n, s, size):
+    """`size` ids of 0 .. n - 1 with probabilities that fall as rank ** -s, the ranks dealt to the ids at random."""
+    cum = np.cumsum(np.arange(1, n + 1, dtype=np.float64) ** -s)
+    rank = np.minimum(np.searchsorted(cum, r.random(size) * cum[-1]), n - 1)
+    return r.permutation(n)[rank]
+
+
+def _prepare_lookup(case, seed):
+    r, g = _generators(seed)
+    T, V, d, dt = case["T"], case["V"], case["d"], DTYPE[case["dtype"]]
+    tokens = _zipf(r, V, 1.0, T).astype(np.int32)
+    tokens[r.random(T) < case["pad"]] = -1
+    st = dict(tokens=torch.from_numpy(tokens).cuda(), scale=math.sqrt(d))
+    if case["kind"] == "lookup":
+        st.update(table=_normal(g, V, d, dtype=dt, std=0.02), out=torch.empty((T, d), dtype=dt, device="cuda"))
+    else:
+        st.update(dout=_normal(g, T, d, dtype=dt, std=0.01), V=V,
+                  out=torch.empty((V, d), dtype=DTYPE[case["grad_dtype"]], device="cuda"))
+    return st
+
+
+def _prepare_norm(case, seed):
+    r, g = _generators(seed)
+    T, d, dt = case["T"], case["d"], DTYPE[case["dtype"]]
+    x = _normal(g, T, d, dtype=torch.float32)
+    x.mul_(torch.rand((T, 1), generator=g, device="cuda") * 2 + 0.5).add_(torch.randn((T, 1), generator=g, device="cuda"))
+    st = dict(x=x.to(dt), gamma=_normal(g, d, dtype=torch.float32, std=0.2).add_(1), beta=_normal(g, d, dtype=torch.float32, std=0.1),
+              y=torch.empty((T, d), dtype=dt, device="cuda"))
+    del x
+    if case["kind"] == "norm_grad":                      # what the forward pass left
+        xf = st["x"].float()
+        mean = xf.mean(1)
+        st.update(mean=mean, rstd=((xf - mean[:, None]).square().mean(1) + EPS).rsqrt(), dy=_normal(g, T, d, dtype=dt, std=0.1))
+    return st
+
+
+def _prepare_product(case, seed):
+    """The rows of all uses, stacked by expert: use a of token a // k stands where a stable sort by expert puts it."""
+    r, g = _generators(seed)
+    T, k, K, N, E = (case[x] for x in ("T", "k", "K", "N", "E"))
+    M, bf = T * k, torch.bfloat16
+    live = max(1, E - int(round(E * case["empty"])))
+    expert = r.permutation(E)[_zipf(r, live, case["zipf"], M)]
+    counts = np.bincount(expert, minlength=E)
+    offsets = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+    st = dict(offsets=torch.from_numpy(offsets).cuda(), counts=counts.tolist(), k=k, fused=case["fused"])
+    st["perm"] = torch.from_numpy(np.argsort(expert, kind="stable").astype(np.int32)).cuda()
+    if case["kind"] != "product_grad_weight":
+        st["W"] = _normal(g, E, N, K, dtype=bf, std=math.sqrt(2.0 / K))
+    if case["kind"] != "product":
+        st["dout"] = _normal(g, M, N, dtype=bf, std=0.01)
+    if case["kind"] != "product_grad_input":             # fused: the tokens' own rows, else rows that have been stacked already
+        st["x"] = _normal(g, T if case["fused"] else M, K, dtype=bf)
+    elif case["fused"]:                                  # what the ReLU left: half of it zeros
+        st["act"] = _normal(g, M, K, dtype=bf).clamp_(min=0)
+    if case["kind"] == "product_grad_weight":
+        st["out"] = torch.empty((E, N, K), dtype=DTYPE[case["grad_dtype"]], device="cuda")
+    else:
+        st["out"] = torch.empty((M, N if case["kind"] == "product" else K), dtype=bf, device="cuda")
+    return st
+
+
+def _clip_sizes(case):
+    """Tensors of very different sizes, as a network's are: from biases to whole expert layers."""
+    n, total = case["tensors"], case["elements"]
+    share = np.exp(np.random.Generator(np.random.Philox(key=[total, n])).normal(0.0, 2.0, n))
+    size = np.maximum(1, np.floor(share / share.sum() * (total - n)).astype(np.int64))
+    size[int(np.argmax(size))] += total - int(size.sum())
+    return size.tolist()
+
+
+def _bucket(sizes, dtype):
+    """One buffer and the tensors in it, each on a border of 64 elements, as an optimiser's flat buffer has them."""
+    at = np.concatenate([[0], np.cumsum([(s + 63) // 64 * 64 for s in sizes])]).tolist()
+    flat = torch.zeros(at[-1], dtype=dtype, device="cuda")
+    return flat, [flat[a:a + s] for a, s in zip(at, sizes)]
+
+
+def _prepare_clip(case, seed):
+    r, g = _generators(seed)
+    sizes, dt = _clip_sizes(case), DTYPE[case["dtype"]]
+    grads = [_normal(g, s, dtype=dt, std=case["scale"] * float(r.uniform(0.2, 2.0))) for s in sizes]
+    flat, out = _bucket(sizes, dt)
+    return dict(grads=grads, out=out, flat=flat, max_norm=1.0)
+
+
+def prepare(case, seed):
+    kind = case["kind"]
+    make = (_prepare_lookup if kind.startswith("lookup") else _prepare_norm if kind.startswith("norm") else
+            _prepare_clip if kind == "clip" else _prepare_product)
+    return dict(make(case, seed), kind=kind)
+
+
+# ------------------------------------------------------------------------------------------ plain forms
+def _plain_lookup(st):
+    tokens, table = st["tokens"].long(), st["table"]
+    known = (tokens >= 0) & (tokens < table.shape[0])
+    rows = table[torch.where(known, tokens, 0)].float() * st["scale"]
+    return torch.where(known[:, None], rows, 0.0).to(table.dtype)
+
+
+def _plain_lookup_grad(st):
+    tokens, V = st["tokens"].long(), st["V"]
+    row = torch.where((tokens >= 0) & (tokens < V), tokens, V)
+    total = torch.zeros((V + 1, st["dout"].shape[1]), dtype=torch.float32, device=row.device)
+    total.index_add_(0, row, st["dout"].float())
+    return (total[:V] * st["scale"]).to(st["out"].dtype)
+
+
+def _plain_norm(st):
+    x = st["x"].float()
+    mean = x.mean(1)
+    centred = x - mean[:, None]
+    rstd = (centred.square().mean(1) + EPS).rsqrt()
+    y = centred * rstd[:, None] * st["gamma"] + st["beta"]
+    return y.to(st["x"].dtype), mean, rstd
+
+
+def _plain_norm_grad(st):
+    dy = st["dy"].float()
+    xhat = (st["x"].float() - st["mean"][:, None]) * st["rstd"][:, None]
+    g = dy * st["gamma"]
+    dx = (g - g.mean(1, keepdim=True) - xhat * (g * xhat).mean(1, keepdim=True)) * st["rstd"][:, None]
+    return dx.to(st["x"].dtype), (dy * xhat).sum(0), dy.sum(0)
+
+
+def _groups(counts):
+    at = 0
+    for e, n in enumerate(counts):
+        if n:
+            yield e, slice(at, at + n)
+        at += n
+
+
+def _plain_rows(st, rows):
+    return st["x"][st["perm"][rows].long() // st["k"]] if st["fused"] else st["x"][rows]
+
+
+def _plain_product(st):
+    out = torch.zeros_like(st["out"])
+    for e, rows in _groups(st["counts"]):
+        y = _plain_rows(st, rows).float() @ st["W"][e].float().t()
+        out[rows] = (y.clamp(min=0) if st["fused"] else y).to(out.dtype)
+    return out
+
+
+def _plain_product_grad_input(st):
+    out = torch.zeros_like(st["out"])
+    for e, rows in _groups(st["counts"]):
+        g = st["dout"][rows].float() @ st["W"][e].float()
+        out[rows] = (torch.where(st["act"][rows] > 0, g, 0.0) if st["fused"] else g).to(out.dtype)
+    return out
+
+
+def _plain_product_grad_weight(st):
+    out = torch.zeros_like(st["out"])
+    for e, rows in _groups(st["counts"]):
+        out[e] = (st["dout"][rows].float().t() @ _plain_rows(st, rows).float()).to(out.dtype)
+    return out
+
+
+def _plain_clip(st):
+    total = torch.zeros((), dtype=torch.float32, device="cuda")
+    for t in st["grads"]:
+        total = total + t.float().square().sum()
+    norm = total.sqrt()
+    factor = torch.where(torch.isfinite(norm) & (norm > st["max_norm"]), st["max_norm"] / norm, 1.0)
+    for t, o in zip(st["grads"], st["out"]):
+        o.copy_(t.float() * factor)
+    return norm, st["flat"]
+
+
+PLAIN = dict(lookup=_plain_lookup, lookup_grad=_plain_lookup_grad, norm=_plain_norm, norm_grad=_plain_norm_grad, product=_plain_product,
+             product_grad_input=_plain_product_grad_input, product_grad_weight=_plain_product_grad_weight, clip=_plain_clip)
+
+
+# ------------------------------------------------------------------------------------------ the framework's
+def _own(st):
+    import paper_1707_02402_amd as dyn
+    kind = st["kind"]
+    if kind == "lookup":
+        return dyn.dynb_embed(st["tokens"], st["table"], scale=st["scale"], out=st["out"])
+    if kind == "lookup_grad":
+        return dyn.dynb_embed_backward(st["tokens"], st["dout"], st["V"], scale=st["scale"], dtable=st["out"])
+    if kind == "norm":
+        return dyn.dynb_layer_norm(st["x"], st["gamma"], st["beta"], eps=EPS, out=st["y"], want_stats=True)
+    if kind == "norm_grad":
+        return dyn.dynb_layer_norm_backward(st["dy"], st["x"], st["gamma"], st["mean"], st["rstd"], dx=st["y"])
+    if kind == "clip":
+        norm, _ = dyn.dynb_clip_gradients(st["grads"], st["max_norm"], out=st["out"])
+        return norm, st["flat"]
+    gathered = dict(perm=st["perm"], k=st["k"]) if st["fused"] else {}
+    if kind == "product":
+        return dyn.moe_product(st["x"], st["W"], st["offsets"], relu=st["fused"], out=st["out"], **gathered)
+    if kind == "product_grad_input":
+        return dyn.moe_product_grad_input(st["dout"], st["W"], st["offsets"], act=st.get("act"), out=st["out"])
+    return dyn.moe_product_grad_weight(st["dout"], st["x"], st["offsets"], dW=st["out"], **gathered)
+
+
+def run(state):
+    return _own(state) if own else PLAIN[state["kind"]](state)
+
+
+# ------------------------------------------------------------------------------------------ in 64 bits
+def _by_expert(offsets):
+    """expert, first and last row (exclusive) of each, from the offsets alone"""
+    at = offsets.cpu().tolist()
+    return [(e, at[e], at[e + 1]) for e in range(len(at) - 1) if at[e + 1] > at[e]]
+
+
+def exact(case, seed):
+    st, kind, f8 = prepare(case, seed), case["kind"], torch.float64
+    if kind == "lookup":
+        out = torch.zeros(st["out"].shape, dtype=f8, device="cuda")
+        at = torch.nonzero(st["tokens"] >= 0)[:, 0]
+        out[at] = st["table"].index_select(0, st["tokens"][at]).to(f8) * st["scale"]
+        return out
+    if kind == "lookup_grad":
+        # a running sum over the uses in the order of their tokens: a token's gradient is the difference of two of its places
+        tokens, d = st["tokens"], case["d"]
+        order = torch.argsort(tokens)
+        ends = torch.searchsorted(tokens[order].contiguous(), torch.arange(-1, case["V"], device="cuda", dtype=torch.int32), right=True)
+        out = torch.empty((case["V"], d), dtype=f8, device="cuda")
+        for c in range(0, d, 128):
+            run_ = torch.zeros((len(order) + 1, min(128, d - c)), dtype=f8, device="cuda")
+            torch.cumsum(st["dout"][order, c:c + 128].to(f8), 0, out=run_[1:])
+            out[:, c:c + 128] = (run_[ends[1:]] - run_[ends[:-1]]) * st["scale"]
+        return out
+    if kind == "norm":
+        x = st["x"].to(f8)
+        var, mean = torch.var_mean(x, 1, correction=0)
+        rstd = 1.0 / torch.sqrt(var + EPS)
+        return (x - mean[:, None]) * rstd[:, None] * st["gamma"].to(f8) + st["beta"].to(f8), mean, rstd
+    if kind == "norm_grad":
+        d = case["d"]
+        x, dy, rstd = st["x"].to(f8), st["dy"].to(f8), st["rstd"].to(f8)[:, None]
+        h = (x - st["mean"].to(f8)[:, None]) * rstd
+        p = torch.stack([dy @ st["gamma"].to(f8), (dy * h) @ st["gamma"].to(f8)], 1) / d
+        dx = rstd * (dy * st["gamma"].to(f8) - p[:, :1] - h * p[:, 1:])
+        return dx, torch.einsum("td,td->d", dy, h), torch.ones(len(x), dtype=f8, device="cuda") @ dy
+    if kind == "clip":
+        parts = [torch.linalg.vector_norm(t.to(f8)).item() for t in st["grads"]]
+        norm = math.sqrt(math.fsum(p * p for p in parts))
+        flat, out = _bucket([t.numel() for t in st["grads"]], f8)
+        for t, o in zip(st["grads"], out):
+            o.copy_(t).mul_(st["max_norm"] / norm if st["max_norm"] < norm < math.inf else 1.0)
+        return torch.tensor(norm, dtype=f8, device="cuda"), flat
+    x = st.get("x")
+    if x is not None:
+        x = x.to(f8)
+        if st["fused"]:
+            x = x.index_select(0, torch.div(st["perm"], st["k"], rounding_mode="floor"))
+    out = torch.zeros(st["out"].shape, dtype=f8, device="cuda")
+    for e, lo, hi in _by_expert(st["offsets"]):
+        if kind == "product":
+            torch.mm(x[lo:hi], st["W"][e].to(f8).t(), out=out[lo:hi])
+        elif kind == "product_grad_input":
+            torch.mm(st["dout"][lo:hi].to(f8), st["W"][e].to(f8), out=out[lo:hi])
+        else:
+            torch.mm(st["dout"][lo:hi].to(f8).t(), x[lo:hi], out=out[e])
+    if kind == "product" and st["fused"]:
+        out.relu_()
+    if kind == "product_grad_input" and st["fused"]:
+        out.mul_((st["act"] > 0).to(f8))
+    return out
+
+
+# ------------------------------------------------------------------------------------------ what a pass cannot do without
+def _expected_distinct(n, s, draws):
+    """How many of n ids turn up in so many draws by Zipf's law."""
+    p = np.arange(1, n + 1, dtype=np.float64) ** -s
+    return float(-np.expm1(draws * np.log1p(-np.minimum(p / p.sum(), 1 - 1e-12))).sum())
+
+
+def work(case):
+    kind = case["kind"]
+    if kind.startswith("lookup"):
+        T, V, d, e = case["T"], case["V"], case["d"], 2 if case["dtype"] == "bf16" else 4
+        used = T * (1 - case["pad"])
+        if kind == "lookup":
+            return dict(bytes=4 * T + int(_expected_distinct(V, 1.0, used)) * d * e + T * d * e, flops=T * d)
+        return dict(bytes=4 * T + int(used) * d * e + V * d * (2 if case["grad_dtype"] == "bf16" else 4), flops=int(used) * d)
+    if kind.startswith("norm"):
+        T, d, e = case["T"], case["d"], 2 if case["dtype"] == "bf16" else 4
+        if kind == "norm":
+            return dict(bytes=2 * T * d * e + 8 * T + 8 * d, flops=7 * T * d)
+        return dict(bytes=3 * T * d * e + 8 * T + 12 * d, flops=14 * T * d)
+    if kind == "clip":
+        n, e = case["elements"], 2 if case["dtype"] == "bf16" else 4
+        return dict(bytes=2 * n * e, flops=3 * n)
+    T, k, K, N, E = (case[x] for x in ("T", "k", "K", "N", "E"))
+    M = T * k
+    live = max(1, E - int(round(E * case["empty"])))
+    used = int(_expected_distinct(live, case["zipf"], M))
+    in_rows = (T if case["fused"] else M) * K * 2
+    if kind == "product":
+        nbytes = in_rows + M * N * 2 + used * N * K * 2 + 4 * E
+    elif kind == "product_grad_input":
+        nbytes = M * N * 2 + M * K * 2 * (2 if case["fused"] else 1) + used * N * K * 2 + 4 * E
+    else:
+        nbytes = in_rows + M * N * 2 + E * N * K * (2 if case["grad_dtype"] == "bf16" else 4) + 4 * E
+    return dict(bytes=nbytes, flops=2 * M * N * K)
