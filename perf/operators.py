@@ -208,7 +208,11 @@ def _prepare_clip(case, seed):
     sizes, dt = _clip_sizes(case), DTYPE[case["dtype"]]
     grads = [_normal(g, s, dtype=dt, std=case["scale"] * float(r.uniform(0.2, 2.0))) for s in sizes]
     flat, out = _bucket(sizes, dt)
-    return dict(grads=grads, out=out, flat=flat, max_norm=1.0)
+    st = dict(grads=grads, out=out, flat=flat, max_norm=1.0)
+    if own:                                              # the list of a network's gradients, which stay where they are from step to step
+        import paper_1707_02402_amd as dyn
+        st["list"] = dyn.GradTensors(grads, out)
+    return st
 
 
 def prepare(case, seed):
@@ -314,8 +318,7 @@ def _own(st):
     if kind == "norm_grad":
         return dyn.dynb_layer_norm_backward(st["dy"], st["x"], st["gamma"], st["mean"], st["rstd"], dx=st["y"])
     if kind == "clip":
-        norm, _ = dyn.dynb_clip_gradients(st["grads"], st["max_norm"], out=st["out"])
-        return norm, st["flat"]
+        return dyn.dynb_clip_gradients(st["list"], st["max_norm"]), st["flat"]
     gathered = dict(perm=st["perm"], k=st["k"]) if st["fused"] else {}
     if kind == "product":
         return dyn.moe_product(st["x"], st["W"], st["offsets"], relu=st["fused"], out=st["out"], **gathered)
