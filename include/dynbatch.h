@@ -14,6 +14,8 @@
  *   2. Sparsely gated mixture of experts (Results / Sparsely Gated Mixture of Experts):
  *      moe_forward()      GPU   — noisy top-k gate, grouping of the k*b known expert uses by
  *                                 expert, one grouped FFN per expert, weighted combine
+ *      moe_product*()     GPU   — the expert layers' matrix products by themselves, and their gradients; with
+ *      dynb_embed*(), dynb_layer_norm*(), dynb_clip_gradients(): what training around such layers takes
  *
  * Conventions
  *   - Every function returns DYNB_OK (0) or a negative DYNB_E_* code; dynb_last_error() gives a
@@ -454,6 +456,121 @@ int moe_forward_naive(const moe_shape* shape, const void* x, const void* Wg, con
                       const float* noise, const void* W1, const void* W2, void* out,
                       const moe_aux* aux, void* workspace, size_t workspace_bytes, void* stream,
                       int32_t use_stride);
+
+/* ------------------------------------------------------------------------------------------- */
+/* Training around the expert layer: products grouped by expert, embeddings, layer norm, clipping */
+/* ------------------------------------------------------------------------------------------- */
+
+/* The three matrix products of a layer whose rows are stacked by expert (what moe_forward does inside, and its
+ * gradients): group e of the rows is multiplied with matrix W_e.
+ *   out[r]  = f(in[row(r)] W_e^T)                          f: nothing, or ReLU
+ *   din[r]  = (dout[r] W_e), set to 0 where !(act > 0)     act: the ReLU's results that `in` consists of, or NULL
+ *   dW_e    = sum over group e of dout[r]^T in[row(r)]     an empty group's is 0                  */
+typedef struct {
+    int32_t M;                /* rows of all groups together (0: no work, gradients of W are 0)  */
+    int32_t K;                /* channels of a row of in                                         */
+    int32_t N;                /* features of a row of out                                        */
+    int32_t E;                /* experts                                                         */
+    int32_t dtype;            /* DYNB_BF16 only: rows and weights (sums are fp32)                */
+    uint32_t flags;           /* 0, or MOE_PRODUCT_RELU (moe_product)                            */
+} moe_product_shape;
+enum { MOE_PRODUCT_RELU = 1 };
+
+/* Which rows are whose: moe_aux's offsets and perm have this form. */
+typedef struct {
+    const int32_t* offsets;   /* device [E+1]: group e is rows offsets[e] .. offsets[e+1]; 0 first, never falling, at most
+                                 M (rows behind the last group: results are 0).  Never read by the host; values
+                                 that break this give wrong results, but no access out of bounds  */
+    const int32_t* perm;      /* device [M] or NULL: row r of the groups is row perm[r] / k of the tensor `in`
+                                 (moe_product, moe_product_grad_weight; NULL elsewhere)           */
+    int32_t k;                /* with perm: uses of a row (1: perm[r] is the row itself)         */
+    int32_t rows;             /* with perm: rows of `in` (perm is kept within them)              */
+} moe_groups;
+
+/* All tensors on the device; a row's elements lie side by side, and rows `..._stride` elements apart (at least their length).
+ *   in    [M or groups->rows][K] bf16     W [E][N][K] bf16, dense     out, dout [M][N] bf16
+ *   act, din [M][K] bf16                  dW [E][N][K] grad_dtype (DYNB_F32 or DYNB_BF16), dense
+ * Results may not overlap with what is read.  Any sizes and addresses are accepted; K and N that are multiples of 8 with
+ * rows on 16-byte borders run the fast kernels.  Nothing is read back and nothing waits on the host.  Sums are in a fixed order: equal calls
+ * give equal bits.
+ * Errors: DYNB_E_INVAL (NULL, sizes <= 0, strides below a row's length, misaligned), DYNB_E_UNSUPPORTED (dtype, flag, more
+ * than 2^30 rows, 2^22 channels, 2^20 experts or 2^24 tiles of results), DYNB_E_WORKSPACE, DYNB_E_HIP.  */
+int moe_product(const moe_product_shape* shape, const moe_groups* groups, const void* in, int64_t in_stride,
+                const void* W, void* out, int64_t out_stride, void* stream);
+int moe_product_grad_input(const moe_product_shape* shape, const moe_groups* groups, const void* dout, int64_t dout_stride,
+                           const void* W, const void* act, int64_t act_stride, void* din, int64_t din_stride, void* stream);
+/* workspace: device, >= moe_product_grad_weight_workspace_bytes, 256-byte aligned, scratch       */
+size_t moe_product_grad_weight_workspace_bytes(const moe_product_shape* shape);
+int moe_product_grad_weight(const moe_product_shape* shape, const moe_groups* groups, const void* dout, int64_t dout_stride,
+                            const void* in, int64_t in_stride, void* dW, int32_t grad_dtype, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/* Token embeddings: out[t] = scale * table[tokens[t]], and the gradient of the table,
+ * dtable[v] = scale * sum over t with tokens[t] = v of dout[t].  A token outside [0, V), such as a padding of -1, has a
+ * row of zeros and gives no gradient.                                                            */
+typedef struct {
+    int32_t T;                /* tokens (0: no work; the gradient is 0)                          */
+    int32_t V;                /* rows of the table                                               */
+    int32_t d;                /* width                                                           */
+    int32_t dtype;            /* DYNB_F32 or DYNB_BF16: table, out and dout (sums are fp32)      */
+    float scale;
+} dynb_embed_shape;
+
+/*   tokens device [T]   table device [V][d] dtype, dense   out device [T][d] dtype, rows out_stride elements apart
+ * Errors: DYNB_E_INVAL (NULL, sizes <= 0, out_stride < d, misaligned), DYNB_E_UNSUPPORTED (dtype), DYNB_E_HIP.       */
+int dynb_embed(const dynb_embed_shape* shape, const int32_t* tokens, const void* table, void* out, int64_t out_stride,
+               void* stream);
+/*   dout device [T][d] dtype, rows dout_stride elements apart; dtable device [V][d] grad_dtype (DYNB_F32 or DYNB_BF16), dense: every
+ *   row is written; workspace device, >= dynb_embed_backward_workspace_bytes, 256-byte aligned, scratch.
+ * A row's sum runs over its tokens in their order, in pieces whose borders depend on the tokens only: equal calls give equal bits.
+ * Errors as dynb_embed, and DYNB_E_WORKSPACE.                                                    */
+size_t dynb_embed_backward_workspace_bytes(const dynb_embed_shape* shape);
+int dynb_embed_backward(const dynb_embed_shape* shape, const int32_t* tokens, const void* dout, int64_t dout_stride,
+                        void* dtable, int32_t grad_dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Layer norm of rows: m = mean(x), r = 1 / sqrt(mean((x - m)^2) + eps), y = (x - m) r gamma + beta.
+ * Backward, g = dy gamma, h = (x - m) r: dx = r (g - mean(g) - h mean(g h)), dgamma = sum over rows of dy h,
+ * dbeta = sum over rows of dy.                                                                   */
+typedef struct {
+    int32_t T;                /* rows (0: no work; dgamma and dbeta are 0)                       */
+    int32_t d;                /* width                                                           */
+    int32_t dtype;            /* DYNB_F32 or DYNB_BF16: x, y, dy, dx (sums and statistics are fp32) */
+    float eps;                /* >= 0                                                            */
+} dynb_norm_shape;
+
+/*   x, y, dy, dx device [T][d] dtype, rows `..._stride` elements apart (y may be x, dx may be dy or x, with the same stride)
+ *   gamma, beta device [d] fp32, NULL: 1 and 0
+ *   mean, rstd  device [T] fp32: what the backward pass wants (moments of x); dynb_layer_norm: may be NULL
+ *   dx, dgamma, dbeta  may be NULL where they are not wanted; dgamma, dbeta device [d] fp32
+ *   workspace   device, >= dynb_layer_norm_backward_workspace_bytes, 256-byte aligned, scratch
+ * Errors: DYNB_E_INVAL (NULL, sizes <= 0, negative eps, strides below d, misaligned), DYNB_E_UNSUPPORTED (dtype),
+ * DYNB_E_WORKSPACE, DYNB_E_HIP.                                                                  */
+int dynb_layer_norm(const dynb_norm_shape* shape, const void* x, int64_t x_stride, const float* gamma, const float* beta,
+                    void* y, int64_t y_stride, float* mean, float* rstd, void* stream);
+size_t dynb_layer_norm_backward_workspace_bytes(const dynb_norm_shape* shape);
+int dynb_layer_norm_backward(const dynb_norm_shape* shape, const void* dy, int64_t dy_stride, const void* x, int64_t x_stride,
+                             const float* gamma, const float* mean, const float* rstd, void* dx, int64_t dx_stride,
+                             float* dgamma, float* dbeta, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The norm of many gradient tensors together, sqrt(sum of g^2), and the gradients scaled down to a largest one:
+ * out = g * max_norm / norm if norm is finite and above max_norm, else out = g.  (A norm that is not finite is for the
+ * caller to see, who will want to leave the step out.)  The squares are added up in fp64.        */
+typedef struct {
+    const void* grad;         /* device [count] dtype, dense                                     */
+    void* out;                /* device [count] dtype: grad itself or a tensor that overlaps with none; NULL: the tensor counts for the
+                                 norm only                                                       */
+    int64_t count;            /* elements; 0: nothing                                            */
+    int32_t dtype;            /* DYNB_F32 or DYNB_BF16                                           */
+} dynb_grad_tensor;
+
+/*   tensors  host [n], read before the call returns
+ *   norm     device, one float
+ *   workspace device, >= dynb_clip_workspace_bytes, 256-byte aligned, scratch
+ * Errors: DYNB_E_INVAL (NULL, negative sizes, max_norm not positive, misaligned), DYNB_E_UNSUPPORTED (dtype),
+ * DYNB_E_WORKSPACE, DYNB_E_HIP.                                                                  */
+size_t dynb_clip_workspace_bytes(void);
+int dynb_clip_gradients(const dynb_grad_tensor* tensors, int32_t n, float max_norm, float* norm, void* workspace,
+                        size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------------------------- */
 /* Per-stage timing (the paper reports "neural cell execution time" and "data stacking" apart   */

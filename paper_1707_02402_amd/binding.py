@@ -29,6 +29,10 @@ EXPORTS = ["dynb_last_error", "dynbatch_plan", "dynbatch_plan_dag", "dynbatch_pl
            "dynbatch_packed_weights_bytes", "dynbatch_pack_weights",
            "dynbatch_classify_workspace_bytes", "dynbatch_classify", "dynbatch_backward_workspace_bytes", "dynbatch_backward",
            "dynbatch_execute", "dynbatch_execute_check", "dynb_set_spin_limit", "moe_workspace_bytes", "moe_forward", "moe_forward_static", "moe_forward_naive",
+           "moe_product", "moe_product_grad_input", "moe_product_grad_weight_workspace_bytes", "moe_product_grad_weight",
+           "dynb_embed", "dynb_embed_backward_workspace_bytes", "dynb_embed_backward",
+           "dynb_layer_norm", "dynb_layer_norm_backward_workspace_bytes", "dynb_layer_norm_backward",
+           "dynb_clip_workspace_bytes", "dynb_clip_gradients",
            "dynb_timing_enable", "dynb_probe_mfma_bf16", "dynb_probe_copy", "dynb_probe_read",
            "dynb_timing_read"]
 
@@ -86,6 +90,26 @@ class _MoeAux(ct.Structure):
     _fields_ = [(n, ct.c_void_p) for n in ("logits", "topk_idx", "topk_w", "counts", "offsets", "perm", "inv")]
 
 
+class _ProductShape(ct.Structure):
+    _fields_ = [(n, ct.c_int32) for n in ("M", "K", "N", "E", "dtype")] + [("flags", ct.c_uint32)]
+
+
+class _Groups(ct.Structure):
+    _fields_ = [("offsets", ct.c_void_p), ("perm", ct.c_void_p), ("k", ct.c_int32), ("rows", ct.c_int32)]
+
+
+class _EmbedShape(ct.Structure):
+    _fields_ = [(n, ct.c_int32) for n in ("T", "V", "d", "dtype")] + [("scale", ct.c_float)]
+
+
+class _NormShape(ct.Structure):
+    _fields_ = [(n, ct.c_int32) for n in ("T", "d", "dtype")] + [("eps", ct.c_float)]
+
+
+class _GradTensor(ct.Structure):
+    _fields_ = [("grad", ct.c_void_p), ("out", ct.c_void_p), ("count", ct.c_int64), ("dtype", ct.c_int32)]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is missing: build it first (python -c 'import __graft_entry__ as g; g.build()')")
@@ -126,6 +150,24 @@ def _load():
                               ct.c_void_p, ct.c_void_p, ct.POINTER(_MoeAux), ct.c_void_p, ct.c_size_t, ct.c_void_p]
     L.moe_forward_naive.argtypes = L.moe_forward.argtypes + [ct.c_int32]
     L.moe_forward_static.argtypes = L.moe_forward.argtypes[:9] + [ct.c_void_p]
+    VP, I64, SZ = ct.c_void_p, ct.c_int64, ct.c_size_t
+    PS, GR, ES, NS = (ct.POINTER(t) for t in (_ProductShape, _Groups, _EmbedShape, _NormShape))
+    L.moe_product.argtypes = [PS, GR, VP, I64, VP, VP, I64, VP]
+    L.moe_product_grad_input.argtypes = [PS, GR, VP, I64, VP, VP, I64, VP, I64, VP]
+    L.moe_product_grad_weight_workspace_bytes.argtypes = [PS]
+    L.moe_product_grad_weight_workspace_bytes.restype = SZ
+    L.moe_product_grad_weight.argtypes = [PS, GR, VP, I64, VP, I64, VP, ct.c_int32, VP, SZ, VP]
+    L.dynb_embed.argtypes = [ES, VP, VP, VP, I64, VP]
+    L.dynb_embed_backward_workspace_bytes.argtypes = [ES]
+    L.dynb_embed_backward_workspace_bytes.restype = SZ
+    L.dynb_embed_backward.argtypes = [ES, VP, VP, I64, VP, ct.c_int32, VP, SZ, VP]
+    L.dynb_layer_norm.argtypes = [NS, VP, I64, VP, VP, VP, I64, VP, VP, VP]
+    L.dynb_layer_norm_backward_workspace_bytes.argtypes = [NS]
+    L.dynb_layer_norm_backward_workspace_bytes.restype = SZ
+    L.dynb_layer_norm_backward.argtypes = [NS, VP, I64, VP, I64, VP, VP, VP, VP, I64, VP, VP, VP, SZ, VP]
+    L.dynb_clip_workspace_bytes.argtypes = []
+    L.dynb_clip_workspace_bytes.restype = SZ
+    L.dynb_clip_gradients.argtypes = [ct.POINTER(_GradTensor), ct.c_int32, ct.c_float, VP, VP, SZ, VP]
     L.dynb_probe_mfma_bf16.argtypes = [ct.c_int32, ct.c_int32, ct.c_void_p, ct.c_void_p, ct.POINTER(ct.c_double)]
     L.dynb_probe_copy.argtypes = [ct.c_void_p, ct.c_void_p, ct.c_size_t, ct.c_void_p]
     L.dynb_probe_read.argtypes = [ct.c_void_p, ct.c_size_t, ct.c_void_p, ct.c_void_p]
@@ -487,6 +529,223 @@ def dynb_moe_kernels(T: int, d: int, h: int, E: int, k: int, noisy: bool = False
     if bits < 0:
         _check(bits)
     return {name for i, name in enumerate(MOE_KERNELS) if bits >> i & 1}
+
+
+# ------------------------------------------------------------------------------------------ products grouped by expert
+MOE_PRODUCT_RELU = 1
+
+
+def _dtype_code(t) -> int:
+    import torch
+    if t.dtype == torch.float32:
+        return DYNB_F32
+    assert t.dtype == torch.bfloat16, t.dtype
+    return DYNB_BF16
+
+
+def _rows(t, n: int, width: int, like=None) -> int:
+    """Checks a tensor of n rows of `width` neighbouring elements; returns the elements from a row to the next."""
+    assert t.is_cuda and t.dim() == 2 and t.shape[0] == n and t.shape[1] == width and (width == 1 or t.stride(1) == 1), (t.shape, t.stride())
+    assert like is None or t.dtype == like.dtype
+    return t.stride(0) if n > 1 else max(t.stride(0), width)
+
+
+def _new(stream, *shape, like, dtype=None):
+    """An uninitialised result; where the work runs on another stream than the current one, the allocator is told."""
+    import torch
+    t = torch.empty(shape, dtype=dtype if dtype is not None else like.dtype, device=like.device)
+    if stream is not None and stream != torch.cuda.current_stream():
+        t.record_stream(stream)
+    return t
+
+
+def _groups_struct(offsets, perm, k: int, M: int, rows: int) -> _Groups:
+    import torch
+    assert offsets.is_cuda and offsets.is_contiguous() and offsets.dtype == torch.int32
+    assert perm is None or (perm.is_cuda and perm.is_contiguous() and perm.dtype == torch.int32 and perm.shape == (M,))
+    return _Groups(offsets.data_ptr(), None if perm is None else perm.data_ptr(), k, rows)
+
+
+def moe_product(x, W, offsets, perm=None, k: int = 1, relu: bool = False, out=None, stream=None):
+    """out[r] = f(x[row(r)] W_e^T) for the rows r of every group e.  x [rows,K], W [E,N,K] bf16; offsets [E+1] int32: group e is rows
+    offsets[e] .. offsets[e+1]; perm [M] int32: row(r) = perm[r] // k, None: row(r) = r (moe_forward's aux gives offsets and perm
+    in this form).  f: ReLU or nothing.  Returns out [M,N] bf16."""
+    import torch
+    E, N, K = W.shape
+    M = x.shape[0] if perm is None else perm.shape[0]
+    xs = _rows(x, x.shape[0], K)
+    assert W.is_cuda and W.is_contiguous() and W.dtype == x.dtype == torch.bfloat16 and offsets.shape == (E + 1,)
+    if out is None:
+        out = _new(stream, M, N, like=x)
+    os_ = _rows(out, M, N, x)
+    g = _groups_struct(offsets, perm, k, M, x.shape[0])
+    shape = _ProductShape(M, K, N, E, DYNB_BF16, MOE_PRODUCT_RELU if relu else 0)
+    _check(lib.moe_product(ct.byref(shape), ct.byref(g), x.data_ptr(), xs, W.data_ptr(), out.data_ptr(), os_, _stream(stream)))
+    return out
+
+
+def moe_product_grad_input(dout, W, offsets, act=None, out=None, stream=None):
+    """din[r] = dout[r] W_e for the rows r of every group e, set to 0 where `act` (the ReLU's results that the layer read, or None)
+    is not positive.  dout [M,N], W [E,N,K], act [M,K] bf16; offsets as in moe_product.  Returns din [M,K] bf16."""
+    import torch
+    E, N, K = W.shape
+    M = dout.shape[0]
+    ds = _rows(dout, M, N)
+    assert W.is_cuda and W.is_contiguous() and W.dtype == dout.dtype == torch.bfloat16 and offsets.shape == (E + 1,)
+    as_ = 0 if act is None else _rows(act, M, K, dout)
+    if out is None:
+        out = _new(stream, M, K, like=dout)
+    os_ = _rows(out, M, K, dout)
+    g = _groups_struct(offsets, None, 1, M, M)
+    shape = _ProductShape(M, K, N, E, DYNB_BF16, 0)
+    _check(lib.moe_product_grad_input(ct.byref(shape), ct.byref(g), dout.data_ptr(), ds, W.data_ptr(),
+                                      None if act is None else act.data_ptr(), as_, out.data_ptr(), os_, _stream(stream)))
+    return out
+
+
+def moe_product_grad_weight_workspace_bytes(M: int, K: int, N: int, E: int) -> int:
+    return int(lib.moe_product_grad_weight_workspace_bytes(ct.byref(_ProductShape(M, K, N, E, DYNB_BF16, 0))))
+
+
+def moe_product_grad_weight(dout, x, offsets, perm=None, k: int = 1, dW=None, grad_dtype: int = DYNB_F32, workspace=None, stream=None):
+    """dW_e = sum over the rows r of group e of dout[r]^T x[row(r)] (0 for an empty group).  dout [M,N], x [rows,K] bf16; offsets, perm and
+    k as in moe_product.  Returns dW [E,N,K] in grad_dtype (`dW`: such a tensor of an earlier call, float32 or bfloat16, to be overwritten)."""
+    import torch
+    M, N = dout.shape
+    K, E = x.shape[1], offsets.shape[0] - 1
+    ds, xs = _rows(dout, M, N), _rows(x, M if perm is None else x.shape[0], K, dout)
+    assert dout.dtype == torch.bfloat16
+    if dW is None:
+        dW = _new(stream, E, N, K, like=x, dtype=torch.float32 if grad_dtype == DYNB_F32 else torch.bfloat16)
+    assert dW.is_cuda and dW.is_contiguous() and dW.shape == (E, N, K)
+    g = _groups_struct(offsets, perm, k, M, x.shape[0])
+    shape = _ProductShape(M, K, N, E, DYNB_BF16, 0)
+    if workspace is None:
+        workspace = _scratch(lib.moe_product_grad_weight_workspace_bytes(ct.byref(shape)), x.device, stream)
+    _check(lib.moe_product_grad_weight(ct.byref(shape), ct.byref(g), dout.data_ptr(), ds, x.data_ptr(), xs, dW.data_ptr(), _dtype_code(dW),
+                                       workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream)))
+    return dW
+
+
+# ------------------------------------------------------------------------------------------ embeddings
+def dynb_embed(tokens, table, scale: float = 1.0, out=None, stream=None):
+    """out[t] = scale * table[tokens[t]], a row of zeros for a token outside [0, V).  tokens [T] int32, table [V,d] float32 or bfloat16
+    (device, contiguous).  Returns out [T,d] in the table's dtype."""
+    import torch
+    T, (V, d) = tokens.shape[0], table.shape
+    assert tokens.is_cuda and tokens.is_contiguous() and tokens.dtype == torch.int32 and tokens.dim() == 1
+    assert table.is_cuda and table.is_contiguous()
+    if out is None:
+        out = _new(stream, T, d, like=table)
+    os_ = _rows(out, T, d, table)
+    shape = _EmbedShape(T, V, d, _dtype_code(table), scale)
+    _check(lib.dynb_embed(ct.byref(shape), tokens.data_ptr(), table.data_ptr(), out.data_ptr(), os_, _stream(stream)))
+    return out
+
+
+def dynb_embed_backward_workspace_bytes(T: int, V: int, d: int, dtype: int) -> int:
+    return int(lib.dynb_embed_backward_workspace_bytes(ct.byref(_EmbedShape(T, V, d, dtype, 1.0))))
+
+
+def dynb_embed_backward(tokens, dout, V: int, scale: float = 1.0, dtable=None, grad_dtype: int = DYNB_F32, workspace=None, stream=None):
+    """dtable[v] = scale * sum over t with tokens[t] = v of dout[t], every row written.  dout [T,d] float32 or bfloat16.  Returns dtable
+    [V,d] in grad_dtype (`dtable`: such a tensor of an earlier call, float32 or bfloat16, to be overwritten)."""
+    import torch
+    T, d = dout.shape
+    assert tokens.is_cuda and tokens.is_contiguous() and tokens.dtype == torch.int32 and tokens.shape == (T,)
+    ds = _rows(dout, T, d)
+    if dtable is None:
+        dtable = _new(stream, V, d, like=dout, dtype=torch.float32 if grad_dtype == DYNB_F32 else torch.bfloat16)
+    assert dtable.is_cuda and dtable.is_contiguous() and dtable.shape == (V, d)
+    shape = _EmbedShape(T, V, d, _dtype_code(dout), scale)
+    if workspace is None:
+        workspace = _scratch(lib.dynb_embed_backward_workspace_bytes(ct.byref(shape)), dout.device, stream)
+    _check(lib.dynb_embed_backward(ct.byref(shape), tokens.data_ptr(), dout.data_ptr(), ds, dtable.data_ptr(), _dtype_code(dtable),
+                                   workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream)))
+    return dtable
+
+
+# ------------------------------------------------------------------------------------------ layer norm
+def _fp32(t, n: int):
+    import torch
+    assert t is None or (t.is_cuda and t.is_contiguous() and t.dtype == torch.float32 and t.shape == (n,))
+    return None if t is None else t.data_ptr()
+
+
+def dynb_layer_norm(x, gamma=None, beta=None, eps: float = 1e-5, out=None, want_stats: bool = False, stream=None):
+    """Layer norm of the rows of x [T,d] (float32 or bfloat16); gamma, beta [d] float32 or None.  Returns y in the dtype of x, or
+    (y, mean, rstd), mean and rstd [T] float32, if the backward pass will want them."""
+    import torch
+    T, d = x.shape
+    xs = _rows(x, T, d)
+    if out is None:
+        out = _new(stream, T, d, like=x)
+    ys = _rows(out, T, d, x)
+    mean = _new(stream, T, like=x, dtype=torch.float32) if want_stats else None
+    rstd = _new(stream, T, like=x, dtype=torch.float32) if want_stats else None
+    shape = _NormShape(T, d, _dtype_code(x), eps)
+    _check(lib.dynb_layer_norm(ct.byref(shape), x.data_ptr(), xs, _fp32(gamma, d), _fp32(beta, d), out.data_ptr(), ys, _fp32(mean, T), _fp32(rstd, T),
+                               _stream(stream)))
+    return (out, mean, rstd) if want_stats else out
+
+
+def dynb_layer_norm_backward_workspace_bytes(T: int, d: int, dtype: int) -> int:
+    return int(lib.dynb_layer_norm_backward_workspace_bytes(ct.byref(_NormShape(T, d, dtype, 0.0))))
+
+
+def dynb_layer_norm_backward(dy, x, gamma, mean, rstd, dx=None, workspace=None, stream=None):
+    """Gradients of dynb_layer_norm: dy, x [T,d], mean and rstd what it returned.  Returns (dx [T,d] in the dtype of x, dgamma [d], dbeta [d]
+    float32)."""
+    import torch
+    T, d = x.shape
+    xs, ds = _rows(x, T, d), _rows(dy, T, d, x)
+    if dx is None:
+        dx = _new(stream, T, d, like=x)
+    dxs = _rows(dx, T, d, x)
+    dgamma, dbeta = _new(stream, d, like=x, dtype=torch.float32), _new(stream, d, like=x, dtype=torch.float32)
+    shape = _NormShape(T, d, _dtype_code(x), 0.0)
+    if workspace is None:
+        workspace = _scratch(lib.dynb_layer_norm_backward_workspace_bytes(ct.byref(shape)), x.device, stream)
+    _check(lib.dynb_layer_norm_backward(ct.byref(shape), dy.data_ptr(), ds, x.data_ptr(), xs, _fp32(gamma, d), _fp32(mean, T), _fp32(rstd, T), dx.data_ptr(), dxs,
+                                        dgamma.data_ptr(), dbeta.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                                        _stream(stream)))
+    return dx, dgamma, dbeta
+
+
+# ------------------------------------------------------------------------------------------ clipping
+class GradTensors:
+    """A network's gradient tensors (device, contiguous, float32 or bfloat16) and where the clipped ones go (None: into the gradients
+    themselves), marshalled once for the steps in which they stay where they are.  Keeps the tensors alive."""
+
+    def __init__(self, grads, out=None):
+        self.grads = list(grads)
+        self.out = self.grads if out is None else list(out)
+        assert len(self.grads) == len(self.out)
+        for g, o in zip(self.grads, self.out):
+            assert g.is_cuda and g.is_contiguous() and o.is_cuda and o.is_contiguous() and o.dtype == g.dtype and o.numel() == g.numel()
+        self.array = (_GradTensor * max(len(self.grads), 1))(*[(g.data_ptr(), o.data_ptr(), g.numel(), _dtype_code(g)) for g, o in zip(self.grads, self.out)])
+
+
+def dynb_clip_workspace_bytes() -> int:
+    return int(lib.dynb_clip_workspace_bytes())
+
+
+def dynb_clip_gradients(grads, max_norm: float, norm=None, workspace=None, stream=None):
+    """Scales the gradients (a list of tensors, in place, or a GradTensors) down to a norm of all of them together of max_norm, if that norm is
+    finite and above it.  Returns the norm they had: one float32 on the device."""
+    import torch
+    t = grads if isinstance(grads, GradTensors) else GradTensors(grads)
+    device = t.grads[0].device if t.grads else torch.device("cuda", torch.cuda.current_device())
+    if norm is None:
+        norm = torch.empty((), dtype=torch.float32, device=device)
+        if stream is not None and stream != torch.cuda.current_stream():
+            norm.record_stream(stream)
+    assert norm.is_cuda and norm.dtype == torch.float32 and norm.numel() == 1
+    if workspace is None:
+        workspace = _scratch(lib.dynb_clip_workspace_bytes(), device, stream)
+    _check(lib.dynb_clip_gradients(t.array, len(t.grads), max_norm, norm.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                                   _stream(stream)))
+    return norm
 
 
 # ------------------------------------------------------------------------------------------ timing
