@@ -5,22 +5,226 @@
 
 #include <algorithm>
 #include <string>
+#include <type_traits>
 
 #include "device_utils.h"
 #include "plan_internal.h"
+#include "rows.h"
 
 using dynb::fail;
 
 namespace {
 
-__device__ __forceinline__ float wave_sum(float v)
+// A lane keeps up to 16 elements of a row, so that it is read once: the mean, then the squares of what differs from it, from registers.  Rows of up to
+// 1024 elements are a wave's each, up to 16384 a workgroup's of 4 or 16 waves.  Longer ones are read three times (k_norm_long and its like).
+constexpr int LANE = 16;
+
+// the sum over a row's waves (WAVES > 1: all threads call it, `room` is free)
+template <int WAVES>
+__device__ __forceinline__ float row_sum(float v, float* room)
 {
+    v = wave_sum(v);
+    if constexpr (WAVES > 1) {
+        if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = 0.f;
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+        for (int i = 0; i < WAVES; ++i) v += room[i];
+    }
     return v;
 }
 
-// of all 256 threads
+template <typename T, int NV, int WAVES>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void k_norm(const T* x, int64_t x_stride, const float* __restrict__ gamma, const float* __restrict__ beta, T* y,
+                                                                        int64_t y_stride, float* __restrict__ mean, float* __restrict__ rstd, int n, int d, float eps)
+{
+    constexpr int P = PIECE<T>, NL = WAVES * 64;               // lanes of a row
+    __shared__ float room[2][WAVES > 1 ? WAVES : 1];
+    const int row = WAVES == 1 ? int(blockIdx.x) * 4 + int(threadIdx.x >> 6) : int(blockIdx.x);
+    if (row >= n) return;
+    const int lane = threadIdx.x & (NL - 1);
+    const T* const from = x + row * x_stride;
+    u32x4 raw[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) raw[i] = load_piece(from + (i * NL + lane) * P, d - (i * NL + lane) * P);
+    float v[NV][P], s = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < P; ++j) s += v[i][j] = element<T>(raw[i], j);
+    const float m = row_sum<WAVES>(s, room[0]) / float(d);
+    s = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < P; ++j) {
+            v[i][j] -= m;
+            if ((i * NL + lane) * P + j < d) s += v[i][j] * v[i][j];
+        }
+    const float r = 1.f / sqrtf(row_sum<WAVES>(s, room[1]) / float(d) + eps);
+    T* const to = y + row * y_stride;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (i * NL + lane) * P, left = d - c;
+        float w[P];
+#pragma unroll
+        for (int j = 0; j < P; ++j) w[j] = v[i][j] * r;
+        if (gamma) {
+#pragma unroll
+            for (int h = 0; h < P; h += 4) {
+                const u32x4 g = load_piece(gamma + c + h, left - h);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[h + j] *= element<float>(g, j);
+            }
+        }
+        if (beta) {
+#pragma unroll
+            for (int h = 0; h < P; h += 4) {
+                const u32x4 b = load_piece(beta + c + h, left - h);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[h + j] += element<float>(b, j);
+            }
+        }
+        store_piece<P>(to + c, left, w);
+    }
+    if (lane == 0) {
+        if (mean) mean[row] = m;
+        if (rstd) rstd[row] = r;
+    }
+}
+
+// The backward pass reads dy and x once: a lane has the same columns of every row that its wave (workgroup) goes through and adds up their share of the
+// parameters' gradients in registers.  A workgroup's shares are added in LDS and leave as one line of `partial` ([workgroup][2][d]), which k_norm_join adds up,
+// so that every sum has one order.  The next row is on its way while one is worked on.
+template <typename T, int NV, int WAVES>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void k_norm_grad(const T* dy, int64_t dy_stride, const T* x, int64_t x_stride, const float* __restrict__ gamma,
+                                                                             const float* __restrict__ mean, const float* __restrict__ rstd, T* dx, int64_t dx_stride,
+                                                                             float* __restrict__ partial, int n, int d)
+{
+    constexpr int P = PIECE<T>, NL = WAVES * 64, AT_ONCE = WAVES == 1 ? 4 : 1;
+    __shared__ float room[2][2][WAVES > 1 ? WAVES : 1];
+    __shared__ float share[WAVES == 1 ? 3 : 1][WAVES == 1 ? 64 * NV * P : 1];
+    const int lane = threadIdx.x & (NL - 1), wave = threadIdx.x >> 6;
+    float g_[NV][P], dg[NV][P], db[NV][P];
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int h = 0; h < P; h += 4) {
+            const int c = (i * NL + lane) * P + h;
+            const u32x4 g = gamma ? load_piece(gamma + c, d - c) : u32x4{0x3f800000u, 0x3f800000u, 0x3f800000u, 0x3f800000u};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                g_[i][h + j] = element<float>(g, j);
+                dg[i][h + j] = db[i][h + j] = 0.f;
+            }
+        }
+    const int step = int(gridDim.x) * AT_ONCE;
+    u32x4 a[NV], b[NV];
+    float m = 0.f, r = 0.f;
+    auto load = [&](int64_t row) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * NL + lane) * P;
+            a[i] = load_piece(dy + row * dy_stride + c, d - c);
+            b[i] = load_piece(x + row * x_stride + c, d - c);
+        }
+        m = mean[row];
+        r = rstd[row];
+    };
+    int64_t row = int(blockIdx.x) * AT_ONCE + (WAVES == 1 ? wave : 0);
+    if (row < n) load(row);
+    int turn = 0;
+    for (; row < n; row += step) {
+        float v[NV][P], h[NV][P], s1 = 0.f, s2 = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int j = 0; j < P; ++j) {
+                const bool on = (i * NL + lane) * P + j < d;   // (what lies behind the row must not count, whatever mean and rstd are)
+                h[i][j] = on ? (element<T>(b[i], j) - m) * r : 0.f;
+                const float y = element<T>(a[i], j);
+                dg[i][j] += y * h[i][j];
+                db[i][j] += y;
+                v[i][j] = y * g_[i][j];
+                s1 += v[i][j];
+                s2 += v[i][j] * h[i][j];
+            }
+        const float r0 = r;
+        const int64_t here = row;
+        if (WAVES < 16 && row < n - step) load(row + step);
+        if constexpr (WAVES == 1) {
+            s1 = wave_sum(s1);
+            s2 = wave_sum(s2);
+        } else {
+            // (one meeting for both; the next row's sums lie in the other half)
+            s1 = wave_sum(s1);
+            s2 = wave_sum(s2);
+            if ((threadIdx.x & 63) == 0) { room[turn][0][wave] = s1; room[turn][1][wave] = s2; }
+            __syncthreads();
+            s1 = s2 = 0.f;
+#pragma unroll
+            for (int i = 0; i < WAVES; ++i) { s1 += room[turn][0][i]; s2 += room[turn][1][i]; }
+            turn ^= 1;
+        }
+        if (dx) {
+            const float m1 = s1 / float(d), m2 = s2 / float(d);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = (i * NL + lane) * P;
+#pragma unroll
+                for (int j = 0; j < P; ++j) v[i][j] = r0 * (v[i][j] - m1 - h[i][j] * m2);
+                store_piece<P>(dx + here * dx_stride + c, d - c, v[i]);
+            }
+        }
+        if (WAVES == 16 && row < n - step) load(row + step);   // (sixteen waves have half the registers: no room for two rows)
+    }
+    if (!partial) return;
+    float* const mine = partial + size_t(blockIdx.x) * 2 * size_t(d);
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        auto& sum = which ? db : dg;
+        if constexpr (WAVES == 1) {
+            __syncthreads();
+            if (wave > 0)
+#pragma unroll
+                for (int i = 0; i < NV * P; ++i) share[wave - 1][i * 64 + lane] = sum[i / P][i % P];
+            __syncthreads();
+            if (wave > 0) continue;
+#pragma unroll
+            for (int i = 0; i < NV * P; ++i) sum[i / P][i % P] = (sum[i / P][i % P] + share[0][i * 64 + lane]) + (share[1][i * 64 + lane] + share[2][i * 64 + lane]);
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * NL + lane) * P;
+            store_piece<P>(mine + size_t(which) * size_t(d) + c, d - c, sum[i]);
+        }
+    }
+}
+
+// dgamma and dbeta, as they lie one behind the other in a line of `partial`
+__global__ __launch_bounds__(1024) void k_norm_join(const float* __restrict__ partial, float* __restrict__ dgamma, float* __restrict__ dbeta, int lines, int d)
+{
+    __shared__ float room[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, per = (lines + 15) / 16;
+    const int64_t c = int64_t(blockIdx.x) * 64 + lane;
+    float s = 0.f;
+    if (c < 2 * int64_t(d)) {
+        const int end = min(lines, (wave + 1) * per);
+#pragma unroll 8
+        for (int i = wave * per; i < end; ++i) s += partial[int64_t(i) * 2 * d + c];
+    }
+    room[wave][lane] = s;
+    __syncthreads();
+    if (wave != 0 || c >= 2 * int64_t(d)) return;
+    s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s += room[i][lane];
+    if (c < d) { if (dgamma) dgamma[c] = s; }
+    else if (dbeta) dbeta[c - d] = s;
+}
+
+// ------------------------------------------------------------------------------------------ rows of more than 16384 elements
+// the sum over 256 threads
 __device__ __forceinline__ float group_sum(float v, float* room)
 {
     v = wave_sum(v);
@@ -31,8 +235,8 @@ __device__ __forceinline__ float group_sum(float v, float* room)
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void k_norm(const T* __restrict__ x, int64_t x_stride, const float* __restrict__ gamma, const float* __restrict__ beta,
-                                              T* __restrict__ y, int64_t y_stride, float* __restrict__ mean, float* __restrict__ rstd, int d, float eps)
+__global__ __launch_bounds__(256) void k_norm_long(const T* x, int64_t x_stride, const float* __restrict__ gamma, const float* __restrict__ beta,
+                                              T* y, int64_t y_stride, float* __restrict__ mean, float* __restrict__ rstd, int d, float eps)
 {
     __shared__ float room[4];
     const T* const from = x + int64_t(blockIdx.x) * x_stride;
@@ -52,8 +256,8 @@ __global__ __launch_bounds__(256) void k_norm(const T* __restrict__ x, int64_t x
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void k_norm_dx(const T* __restrict__ dy, int64_t dy_stride, const T* __restrict__ x, int64_t x_stride, const float* __restrict__ gamma,
-                                                 const float* __restrict__ mean, const float* __restrict__ rstd, T* __restrict__ dx, int64_t dx_stride, int d)
+__global__ __launch_bounds__(256) void k_norm_dx_long(const T* dy, int64_t dy_stride, const T* x, int64_t x_stride, const float* __restrict__ gamma,
+                                                 const float* __restrict__ mean, const float* __restrict__ rstd, T* dx, int64_t dx_stride, int d)
 {
     __shared__ float room[4];
     const int64_t t = blockIdx.x;
@@ -73,7 +277,7 @@ __global__ __launch_bounds__(256) void k_norm_dx(const T* __restrict__ dy, int64
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void k_norm_dparams(const T* __restrict__ dy, int64_t dy_stride, const T* __restrict__ x, int64_t x_stride, const float* __restrict__ mean,
+__global__ __launch_bounds__(256) void k_norm_dparams_long(const T* dy, int64_t dy_stride, const T* x, int64_t x_stride, const float* __restrict__ mean,
                                                       const float* __restrict__ rstd, float* __restrict__ dgamma, float* __restrict__ dbeta, int n, int d)
 {
     __shared__ float room[2][4][64];
@@ -101,6 +305,32 @@ int check(const dynb_norm_shape* s, const std::string& who)
     if (s->dtype != DYNB_F32 && s->dtype != DYNB_BF16) return fail(DYNB_E_UNSUPPORTED, who + ": unknown dtype");
     return DYNB_OK;
 }
+constexpr int64_t MOST_ROWS = 1 << 21;                         // of a launch (which has room for 2^32 threads)
+// pieces of a lane and waves of a row (0: long rows)
+int row_waves(int d) { return d <= 64 * LANE ? 1 : d <= 256 * LANE ? 4 : d <= 1024 * LANE ? 16 : 0; }
+template <typename T, typename F>
+void by_width(T in, int d, F&& launch)
+{
+    auto with = [&](auto waves) {
+        constexpr int W = decltype(waves)::value, P = PIECE<T>;
+        if (d <= W * 64 * P) launch(in, std::integral_constant<int, 1>{}, waves);
+        else if (P * 2 == LANE || d <= W * 64 * P * 2) launch(in, std::integral_constant<int, 2>{}, waves);
+        else launch(in, std::integral_constant<int, LANE / P>{}, waves);
+    };
+    switch (row_waves(d)) {
+    case 1: with(std::integral_constant<int, 1>{}); break;
+    case 4: with(std::integral_constant<int, 4>{}); break;
+    case 16: with(std::integral_constant<int, 16>{}); break;
+    default: launch(in, std::integral_constant<int, 1>{}, std::integral_constant<int, 0>{});
+    }
+}
+// workgroups of the backward pass, a line of partial sums each
+int grad_lines(const dynb_norm_shape* s)
+{
+    const int waves = row_waves(s->d);
+    if (waves == 0) return 0;
+    return waves == 1 ? int(std::min<int64_t>((int64_t(s->T) + 3) / 4, 512)) : std::min(s->T, waves == 4 ? 512 : 256);
+}
 bool misaligned(const void* p, int dtype) { return (reinterpret_cast<uintptr_t>(p) & (dtype == DYNB_BF16 ? 1 : 3)) != 0; }
 
 }  // namespace
@@ -117,12 +347,23 @@ extern "C" int dynb_layer_norm(const dynb_norm_shape* s, const void* x, int64_t 
         misaligned(rstd, DYNB_F32))
         return fail(DYNB_E_INVAL, "dynb_layer_norm: misaligned pointer");
     hipStream_t st = static_cast<hipStream_t>(stream);
-    auto launch = [&](auto in) {
+    auto launch = [&](auto in, auto nv, auto waves) {
         using T = decltype(in);
-        hipLaunchKernelGGL((k_norm<T>), dim3(unsigned(s->T)), dim3(256), 0, st, static_cast<const T*>(x), x_stride, gamma, beta, static_cast<T*>(y), y_stride, mean, rstd, s->d, s->eps);
+        constexpr int NV = decltype(nv)::value, WAVES = decltype(waves)::value;
+        const T* const a = static_cast<const T*>(x);
+        T* const b = static_cast<T*>(y);
+        for (int64_t t = 0; t < s->T; t += MOST_ROWS) {
+            const int n = int(std::min<int64_t>(s->T - t, MOST_ROWS));
+            float *const m = mean ? mean + t : nullptr, *const r = rstd ? rstd + t : nullptr;
+            if constexpr (WAVES == 0)
+                hipLaunchKernelGGL((k_norm_long<T>), dim3(unsigned(n)), dim3(256), 0, st, a + t * x_stride, x_stride, gamma, beta, b + t * y_stride, y_stride, m, r, s->d, s->eps);
+            else
+                hipLaunchKernelGGL((k_norm<T, NV, WAVES>), dim3(unsigned(WAVES == 1 ? (n + 3) / 4 : n)), dim3(WAVES == 1 ? 256 : WAVES * 64), 0, st, a + t * x_stride, x_stride, gamma,
+                                   beta, b + t * y_stride, y_stride, m, r, n, s->d, s->eps);
+        }
     };
-    if (s->dtype == DYNB_BF16) launch(bf16_t{});
-    else launch(float{});
+    if (s->dtype == DYNB_BF16) by_width(bf16_t{}, s->d, launch);
+    else by_width(float{}, s->d, launch);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return fail(DYNB_E_HIP, std::string("dynb_layer_norm: ") + hipGetErrorString(e));
     return DYNB_OK;
@@ -131,7 +372,8 @@ extern "C" int dynb_layer_norm(const dynb_norm_shape* s, const void* x, int64_t 
 extern "C" size_t dynb_layer_norm_backward_workspace_bytes(const dynb_norm_shape* s)
 {
     if (check(s, "dynb_layer_norm_backward_workspace_bytes") != DYNB_OK) return 0;
-    return 256;
+    const size_t lines = size_t(grad_lines(s));
+    return std::max<size_t>(lines * 2 * size_t(s->d) * 4, 256);
 }
 
 extern "C" int dynb_layer_norm_backward(const dynb_norm_shape* s, const void* dy, int64_t dy_stride, const void* x, int64_t x_stride, const float* gamma, const float* mean,
@@ -147,15 +389,29 @@ extern "C" int dynb_layer_norm_backward(const dynb_norm_shape* s, const void* dy
         misaligned(rstd, DYNB_F32) || misaligned(dgamma, DYNB_F32) || misaligned(dbeta, DYNB_F32))
         return fail(DYNB_E_INVAL, "dynb_layer_norm_backward: misaligned pointer");
     hipStream_t st = static_cast<hipStream_t>(stream);
-    auto launch = [&](auto in) {
+    float* const partial = dgamma || dbeta ? static_cast<float*>(workspace) : nullptr;
+    const int lines = grad_lines(s);
+    auto launch = [&](auto in, auto nv, auto waves) {
         using T = decltype(in);
+        constexpr int NV = decltype(nv)::value, WAVES = decltype(waves)::value;
         const T *a = static_cast<const T*>(dy), *b = static_cast<const T*>(x);
-        if (dx && s->T > 0) hipLaunchKernelGGL((k_norm_dx<T>), dim3(unsigned(s->T)), dim3(256), 0, st, a, dy_stride, b, x_stride, gamma, mean, rstd, static_cast<T*>(dx), dx_stride, s->d);
+        T* const to = static_cast<T*>(dx);
+        if constexpr (WAVES > 0) {
+            if (lines > 0)
+                hipLaunchKernelGGL((k_norm_grad<T, NV, WAVES>), dim3(unsigned(lines)), dim3(WAVES == 1 ? 256 : WAVES * 64), 0, st, a, dy_stride, b, x_stride, gamma, mean, rstd, to,
+                                   dx_stride, partial, s->T, s->d);
+            if (partial) hipLaunchKernelGGL(k_norm_join, dim3(unsigned((2 * int64_t(s->d) + 63) / 64)), dim3(1024), 0, st, partial, dgamma, dbeta, lines, s->d);
+            return;
+        }
+        // (the parameters' first: dx may be dy or x)
         if (dgamma || dbeta)
-            hipLaunchKernelGGL((k_norm_dparams<T>), dim3(unsigned((s->d + 63) / 64)), dim3(256), 0, st, a, dy_stride, b, x_stride, mean, rstd, dgamma, dbeta, s->T, s->d);
+            hipLaunchKernelGGL((k_norm_dparams_long<T>), dim3(unsigned((s->d + 63) / 64)), dim3(256), 0, st, a, dy_stride, b, x_stride, mean, rstd, dgamma, dbeta, s->T, s->d);
+        for (int64_t t = 0; t < s->T && dx; t += MOST_ROWS)
+            hipLaunchKernelGGL((k_norm_dx_long<T>), dim3(unsigned(std::min<int64_t>(s->T - t, MOST_ROWS))), dim3(256), 0, st, a + t * dy_stride, dy_stride, b + t * x_stride, x_stride, gamma,
+                               mean + t, rstd + t, to + t * dx_stride, dx_stride, s->d);
     };
-    if (s->dtype == DYNB_BF16) launch(bf16_t{});
-    else launch(float{});
+    if (s->dtype == DYNB_BF16) by_width(bf16_t{}, s->d, launch);
+    else by_width(float{}, s->d, launch);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return fail(DYNB_E_HIP, std::string("dynb_layer_norm_backward: ") + hipGetErrorString(e));
     return DYNB_OK;
