@@ -517,7 +517,8 @@ typedef struct {
 } dynb_embed_shape;
 
 /*   tokens device [T]   table device [V][d] dtype, dense   out device [T][d] dtype, rows out_stride elements apart
- * Errors: DYNB_E_INVAL (NULL, sizes <= 0, out_stride < d, misaligned), DYNB_E_UNSUPPORTED (dtype), DYNB_E_HIP.       */
+ * Errors: DYNB_E_INVAL (NULL, sizes <= 0, out_stride < d, misaligned), DYNB_E_UNSUPPORTED (dtype, more than 2^25 tokens or 2^27
+ * rows), DYNB_E_HIP.                                                                             */
 int dynb_embed(const dynb_embed_shape* shape, const int32_t* tokens, const void* table, void* out, int64_t out_stride,
                void* stream);
 /*   dout device [T][d] dtype, rows dout_stride elements apart; dtable device [V][d] grad_dtype (DYNB_F32 or DYNB_BF16), dense: every
