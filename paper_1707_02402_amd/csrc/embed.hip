@@ -5,6 +5,7 @@
 
 #include <algorithm>
 #include <string>
+#include <type_traits>
 
 #include "device_utils.h"
 #include "plan_internal.h"
@@ -38,100 +39,102 @@ __global__ __launch_bounds__(256) void k_embed(const int32_t* __restrict__ token
 
 // ------------------------------------------------------------------------------------------ gradient of the table
 // The uses are brought into the order of their tokens (each token's in the order they stand in), so that a row's gradient is one sum, in one
-// order; a row without uses is a row of zeros.  A wave sums a row, 1024 columns at a time (16 a lane), and a workgroup's waves share the uses of
-// a row that has many.
-constexpr int SUM_LANE = 16, SUM_COLS = 64 * SUM_LANE;
+// order; a row without uses is a row of zeros.  A wave sums the columns of a row that it reads in pieces of 16 bytes a lane (512 of bfloat16; the launches' y
+// runs over the columns), and a workgroup's waves share the uses of a row that has many.
 constexpr int MANY = 64;                                       // uses of a row that are one wave's
+constexpr int AHEAD = 8;                                       // rows a wave has under way
 
-template <typename T>
+// E: elements of a lane's piece.  Sums that leave in fp32 are stored 16 bytes a lane, lane by lane, so bfloat16 is then read in pieces of 8 bytes (pieces of 16
+// would leave in two stores of 16 bytes of every 32: 50021 rows x 1024, each used once: 77 us instead of 66)
+template <typename T, int E>
 struct Sums {
-    static constexpr int P = PIECE<T>, NV = SUM_LANE / P;
-    float v[NV][P];
+    static constexpr int NV = PIECE<T> / E, COLS = 64 * PIECE<T>, STEP = 64 * E;
+    float v[NV][E];
     __device__ __forceinline__ void clear()
     {
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
-            for (int j = 0; j < P; ++j) v[i][j] = 0.f;
+            for (int j = 0; j < E; ++j) v[i][j] = 0.f;
     }
-    // the rows at(0) .. at(n - 1) of `rows`, from column c0 on
     template <int K, typename At>
-    __device__ __forceinline__ void add_some(const T* rows, int64_t stride, int c0, int d, int u, At&& at)
+    __device__ __forceinline__ void add_some(const T* rows, int64_t stride, int c, int d, int u, At&& at)
     {
-        const int c = c0 + int(threadIdx.x & 63) * P;
-        u32x4 raw[K][NV];
+        Piece<T, E> raw[K][NV];
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            const T* const p = rows + int64_t(at(u + k)) * stride;
+            const T* const p = rows + int64_t(at(u + k)) * stride + c;
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (c0 + i * 64 * P < d) raw[k][i] = load_piece(p + c + i * 64 * P, d - c - i * 64 * P);
+            for (int i = 0; i < NV; ++i) raw[k][i] = load_some<E>(p + i * STEP, d - c - i * STEP);
         }
 #pragma unroll
         for (int k = 0; k < K; ++k)
 #pragma unroll
             for (int i = 0; i < NV; ++i)
-                if (c0 + i * 64 * P < d)
 #pragma unroll
-                    for (int j = 0; j < P; ++j) v[i][j] += element<T>(raw[k][i], j);
+                for (int j = 0; j < E; ++j) v[i][j] += element<T>(raw[k][i], j);
     }
+    // this lane's columns, c .. and STEP further, of the rows at(0) .. at(n - 1)
     template <typename At>
-    __device__ __forceinline__ void add(const T* rows, int64_t stride, int c0, int d, int n, At&& at)
+    __device__ __forceinline__ void add(const T* rows, int64_t stride, int c, int d, int n, At&& at)
     {
         int u = 0;
-        for (; u + 4 <= n; u += 4) add_some<4>(rows, stride, c0, d, u, at);
-        for (; u < n; ++u) add_some<1>(rows, stride, c0, d, u, at);
+        for (; u + AHEAD <= n; u += AHEAD) add_some<AHEAD>(rows, stride, c, d, u, at);
+        if (u + AHEAD / 2 <= n) {
+            add_some<AHEAD / 2>(rows, stride, c, d, u, at);
+            u += AHEAD / 2;
+        }
+        if (u + 2 <= n) {
+            add_some<2>(rows, stride, c, d, u, at);
+            u += 2;
+        }
+        if (u < n) add_some<1>(rows, stride, c, d, u, at);
     }
-    // a row of sums in fp32
-    __device__ __forceinline__ void add_sums(const float* row, int c0, int d)
+    // n rows of sums in fp32, d apart
+    __device__ __forceinline__ void add_sums(const float* rows, int c, int d, int n)
     {
-        const int c = c0 + int(threadIdx.x & 63) * P;
+#pragma unroll 4
+        for (int u = 0; u < n; ++u)
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
+            for (int i = 0; i < NV; ++i)
 #pragma unroll
-            for (int h = 0; h < P; h += 4) {
-                const u32x4 raw = load_piece(row + c + i * 64 * P + h, d - c - i * 64 * P - h);
+                for (int h = 0; h < E; h += 4) {
+                    const u32x4 raw = load_piece(rows + size_t(u) * size_t(d) + c + i * STEP + h, d - c - i * STEP - h);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) v[i][h + j] += element<float>(raw, j);
-            }
+                    for (int j = 0; j < 4; ++j) v[i][h + j] += element<float>(raw, j);
+                }
     }
-    // the sums of all WAVES waves (a power of two), in wave 0: halves of the waves give theirs to the others, half of the columns at a time.  All threads call it.
+    // the sums of all WAVES waves (a power of two), in wave 0: half of the waves give theirs to the others, until one is left.  All threads call it.
     template <int WAVES>
-    __device__ __forceinline__ void join(float (*room)[SUM_COLS / 2], int wave)
+    __device__ __forceinline__ void join(float (*room)[COLS], int wave)
     {
         const int lane = threadIdx.x & 63;
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int half = WAVES / 2; half > 0; half >>= 1) {
+            __syncthreads();
+            if (wave >= half && wave < 2 * half)
 #pragma unroll
-            for (int half = WAVES / 2; half > 0; half >>= 1) {
-                __syncthreads();
-                if (wave >= half && wave < 2 * half)
+                for (int i = 0; i < NV * E; ++i) room[wave - half][i * 64 + lane] = v[i / E][i % E];
+            __syncthreads();
+            if (wave < half)
 #pragma unroll
-                    for (int i = 0; i < NV / 2; ++i)
-#pragma unroll
-                        for (int j = 0; j < P; ++j) room[wave - half][(i * P + j) * 64 + lane] = v[h * (NV / 2) + i][j];
-                __syncthreads();
-                if (wave < half)
-#pragma unroll
-                    for (int i = 0; i < NV / 2; ++i)
-#pragma unroll
-                        for (int j = 0; j < P; ++j) v[h * (NV / 2) + i][j] += room[wave][(i * P + j) * 64 + lane];
-            }
+                for (int i = 0; i < NV * E; ++i) v[i / E][i % E] += room[wave][i * 64 + lane];
+        }
         __syncthreads();
     }
     template <typename TG>
-    __device__ __forceinline__ void store(TG* row, int c0, int d, float scale)
+    __device__ __forceinline__ void store(TG* row, int c, int d, float scale)
     {
-        const int c = c0 + int(threadIdx.x & 63) * P;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            float w[P];
+            float w[E];
 #pragma unroll
-            for (int j = 0; j < P; ++j) w[j] = v[i][j] * scale;
-            if (c0 + i * 64 * P < d) store_piece<P>(row + c + i * 64 * P, d - c - i * 64 * P, w);
+            for (int j = 0; j < E; ++j) w[j] = v[i][j] * scale;
+            store_piece<E>(row + c + i * STEP, d - c - i * STEP, w);
         }
     }
 };
+template <typename T, typename TG> using SumsTo = Sums<T, std::is_same_v<TG, float> ? 4 : PIECE<T>>;
 
 // what this wave's lanes wrote to LDS is there for its other lanes
 __device__ __forceinline__ void wave_sync()
@@ -141,20 +144,21 @@ __device__ __forceinline__ void wave_sync()
 }
 __device__ __forceinline__ int lanes_below(uint64_t who) { return __popcll(who & ((1ull << (threadIdx.x & 63)) - 1)); }
 
-// Up to FEW tokens, one launch: every workgroup picks the uses of its 64 rows from all tokens, whose 32 KB it reads in less than the launches of a
+// Up to FEW tokens, one launch: every workgroup picks the uses of its rows (up to FEW_ROWS) from all tokens, whose 32 KB it reads in less than the launches of a
 // sort would take.
-constexpr int FEW = 8192, FEW_WAVES = 16, FEW_ROWS = 64, FEW_STEPS = FEW / (FEW_WAVES * 64);
+constexpr int FEW = 8192, FEW_WAVES = 16, FEW_ROWS = 128, FEW_STEPS = FEW / (FEW_WAVES * 64);
 
 template <typename T, typename TG>
-__global__ __launch_bounds__(FEW_WAVES * 64) void k_embed_grad_few(const int32_t* __restrict__ tokens, const T* __restrict__ dout, TG* __restrict__ dtable, int n, int V, int d,
-                                                                   int64_t dout_stride, float scale)
+__global__ __launch_bounds__(FEW_WAVES * 64, 8) void k_embed_grad_few(const int32_t* __restrict__ tokens, const T* __restrict__ dout, TG* __restrict__ dtable, int n, int V, int d,
+                                                                      int64_t dout_stride, float scale, int rows_each)
 {
-    __shared__ uint32_t uses[FEW];                             // place of the token * 64 + row, in the tokens' order
+    __shared__ uint32_t uses[FEW];                             // place of the token * FEW_ROWS + row, in the tokens' order
     __shared__ int32_t found[FEW_WAVES], count[FEW_ROWS];
     __shared__ uint32_t mine[FEW_WAVES][MANY];
-    __shared__ float room[FEW_WAVES / 2][SUM_COLS / 2];
+    using S = SumsTo<T, TG>;
+    __shared__ float room[FEW_WAVES / 2][S::COLS];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int v0 = int(blockIdx.x) * FEW_ROWS, rows = min(FEW_ROWS, V - v0);
+    const int v0 = int(blockIdx.x) * rows_each, rows = min(rows_each, V - v0);
     constexpr uint32_t NONE = 0xffffffffu;
     if (threadIdx.x < FEW_ROWS) count[threadIdx.x] = 0;
     // wave w looks through its sixteenth of the tokens
@@ -199,11 +203,11 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_embed_grad_few(const int32_t
             seen += __popcll(who);
         }
         wave_sync();
-        for (int c0 = 0; c0 < d; c0 += SUM_COLS) {
-            Sums<T> s;
+        for (int c = int(blockIdx.y) * S::COLS + lane * S::STEP / 64; c - lane * S::STEP / 64 < d; c += int(gridDim.y) * S::COLS) {
+            S s;
             s.clear();
-            s.add(dout, dout_stride, c0, d, k, [&](int u) { return __builtin_amdgcn_readfirstlane(mine[wave][u]); });
-            s.store(dtable + size_t(v0 + r) * size_t(d), c0, d, scale);
+            s.add(dout, dout_stride, c, d, k, [&](int u) { return __builtin_amdgcn_readfirstlane(mine[wave][u]); });
+            s.store(dtable + size_t(v0 + r) * size_t(d), c, d, scale);
         }
         wave_sync();
     }
@@ -211,8 +215,8 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_embed_grad_few(const int32_t
     for (int r = 0; r < rows; ++r) {
         if (count[r] <= MANY) continue;
         const int from = all * wave / FEW_WAVES, to = all * (wave + 1) / FEW_WAVES;
-        for (int c0 = 0; c0 < d; c0 += SUM_COLS) {
-            Sums<T> s;
+        for (int c = int(blockIdx.y) * S::COLS + lane * S::STEP / 64; c - lane * S::STEP / 64 < d; c += int(gridDim.y) * S::COLS) {
+            S s;
             s.clear();
             for (int u = from; u < to; u += 64) {
                 const uint32_t use = u + lane < to ? uses[u + lane] : NONE;
@@ -220,18 +224,21 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_embed_grad_few(const int32_t
                 const uint64_t who = __ballot(on);
                 if (on) mine[wave][lanes_below(who)] = use / FEW_ROWS;
                 wave_sync();
-                s.add(dout, dout_stride, c0, d, __popcll(who), [&](int i) { return __builtin_amdgcn_readfirstlane(mine[wave][i]); });
+                s.add(dout, dout_stride, c, d, __popcll(who), [&](int i) { return __builtin_amdgcn_readfirstlane(mine[wave][i]); });
                 wave_sync();
             }
             s.template join<FEW_WAVES>(room, wave);
-            if (wave == 0) s.store(dtable + size_t(v0 + r) * size_t(d), c0, d, scale);
+            if (wave == 0) s.store(dtable + size_t(v0 + r) * size_t(d), c, d, scale);
         }
     }
 }
 
 // More tokens: a stable sort by token, digit by digit (the last digit first), with two launches a digit: how often every digit value comes in every
-// block of tokens, and the tokens to their places.  At most SORT_BLOCKS blocks, so that a workgroup can add up what stands ahead of its own by itself.
-constexpr int SORT_BITS = 9, SORT_VALUES = 1 << SORT_BITS, SORT_BLOCKS = 128, SORT_STEP = 2048;
+// block of tokens, and the tokens to their places.  At most SORT_BLOCKS blocks, so that a workgroup can add up what stands ahead of its own by itself; its
+// sixteen waves keep the chains of dependent accesses short, of which such launches are made (65536 tokens: 34 us with four, 22 with sixteen).
+constexpr int SORT_BITS = 9, SORT_VALUES = 1 << SORT_BITS, SORT_BLOCKS = 128, SORT_WAVES = 16, SORT_STEPS = 2, SORT_STEP = SORT_WAVES * SORT_STEPS * 64;
+
+struct Range { int32_t begin, end; };                          // a row's sorted uses
 
 // the sort's key: the token, or V where it is outside the table
 __device__ __forceinline__ uint32_t key_of(const int32_t* tokens, const uint32_t* keys, int i, int V)
@@ -241,68 +248,89 @@ __device__ __forceinline__ uint32_t key_of(const int32_t* tokens, const uint32_t
     return t < uint32_t(V) ? t : uint32_t(V);
 }
 
-__global__ __launch_bounds__(256) void k_sort_count(const int32_t* __restrict__ tokens, const uint32_t* __restrict__ keys, int32_t* __restrict__ counts, int n, int per, int V,
-                                                    int shift, int bits)
+// (workgroups behind the blocks' clear the rows' ranges)
+__global__ __launch_bounds__(1024) void k_sort_count(const int32_t* __restrict__ tokens, const uint32_t* __restrict__ keys, int32_t* __restrict__ counts, int n, int per, int V,
+                                                     int shift, int bits, int blocks, Range* __restrict__ ranges)
 {
     __shared__ int32_t c[SORT_VALUES];
+    if (int(blockIdx.x) >= blocks) {
+        for (int v = (int(blockIdx.x) - blocks) * 1024 + int(threadIdx.x); v < V; v += (int(gridDim.x) - blocks) * 1024) ranges[v] = Range{0, 0};
+        return;
+    }
     const int values = 1 << bits;
-    for (int i = threadIdx.x; i < values; i += 256) c[i] = 0;
+    if (int(threadIdx.x) < values) c[threadIdx.x] = 0;
     __syncthreads();
     const int from = int(blockIdx.x) * per, to = min(n, from + per);
-#pragma unroll 8
-    for (int i = from + int(threadIdx.x); i < to; i += 256) atomicAdd(&c[key_of(tokens, keys, i, V) >> shift & uint32_t(values - 1)], 1);
+#pragma unroll 2
+    for (int i = from + int(threadIdx.x); i < to; i += 1024) atomicAdd(&c[key_of(tokens, keys, i, V) >> shift & uint32_t(values - 1)], 1);
     __syncthreads();
-    for (int i = threadIdx.x; i < values; i += 256) counts[size_t(blockIdx.x) * SORT_VALUES + i] = c[i];
+    if (int(threadIdx.x) < values) counts[size_t(blockIdx.x) * SORT_VALUES + threadIdx.x] = c[threadIdx.x];
 }
 
-__global__ __launch_bounds__(256) void k_sort_place(const int32_t* __restrict__ tokens, const uint32_t* __restrict__ keys, const int32_t* __restrict__ places,
-                                                    const int32_t* __restrict__ counts, uint32_t* __restrict__ keys_out, int32_t* __restrict__ places_out, int n, int per, int V,
-                                                    int shift, int bits, int blocks)
+__global__ __launch_bounds__(1024) void k_sort_place(const int32_t* __restrict__ tokens, const uint32_t* __restrict__ keys, const int32_t* __restrict__ places,
+                                                     const int32_t* __restrict__ counts, uint32_t* __restrict__ keys_out, int32_t* __restrict__ places_out, int n, int per, int V,
+                                                     int shift, int bits, int blocks)
 {
     __shared__ int32_t base[SORT_VALUES];                      // where the next key with this digit goes
-    __shared__ int32_t seen[4][SORT_VALUES];                   // of this step, by wave
-    __shared__ int32_t sums[4];
+    __shared__ int32_t half[2][SORT_VALUES];                   // all and those ahead, of the second half of the blocks
+    __shared__ int32_t seen[SORT_WAVES][SORT_VALUES];          // of this step, by wave; then how many the waves ahead have
+    __shared__ int32_t sums[SORT_VALUES / 64];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, values = 1 << bits;
-    // two digit values a thread: all that is below them, and what is in the blocks ahead
-    int32_t all[2] = {0, 0}, ahead[2] = {0, 0};
-#pragma unroll 8
-    for (int b = 0; b < blocks; ++b)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int32_t c = 2 * tid + i < values ? counts[size_t(b) * SORT_VALUES + 2 * tid + i] : 0;
-            all[i] += c;
-            ahead[i] += b < int(blockIdx.x) ? c : 0;
-        }
-    int32_t sum = all[0] + all[1];
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int32_t v = __shfl_up(sum, o);
-        sum += lane >= o ? v : 0;
-    }
-    if (lane == 63) sums[wave] = sum;
-    __syncthreads();
-    int32_t below = sum - all[0] - all[1];
-    for (int w = 0; w < wave; ++w) below += sums[w];
-    if (2 * tid < values) {
-        base[2 * tid] = below + ahead[0];
-        base[2 * tid + 1] = below + all[0] + ahead[1];
-    }
     const int from = int(blockIdx.x) * per, to = min(n, from + per);
-    for (int s0 = from; s0 < to; s0 += SORT_STEP) {
-        for (int i = tid; i < 4 * SORT_VALUES; i += 256) (&seen[0][0])[i] = 0;
-        __syncthreads();
-        uint32_t key[SORT_STEP / 256];
-        int32_t place[SORT_STEP / 256], rank[SORT_STEP / 256];
-        const int w0 = s0 + wave * (SORT_STEP / 4);
+    uint32_t key[SORT_STEPS];
+    int32_t place[SORT_STEPS], rank[SORT_STEPS];
+    auto load = [&](int s0) {
 #pragma unroll
-        for (int i = 0; i < SORT_STEP / 256; ++i) {
-            const int at = w0 + i * 64 + lane;
+        for (int i = 0; i < SORT_STEPS; ++i) {
+            const int at = s0 + (wave * SORT_STEPS + i) * 64 + lane;
             key[i] = at < to ? key_of(tokens, keys, at, V) : 0u;
             place[i] = at < to ? (places ? places[at] : at) : 0;
         }
+    };
+    load(from);
+    {
+        // half of the blocks a thread: how many of digit value v there are, and how many in the blocks ahead
+        const int v = tid & (SORT_VALUES - 1), h = tid / SORT_VALUES;
+        int32_t all = 0, ahead = 0;
+        if (v < values) {
+#pragma unroll 16
+            for (int b = h * ((blocks + 1) / 2); b < (h ? blocks : (blocks + 1) / 2); ++b) {
+                const int32_t c = counts[size_t(b) * SORT_VALUES + v];
+                all += c;
+                ahead += b < int(blockIdx.x) ? c : 0;
+            }
+        }
+        if (h) { half[0][v] = all; half[1][v] = ahead; }
+        for (int i = tid; i < SORT_WAVES * SORT_VALUES; i += 1024) (&seen[0][0])[i] = 0;
+        __syncthreads();
+        int32_t sum = 0;
+        if (!h) {
+            all += half[0][v];
+            ahead += half[1][v];
+            sum = all;
 #pragma unroll
-        for (int i = 0; i < SORT_STEP / 256; ++i) {
-            const bool on = w0 + i * 64 + lane < to;
+            for (int o = 1; o < 64; o <<= 1) {
+                const int32_t u = __shfl_up(sum, o);
+                sum += lane >= o ? u : 0;
+            }
+            if (lane == 63) sums[wave] = sum;
+        }
+        __syncthreads();
+        if (!h) {
+            int32_t below = sum - all;
+            for (int w = 0; w < wave; ++w) below += sums[w];
+            base[v] = below + ahead;
+        }
+    }
+    for (int s0 = from; s0 < to; s0 += SORT_STEP) {
+        if (s0 > from) {
+            load(s0);
+            for (int i = tid; i < SORT_WAVES * SORT_VALUES; i += 1024) (&seen[0][0])[i] = 0;
+            __syncthreads();
+        }
+#pragma unroll
+        for (int i = 0; i < SORT_STEPS; ++i) {
+            const bool on = s0 + (wave * SORT_STEPS + i) * 64 + lane < to;
             const uint32_t digit = key[i] >> shift & uint32_t(values - 1);
             uint64_t same = __ballot(on);                      // the lanes with this digit
             for (int b = 0; b < bits; ++b) {
@@ -319,116 +347,103 @@ __global__ __launch_bounds__(256) void k_sort_place(const int32_t* __restrict__ 
             wave_sync();
         }
         __syncthreads();
+        int32_t sum = 0;
+        if (tid < values) {
+            int32_t c[SORT_WAVES];
 #pragma unroll
-        for (int i = 0; i < SORT_STEP / 256; ++i)
-            if (w0 + i * 64 + lane < to) {
+            for (int w = 0; w < SORT_WAVES; ++w) c[w] = seen[w][tid];
+#pragma unroll
+            for (int w = 0; w < SORT_WAVES; ++w) { seen[w][tid] = sum; sum += c[w]; }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < SORT_STEPS; ++i)
+            if (s0 + (wave * SORT_STEPS + i) * 64 + lane < to) {
                 const uint32_t digit = key[i] >> shift & uint32_t(values - 1);
-                int32_t to_place = base[digit] + rank[i];
-                for (int w = 0; w < wave; ++w) to_place += seen[w][digit];
-                keys_out[to_place] = key[i];
-                places_out[to_place] = place[i];
+                const int32_t at = base[digit] + seen[wave][digit] + rank[i];
+                keys_out[at] = key[i];
+                places_out[at] = place[i];
             }
         __syncthreads();
-        for (int i = tid; i < values; i += 256) base[i] += seen[0][i] + seen[1][i] + seen[2][i] + seen[3][i];
-        __syncthreads();
+        if (tid < values) base[tid] += sum;
     }
 }
 
-// Chunks of CHUNK sorted uses that are all of one row: their sums, for rows with many uses
+// Chunks of CHUNK sorted uses: where a row's begin and end, and of those that are all of one row the sum, for rows with many uses
 constexpr int CHUNK = 64;
 
 template <typename T>
 __global__ __launch_bounds__(256) void k_embed_chunks(const uint32_t* __restrict__ keys, const int32_t* __restrict__ places, const T* __restrict__ dout, float* __restrict__ sums,
-                                                      int V, int d, int64_t dout_stride)
+                                                      Range* __restrict__ ranges, int n, int V, int d, int64_t dout_stride)
 {
-    __shared__ float room[2][SUM_COLS / 2];
-    const size_t u0 = size_t(blockIdx.x) * CHUNK;
-    if (keys[u0] != keys[u0 + CHUNK - 1] || keys[u0] >= uint32_t(V)) return;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int32_t mine = places[u0 + size_t(wave) * (CHUNK / 4) + (threadIdx.x & (CHUNK / 4 - 1))];
-    for (int c0 = 0; c0 < d; c0 += SUM_COLS) {
-        Sums<T> s;
+    using S = SumsTo<T, float>;
+    __shared__ float room[2][S::COLS];
+    const int u0 = int(blockIdx.x) * CHUNK, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int u = u0 + lane;
+    const uint32_t key = keys[min(u, n - 1)];
+    if (wave == 0 && blockIdx.y == 0 && u < n && key < uint32_t(V)) {
+        if (u == 0 || keys[u - 1] != key) ranges[key].begin = u;
+        if (u == n - 1 || keys[u + 1] != key) ranges[key].end = u + 1;
+    }
+    if (u0 + CHUNK > n || key >= uint32_t(V) || __ballot(key == uint32_t(__builtin_amdgcn_readfirstlane(key))) != ~0ull) return;
+    const int32_t mine = places[u0 + wave * (CHUNK / 4) + (lane & (CHUNK / 4 - 1))];
+    for (int c = int(blockIdx.y) * S::COLS + lane * S::STEP / 64; c - lane * S::STEP / 64 < d; c += int(gridDim.y) * S::COLS) {
+        S s;
         s.clear();
-        s.add(dout, dout_stride, c0, d, CHUNK / 4, [&](int u) { return __builtin_amdgcn_readlane(mine, u); });
+        s.add(dout, dout_stride, c, d, CHUNK / 4, [&](int i) { return __builtin_amdgcn_readlane(mine, i); });
         s.template join<4>(room, wave);
-        if (wave == 0) s.store(sums + size_t(blockIdx.x) * size_t(d), c0, d, 1.f);
+        if (wave == 0) s.store(sums + size_t(blockIdx.x) * size_t(d), c, d, 1.f);
     }
 }
 
-// the first sorted use whose key is not below `key`, among lo .. hi
-__device__ __forceinline__ int first_use(const uint32_t* keys, int lo, int hi, uint32_t key)
-{
-    while (lo < hi) {
-        const int mid = lo + (hi - lo) / 2;
-        if (keys[mid] < key) lo = mid + 1;
-        else hi = mid;
-    }
-    return lo;
-}
-
-constexpr int GRAD_ROWS = 32;                                  // rows of the table of a workgroup
+constexpr int GRAD_ROWS = 16;                                  // rows of the table of a workgroup
 
 template <typename T, typename TG>
-__global__ __launch_bounds__(256) void k_embed_grad(const uint32_t* __restrict__ keys, const int32_t* __restrict__ places, const T* __restrict__ dout,
-                                                    const float* __restrict__ sums, TG* __restrict__ dtable, int n, int V, int d, int64_t dout_stride, float scale)
+__global__ __launch_bounds__(256) void k_embed_grad(const Range* __restrict__ ranges, const int32_t* __restrict__ places, const T* __restrict__ dout,
+                                                    const float* __restrict__ sums, TG* __restrict__ dtable, int V, int d, int64_t dout_stride, float scale)
 {
-    __shared__ int32_t first[GRAD_ROWS + 1];
-    __shared__ int32_t mine[4][MANY];
-    __shared__ float room[2][SUM_COLS / 2];
+    using S = SumsTo<T, TG>;
+    __shared__ float room[2][S::COLS];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int v0 = int(blockIdx.x) * GRAD_ROWS, rows = min(GRAD_ROWS, V - v0);
-    if (wave == 0) {
-        // the rows' uses: 64 places of the list at a time narrow down where they begin, then every lane looks for a row
-        int lo = 0, hi = n;
-        while (hi - lo > 64) {
-            const int step = (hi - lo + 63) / 64, at = lo + lane * step;
-            const uint64_t less = __ballot(at < hi && keys[min(at, hi - 1)] < uint32_t(v0));
-            if (less == 0) { hi = lo; break; }
-            const int last = 63 - __builtin_clzll(less);
-            hi = min(hi, lo + (last + 1) * step);
-            lo += last * step;
-        }
-        const int begin = first_use(keys, lo, hi, uint32_t(v0));
-        int end = n;                                           // (of lane r's search: doubled until it is behind row v0 + r)
-        for (int64_t step = 64; begin + step < n; step *= 2)
-            if (keys[begin + step] >= uint32_t(v0 + rows)) { end = int(begin + step); break; }
-        if (lane <= rows) first[lane] = first_use(keys, begin, end, uint32_t(v0 + lane));
-    }
-    __syncthreads();
-    for (int r = wave; r < rows; r += 4) {
-        const int s0 = __builtin_amdgcn_readfirstlane(first[r]), k = __builtin_amdgcn_readfirstlane(first[r + 1]) - s0;
-        if (k > MANY) continue;
-        const int32_t use = lane < k ? places[s0 + lane] : 0;
-        for (int c0 = 0; c0 < d; c0 += SUM_COLS) {
-            Sums<T> s;
+    const Range mine = ranges[v0 + min(lane, rows - 1)];
+    const int k_mine = mine.end - mine.begin;
+    // rows with few uses: four neighbours a wave
+#pragma unroll
+    for (int i = 0; i < GRAD_ROWS / 4; ++i) {
+        const int r = wave * (GRAD_ROWS / 4) + i;
+        const int from = __builtin_amdgcn_readlane(mine.begin, r), k = __builtin_amdgcn_readlane(k_mine, r);
+        if (r >= rows || k > MANY) continue;
+        const int32_t use = lane < k ? places[from + lane] : 0;
+        for (int c = int(blockIdx.y) * S::COLS + lane * S::STEP / 64; c - lane * S::STEP / 64 < d; c += int(gridDim.y) * S::COLS) {
+            S s;
             s.clear();
-            s.add(dout, dout_stride, c0, d, k, [&](int u) { return __builtin_amdgcn_readlane(use, u); });
-            s.store(dtable + size_t(v0 + r) * size_t(d), c0, d, scale);
+            s.add(dout, dout_stride, c, d, k, [&](int u) { return __builtin_amdgcn_readlane(use, u); });
+            s.store(dtable + size_t(v0 + r) * size_t(d), c, d, scale);
         }
     }
-    for (int r = 0; r < rows; ++r) {
-        const int from = __builtin_amdgcn_readfirstlane(first[r]), to = __builtin_amdgcn_readfirstlane(first[r + 1]);
-        if (to - from <= MANY) continue;
-        // the uses ahead of the first whole chunk (wave 0), the chunks (a quarter each), the uses behind them (wave 3)
-        const int c_from = (from + CHUNK - 1) / CHUNK, chunks = to / CHUNK - c_from;
-        const int at = wave == 0 ? from : to / CHUNK * CHUNK, k = wave == 0 ? c_from * CHUNK - from : wave == 3 ? to - at : 0;
-        const int32_t use = lane < k ? places[at + lane] : 0;
-        for (int c0 = 0; c0 < d; c0 += SUM_COLS) {
-            Sums<T> s;
+    // rows with many: the whole chunks' sums, and the uses ahead of the first and behind the last of them (fewer than 2 * CHUNK), a quarter a wave
+    uint64_t many = __ballot(lane < rows && k_mine > MANY);
+    for (; many; many &= many - 1) {
+        const int r = __builtin_ctzll(many), from = __builtin_amdgcn_readlane(mine.begin, r), to = from + __builtin_amdgcn_readlane(k_mine, r);
+        const int c_from = (from + CHUNK - 1) / CHUNK, chunks = to / CHUNK - c_from, ahead = c_from * CHUNK - from, loose = ahead + to % CHUNK;
+        const int at = loose * wave / 4, k = loose * (wave + 1) / 4 - at, at_c = int(int64_t(chunks) * wave / 4), k_c = int(int64_t(chunks) * (wave + 1) / 4) - at_c;
+        const int i = at + lane;
+        const int32_t use = lane < k ? places[i < ahead ? from + i : to - to % CHUNK + i - ahead] : 0;
+        for (int c = int(blockIdx.y) * S::COLS + lane * S::STEP / 64; c - lane * S::STEP / 64 < d; c += int(gridDim.y) * S::COLS) {
+            S s;
             s.clear();
-            if (wave == 0) s.add(dout, dout_stride, c0, d, k, [&](int u) { return __builtin_amdgcn_readlane(use, u); });
-#pragma unroll 4
-            for (int c = int(int64_t(chunks) * wave / 4); c < int(int64_t(chunks) * (wave + 1) / 4); ++c) s.add_sums(sums + size_t(c_from + c) * size_t(d), c0, d);
-            if (wave == 3) s.add(dout, dout_stride, c0, d, k, [&](int u) { return __builtin_amdgcn_readlane(use, u); });
+            s.add_sums(sums + size_t(c_from + at_c) * size_t(d), c, d, k_c);
+            s.add(dout, dout_stride, c, d, k, [&](int u) { return __builtin_amdgcn_readlane(use, u); });
             s.template join<4>(room, wave);
-            if (wave == 0) s.store(dtable + size_t(v0 + r) * size_t(d), c0, d, scale);
+            if (wave == 0) s.store(dtable + size_t(v0 + r) * size_t(d), c, d, scale);
         }
     }
 }
 
 struct SortLayout {
     int per, blocks, passes, bits;                             // tokens of a block, blocks; digits, their bits
-    size_t counts, keys[2], places[2], sums, total;
+    size_t counts, keys[2], places[2], sums, ranges, total;
 };
 
 SortLayout sort_layout(const dynb_embed_shape* s)
@@ -450,6 +465,7 @@ SortLayout sort_layout(const dynb_embed_shape* s)
         L.places[i] = take(size_t(T) * 4);
     }
     L.sums = take(size_t(T / CHUNK) * size_t(s->d) * 4);
+    L.ranges = take(size_t(s->V) * sizeof(Range));
     L.total = o;
     return L;
 }
@@ -509,12 +525,14 @@ extern "C" int dynb_embed_backward(const dynb_embed_shape* s, const int32_t* tok
     char* const ws = static_cast<char*>(workspace);
     const uint32_t* keys = nullptr;
     const int32_t* places = nullptr;
+    Range* const ranges = reinterpret_cast<Range*>(ws + L.ranges);
     for (int i = 0; i < L.passes; ++i) {
         int32_t* const counts = reinterpret_cast<int32_t*>(ws + L.counts);
         uint32_t* const to = reinterpret_cast<uint32_t*>(ws + L.keys[i & 1]);
         int32_t* const places_to = reinterpret_cast<int32_t*>(ws + L.places[i & 1]);
-        hipLaunchKernelGGL(k_sort_count, dim3(unsigned(L.blocks)), dim3(256), 0, st, tokens, keys, counts, s->T, L.per, s->V, i * L.bits, L.bits);
-        hipLaunchKernelGGL(k_sort_place, dim3(unsigned(L.blocks)), dim3(256), 0, st, tokens, keys, places, counts, to, places_to, s->T, L.per, s->V, i * L.bits, L.bits, L.blocks);
+        const unsigned clearing = i == 0 ? unsigned(std::min(s->V / 1024 + 1, 512)) : 0u;
+        hipLaunchKernelGGL(k_sort_count, dim3(unsigned(L.blocks) + clearing), dim3(1024), 0, st, tokens, keys, counts, s->T, L.per, s->V, i * L.bits, L.bits, L.blocks, ranges);
+        hipLaunchKernelGGL(k_sort_place, dim3(unsigned(L.blocks)), dim3(1024), 0, st, tokens, keys, places, counts, to, places_to, s->T, L.per, s->V, i * L.bits, L.bits, L.blocks);
         keys = to;
         places = places_to;
     }
@@ -523,15 +541,17 @@ extern "C" int dynb_embed_backward(const dynb_embed_shape* s, const int32_t* tok
         using TG = decltype(grad);
         const T* const from = static_cast<const T*>(dout);
         TG* const to = static_cast<TG*>(dtable);
+        const unsigned tiles = unsigned(std::min((s->d - 1) / SumsTo<T, TG>::COLS + 1, 64));
         if (L.passes == 0) {
-            hipLaunchKernelGGL((k_embed_grad_few<T, TG>), dim3(unsigned((s->V + FEW_ROWS - 1) / FEW_ROWS)), dim3(FEW_WAVES * 64), 0, st, tokens, from, to, s->T, s->V, s->d, dout_stride,
-                               s->scale);
+            // two workgroups a CU, if the rows are not too many for that
+            const int rows = int(std::min<int64_t>(std::max<int64_t>((int64_t(s->V) * tiles + 511) / 512, 16), FEW_ROWS));
+            hipLaunchKernelGGL((k_embed_grad_few<T, TG>), dim3(unsigned((s->V + rows - 1) / rows), tiles), dim3(FEW_WAVES * 64), 0, st, tokens, from, to, s->T, s->V, s->d, dout_stride,
+                               s->scale, rows);
             return;
         }
         float* const sums = reinterpret_cast<float*>(ws + L.sums);
-        hipLaunchKernelGGL((k_embed_chunks<T>), dim3(unsigned(s->T / CHUNK)), dim3(256), 0, st, keys, places, from, sums, s->V, s->d, dout_stride);
-        hipLaunchKernelGGL((k_embed_grad<T, TG>), dim3(unsigned((s->V + GRAD_ROWS - 1) / GRAD_ROWS)), dim3(256), 0, st, keys, places, from, sums, to, s->T, s->V, s->d, dout_stride,
-                           s->scale);
+        hipLaunchKernelGGL((k_embed_chunks<T>), dim3(unsigned((s->T + CHUNK - 1) / CHUNK), tiles), dim3(256), 0, st, keys, places, from, sums, ranges, s->T, s->V, s->d, dout_stride);
+        hipLaunchKernelGGL((k_embed_grad<T, TG>), dim3(unsigned((s->V + GRAD_ROWS - 1) / GRAD_ROWS), tiles), dim3(256), 0, st, ranges, places, from, sums, to, s->V, s->d, dout_stride, s->scale);
     };
     if (s->dtype == DYNB_BF16 && grad_dtype == DYNB_BF16) launch(bf16_t{}, bf16_t{});
     else if (s->dtype == DYNB_BF16) launch(bf16_t{}, float{});

@@ -1,6 +1,8 @@
 // Rows of bf16 or fp32 elements in pieces of 16 bytes a lane, at any address and of any length.
 #pragma once
 
+#include <type_traits>
+
 #include "device_utils.h"
 
 // 16 bytes at an address of any element: global memory takes such an access whole (a lane pays for a second line where its piece crosses one)
@@ -30,6 +32,27 @@ template <> __device__ __forceinline__ u32x4 load_piece<float>(const float* p, i
     return v;
 }
 
+// the same in pieces of E elements: 8 bytes of bfloat16 (E = 4), or 16
+template <typename T, int E> using Piece = std::conditional_t<(E * sizeof(T) == 8), u32x2, u32x4>;
+template <int E, typename T> __device__ __forceinline__ Piece<T, E> load_some(const T* p, int left)
+{
+    if constexpr (E * sizeof(T) == 8) {
+        typedef uint32_t u32x2_at2 __attribute__((ext_vector_type(2), aligned(2)));
+        if (left >= 4) return *reinterpret_cast<const u32x2_at2*>(p);
+        u32x2 v = {0u, 0u};
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (i < left) v[i >> 1] |= uint32_t(p[i]) << (16 * (i & 1));
+        return v;
+    } else
+        return load_piece(p, left);
+}
+
+template <typename T> __device__ __forceinline__ float element(const u32x2& v, int i)
+{
+    static_assert(sizeof(T) == 2, "eight bytes of bfloat16");
+    return __uint_as_float(i & 1 ? v[i >> 1] & 0xffff0000u : v[i >> 1] << 16);
+}
 template <typename T> __device__ __forceinline__ float element(const u32x4& v, int i);
 template <> __device__ __forceinline__ float element<bf16_t>(const u32x4& v, int i) { return __uint_as_float(i & 1 ? v[i >> 1] & 0xffff0000u : v[i >> 1] << 16); }
 template <> __device__ __forceinline__ float element<float>(const u32x4& v, int i) { return __uint_as_float(v[i]); }
