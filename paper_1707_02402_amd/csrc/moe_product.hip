@@ -7,10 +7,13 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <atomic>
+#include <initializer_list>
 #include <string>
 #include <type_traits>
 
 #include "device_utils.h"
+#include "lds_copy.h"
 #include "plan_internal.h"
 
 using dynb::fail;
@@ -23,16 +26,22 @@ struct Groups {
     int32_t k, rows;          // ... which has `rows` rows
     int32_t M, E;
     __device__ __forceinline__ int begin(int e) const { return e <= 0 ? 0 : e > E ? M : min(max(offsets[e], 0), M); }
-    __device__ __forceinline__ int64_t row(int r) const
-    {
-        if (!perm) return r;
-        return min(uint32_t(perm[r]) / uint32_t(k), uint32_t(rows - 1));
-    }
+    __device__ __forceinline__ int64_t row_of(int32_t use) const { return min(uint32_t(use) / uint32_t(k), uint32_t(rows - 1)); }
+    __device__ __forceinline__ int64_t row(int r) const { return perm ? row_of(perm[r]) : r; }
 };
 
-struct Piece { int e, begin, rows, part, parts; };             // rows begin .. of group e (E: what lies behind the last group)
+struct Piece { int e, begin, rows; };                          // rows begin .. of group e (E: what lies behind the last group)
 
-// the unit's group and its piece of at most P rows; parts: how many the group has (0: it is empty).  All 64 lanes of a wave call it.
+__device__ __forceinline__ Piece piece_of(const Groups& g, int P, int unit, int e)
+{
+    Piece p;
+    p.e = e;
+    const int a = g.begin(e), rows = g.begin(e + 1) - a, part = unit - (a / P + e);
+    p.begin = a + part * P;
+    p.rows = rows > 0 && part <= (rows - 1) / P ? min(P, rows - part * P) : 0;
+    return p;
+}
+// the unit's group and its piece of at most P rows (0: it has none).  All 64 lanes of a wave call it.
 __device__ __forceinline__ Piece find_piece(const Groups& g, int P, int unit)
 {
     const int lane = threadIdx.x & 63;
@@ -44,14 +53,18 @@ __device__ __forceinline__ Piece find_piece(const Groups& g, int P, int unit)
         lo += last * step;
         n = min(step, n - last * step);
     }
-    Piece p;
-    p.e = __builtin_amdgcn_readfirstlane(lo);
-    const int a = g.begin(p.e), rows = g.begin(p.e + 1) - a;
-    p.part = unit - (a / P + p.e);
-    p.parts = rows > 0 ? (rows - 1) / P + 1 : 0;
-    p.begin = a + p.part * P;
-    p.rows = p.part < p.parts ? min(P, rows - p.part * P) : 0;
-    return p;
+    return piece_of(g, P, unit, __builtin_amdgcn_readfirstlane(lo));
+}
+// ... for every lane its own
+__device__ __forceinline__ Piece find_piece_alone(const Groups& g, int P, int unit)
+{
+    int lo = 0, n = g.E + 1;
+    while (n > 1) {
+        const int half = n >> 1;
+        if (g.begin(lo + half) / P + lo + half <= unit) { lo += half; n -= half; }
+        else n = half;
+    }
+    return piece_of(g, P, unit, lo);
 }
 
 struct Args {
@@ -132,6 +145,425 @@ __global__ __launch_bounds__(256) void k_product_any(Args p)
     }
 }
 
+// ------------------------------------------------------------------------------------------ K and N multiples of 8, rows on 16-byte borders
+// Tiles of results whose operands go straight from memory into LDS, a chunk of 64 places of the sum at a time and at least one chunk ahead, and
+// are multiplied by 32x32x16 MFMAs.  Both operands lie in LDS as they lie in memory.  One whose places of the sum are neighbours there ("along": the rows and the weights of
+// the forward pass, the rows of the input's gradient) is read 16 bytes a lane; one whose places are rows ("across": the weights of the input's gradient, both
+// operands of the weights' gradient) by the transposing LDS load, four places of one column a lane.
+//
+// An across unit is 64 places x 64 columns in eight blocks of 8 places (128 bytes each).  The four places that 32 lanes read together are two neighbours of an
+// even and two of an odd block, and blocks are 64 bytes further apart than their size: all banks.
+constexpr int YBLOCK = 1024 + 64, YUNIT = 8 * YBLOCK;
+// the place of the sum that lane `lane` copies into block `block`
+__device__ __forceinline__ int copied_place(int block, int lane) { return (block >> 1) * 16 + (lane >> 4) * 4 + (block & 1) * 2 + (lane >> 3 & 1); }
+// where in a unit lane `lane` reads four places of its column of the first 32 (the others lie 64 bytes further), K-step 0: the second four lie 256 bytes, each
+// next step 2 * YBLOCK further.  The 16 lanes of a group read 16 columns of four places, four columns of one place each; natural: lane q gets column q; else
+// column 16 h + 4 b + c for q = 8 b + 4 h + c, so that a lane's results (rows 8 b + 4 h + c of the accumulators) are 16 neighbours.
+__device__ __forceinline__ uint32_t places_at(int lane, bool natural)
+{
+    const int r = lane >> 2 & 3, g = lane >> 4 & 1, p = lane & 3, hk = lane >> 5;
+    const int col = natural ? 16 * g + 4 * p : 16 * (p & 1) + 8 * g + 4 * (p >> 1);
+    return uint32_t((r >> 1) * YBLOCK + hk * 512 + (r & 1) * 128 + col * 2);
+}
+__device__ __forceinline__ bf16x8 read_across(lds_ptr p)
+{
+    using lds_i16x4 = __attribute__((address_space(3))) i16x4;
+    const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_i16x4*>(p));
+    const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_i16x4*>(p + 256));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+__device__ __forceinline__ bf16x8 read_along(lds_ptr p) { return *reinterpret_cast<const __attribute__((address_space(3))) bf16x8*>(p); }
+__device__ const u32x4 zeros_16 = {0u, 0u, 0u, 0u};            // what stands behind the end of a sum
+
+// A kind of tile: CG x RG waves, each with FA x 32 columns and NB x 32 rows of the results
+template <int FA_, int NB_, int CG_, int RG_, int BUFS_, int SIMD_>
+struct Kind {
+    static constexpr int FA = FA_, NB = NB_, CG = CG_, RG = RG_, BUFS = BUFS_, SIMD = SIMD_, WAVES = CG * RG, THREADS = WAVES * 64, COLS = CG * FA * 32, ROWS = RG * NB * 32;
+};
+using Big = Kind<2, 4, 4, 2, 2, 2>;      // 256 x 256: an operand's bytes are multiplied 256 times
+using Mid = Kind<2, 2, 2, 2, 2, 2>;      // 128 x 128, two workgroups a CU
+using Few = Kind<1, 2, 4, 1, 3, 2>;      // 128 columns x 64 rows, two chunks ahead: a stream of weights
+
+constexpr int LIST = 256;                // tiles that a staying workgroup looks up at once
+template <int DIR, class S> constexpr uint32_t BUF_BYTES = uint32_t((S::COLS / 64) * (DIR == FORWARD ? XUNIT : YUNIT) + (S::ROWS / 64) * (DIR == GRAD_WEIGHT ? YUNIT : XUNIT));
+template <int DIR, class S> constexpr uint32_t LDS_BYTES = BUF_BYTES<DIR, S> * S::BUFS + (DIR != GRAD_WEIGHT ? LIST * 16 : 0);
+
+// How the weights' gradient is shared out.  The sums run over the rows of a group; every tile of W_e's gradient is the work of one workgroup, or, where there are
+// fewer tiles than CUs, of several ("lanes") that take a share of all rows each.  A group counts as its rows and `extra` more for its tile's way to memory;
+// group e starts at  offsets[e] + extra * e  of the M + extra * E that are shared out evenly.  A group cut by a border leaves partial sums (slots 2 lane for a part
+// that does not begin the group, 2 lane + 1 for one that does) that k_join adds up in order.
+struct Shares {
+    int lanes, extra;
+    int64_t each;
+};
+__device__ __forceinline__ int64_t start_of(const Groups& g, const Shares& s, int e) { return int64_t(g.begin(e)) + int64_t(s.extra) * e; }
+// the last group that starts at or ahead of x.  All 64 lanes of a wave call it.
+__device__ __forceinline__ int group_at(const Groups& g, const Shares& s, int64_t x)
+{
+    const int lane = threadIdx.x & 63;
+    int lo = 0, n = g.E;
+    while (n > 1) {
+        const int step = (n + 63) / 64, e = lo + lane * step;
+        const bool here = lane * step < n && start_of(g, s, e) <= x;
+        const int last = 63 - __builtin_clzll(__ballot(here) | 1ull);
+        lo += last * step;
+        n = min(step, n - last * step);
+    }
+    return __builtin_amdgcn_readfirstlane(lo);
+}
+
+struct Tile {
+    int e, begin, rows, c0, r0, depth;   // group; its first row here; rows of results; first column, row of W's gradient; places of the sum
+    int slot;                            // of the partial sums, or -1
+};
+
+template <int DIR, typename TO, class S>
+__global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int units, int ct, int rt, Shares shares, float* __restrict__ partial)
+{
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
+    constexpr bool A_ACROSS = DIR != FORWARD, B_ACROSS = DIR == GRAD_WEIGHT, STAYS = S::BUFS == 2 && (S::WAVES == 8 || DIR == GRAD_WEIGHT);
+    constexpr int AU = S::COLS / 64, BU = S::ROWS / 64, UA = A_ACROSS ? YUNIT : XUNIT, UB = B_ACROSS ? YUNIT : XUNIT, EACH = 8 / S::WAVES, REQUESTS = (AU + BU) * EACH;
+    constexpr uint32_t BUF = BUF_BYTES<DIR, S>;
+    constexpr int AHEAD = S::BUFS - 1, FA = S::FA, NB = S::NB;
+    static_assert(AHEAD == 1 || !STAYS, "a tile's first chunk is asked for under the last one's last chunk");
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, q = lane & 31, hk = lane >> 5;
+    const int cg = wave % S::CG, rg = wave / S::CG;
+    const int cols = DIR == FORWARD ? p.N : p.K;
+    const lds_ptr lds = (lds_ptr)lds_raw;
+
+    // workgroups of a die (every eighth) are neighbours among the units: they share weights and rows in its L2
+    const int per_die = int(gridDim.x) / 8, place = int(blockIdx.x) < per_die * 8 ? int(blockIdx.x & 7) * per_die + int(blockIdx.x >> 3) : int(blockIdx.x);
+
+    // ---- the tiles
+    // forward, input's gradient: unit = piece of rows * ct + column; a workgroup that stays takes every gridDim.x-th unit, by the list
+    const int count = DIR == GRAD_WEIGHT ? 0 : STAYS ? (units - place + int(gridDim.x) - 1) / int(gridDim.x) : 1;
+    int at_unit = -1;
+    // weights' gradient: a lane's groups
+    const int w_tile = place % (ct * rt), w_lane = place / (ct * rt);
+    const int64_t w_from = shares.each * w_lane, w_to = w_from + shares.each;
+    int w_e = 0;
+    auto tile_of = [&](const Piece& at, int col) {
+        return Tile{at.e, at.begin, at.rows, col * S::COLS, 0, at.e < p.g.E ? (DIR == FORWARD ? p.K : p.N) : 0, -1};
+    };
+    auto list_units = [&](int from) {
+        meet();
+        if (tid < LIST && from + tid < count) {
+            const int unit = place + (from + tid) * int(gridDim.x);
+            const Piece at = find_piece_alone(p.g, S::ROWS, unit / ct);
+            *reinterpret_cast<u32x4*>(lds_raw + BUF * S::BUFS + tid * 16) = u32x4{uint32_t(at.e), uint32_t(at.begin), uint32_t(at.rows), uint32_t(unit % ct)};
+        }
+        meet();
+    };
+    // the next tile, if there is one (rows 0: none)
+    auto next_tile = [&]() -> Tile {
+        Tile t = {};
+        if constexpr (DIR == GRAD_WEIGHT) {
+            for (; w_e < p.g.E; ++w_e) {
+                const int a = min(max(w_e ? uniform_load(p.g.offsets + w_e) : 0, 0), p.g.M), n = max(min(max(uniform_load(p.g.offsets + w_e + 1), 0), p.g.M) - a, 0);
+                const int64_t s = int64_t(a) + int64_t(shares.extra) * w_e, first = s + shares.extra;
+                if (s >= w_to) break;
+                const int lo = int(min(max(w_from - first, int64_t(0)), int64_t(n))), hi = int(min(max(w_to - first, int64_t(0)), int64_t(n)));
+                if (n == 0 ? s < w_from : hi <= lo) continue;
+                t = Tile{w_e, a + lo, p.N - w_tile / ct * S::ROWS, w_tile % ct * S::COLS, w_tile / ct * S::ROWS, hi - lo, hi - lo == n ? -1 : 2 * w_lane + (lo > 0 ? 0 : 1)};
+                t.rows = min(t.rows, S::ROWS);
+                ++w_e;
+                break;
+            }
+        } else if constexpr (STAYS) {
+            while (++at_unit < count) {
+                if (at_unit % LIST == 0) list_units(at_unit);
+                const u32x4 v = *reinterpret_cast<const u32x4*>(lds_raw + BUF * S::BUFS + at_unit % LIST * 16);
+                Piece at;
+                at.e = __builtin_amdgcn_readfirstlane(v.x);
+                at.begin = __builtin_amdgcn_readfirstlane(v.y);
+                at.rows = __builtin_amdgcn_readfirstlane(v.z);
+                if (at.rows > 0) { t = tile_of(at, __builtin_amdgcn_readfirstlane(v.w)); break; }
+            }
+        } else if (++at_unit == 0) {
+            t = tile_of(find_piece(p.g, S::ROWS, place / ct), place % ct);
+        }
+        return t;
+    };
+    if constexpr (DIR == GRAD_WEIGHT) {
+        if (w_lane >= shares.lanes) return;
+        w_e = group_at(p.g, shares, w_from);
+    }
+
+    // ---- copying: wave w's blocks are w, w + WAVES ..
+    const uint32_t piece = uint32_t(lane & 7) * 16u;
+    const char* a_at[A_ACROSS ? 1 : AU][EACH];                 // along: a unit's rows; across: its first place
+    const char* b_at[B_ACROSS ? 1 : BU][EACH];
+    uint32_t a_col[AU], b_col[BU];                             // across: bytes from a row's beginning
+    int32_t z_row[EACH];                                       // weights' gradient: `in`'s row of this lane's places in the chunk that is asked for next
+    int32_t rows_then[BU][EACH];                               // forward: `perm` at the next tile's rows
+    Tile asked = {};                                           // the tile that is asked for
+    auto look_up_rows = [&](const Tile& t) {
+        if constexpr (DIR == FORWARD)
+            if (p.g.perm)
+#pragma unroll
+                for (int i = 0; i < BU; ++i)
+#pragma unroll
+                    for (int j = 0; j < EACH; ++j) rows_then[i][j] = p.g.perm[t.begin + min(i * 64 + (lane >> 5) * 32 + copied_row(wave + j * S::WAVES, lane), t.rows - 1)];
+    };
+    auto look_up_places = [&](int z0) {
+        if constexpr (DIR == GRAD_WEIGHT)
+#pragma unroll
+            for (int j = 0; j < EACH; ++j) {
+                const int r = asked.begin + min(z0 + copied_place(wave + j * S::WAVES, lane), asked.depth - 1);
+                z_row[j] = p.g.perm ? p.g.perm[r] : r;
+            }
+    };
+    auto open = [&](const Tile& t) {
+        asked = t;
+        if (DIR == GRAD_WEIGHT || A_ACROSS)
+#pragma unroll
+            for (int i = 0; i < AU; ++i) a_col[i] = uint32_t(min(t.c0 + i * 64 + (lane & 7) * 8, cols - 8)) * 2u;
+        if (DIR == GRAD_WEIGHT)
+#pragma unroll
+            for (int i = 0; i < BU; ++i) b_col[i] = uint32_t(min(t.r0 + i * 64 + (lane & 7) * 8, p.N - 8)) * 2u;
+        if constexpr (DIR != GRAD_WEIGHT) {
+            const char* const w = reinterpret_cast<const char*>(p.a + size_t(t.e) * size_t(p.N) * size_t(p.K));
+#pragma unroll
+            for (int j = 0; j < EACH; ++j) {
+                const int block = wave + j * S::WAVES, s_q = copied_row(block, lane);
+                if constexpr (A_ACROSS) a_at[0][j] = w + size_t(copied_place(block, lane)) * size_t(p.K) * 2;
+                else
+#pragma unroll
+                    for (int i = 0; i < AU; ++i)               // (the features in the order that gives a lane 16 neighbours)
+                        a_at[i][j] = w + size_t(min(t.c0 + i * 64 + (lane >> 5) * 32 + (s_q >> 2 & 1) * 16 + (s_q >> 3) * 4 + (s_q & 3), cols - 1)) * size_t(p.K) * 2 + piece;
+#pragma unroll
+                for (int i = 0; i < BU; ++i) {
+                    int64_t row = t.begin + min(i * 64 + (lane >> 5) * 32 + s_q, t.rows - 1);
+                    if (DIR == FORWARD && p.g.perm) row = p.g.row_of(rows_then[i][j]);
+                    b_at[i][j] = reinterpret_cast<const char*>(p.b + row * p.b_stride) + piece;
+                }
+            }
+        } else look_up_places(0);
+    };
+    uint32_t fill = 0, take = 0;                               // the chunk's place in LDS that is filled next, and the one that is read
+    const char *w_in[EACH], *w_dout[EACH];
+    // requests i0 .. i1 of the chunk that begins at place z0 of the sum
+    auto request = [&](lds_ptr to, int z0, int i0, int i1) {
+        const bool whole = z0 + 64 <= asked.depth;
+        if (DIR == GRAD_WEIGHT && i0 == 0) {
+#pragma unroll
+            for (int j = 0; j < EACH; ++j) {
+                const int64_t r = asked.begin + min(z0 + copied_place(wave + j * S::WAVES, lane), asked.depth - 1);
+                w_in[j] = reinterpret_cast<const char*>(p.a + (p.g.perm ? p.g.row_of(z_row[j]) : int64_t(z_row[j])) * p.a_stride);
+                w_dout[j] = reinterpret_cast<const char*>(p.b + r * p.b_stride);
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < REQUESTS; ++n) {
+            if (n < i0 || n >= i1) continue;
+            const int i = n / EACH, j = n % EACH, block = wave + j * S::WAVES;
+            const bool is_a = i < AU;
+            const char* from;
+            bool there;
+            if (is_a ? A_ACROSS : B_ACROSS) {
+                if constexpr (DIR == GRAD_WEIGHT) from = is_a ? w_in[j] + a_col[i % AU] : w_dout[j] + b_col[(i - AU + BU) % BU];
+                else from = a_at[0][j] + a_col[i % AU];
+                there = whole || z0 + copied_place(block, lane) < asked.depth;
+            } else {
+                from = is_a ? a_at[A_ACROSS ? 0 : i % AU][j] : b_at[B_ACROSS ? 0 : (i - AU + BU) % BU][j];
+                there = whole || z0 + (lane & 7) * 8 < asked.depth;
+            }
+            if (!there) from = reinterpret_cast<const char*>(&zeros_16);
+            lds_copy16_from(from, to + uint32_t(is_a ? i * UA + block * (A_ACROSS ? YBLOCK : XBLOCK) : AU * UA + (i - AU) * UB + block * (B_ACROSS ? YBLOCK : XBLOCK)));
+        }
+    };
+    auto requested = [&](int z0) {
+        fill = fill == AHEAD * BUF ? 0 : fill + BUF;
+        if constexpr (DIR == GRAD_WEIGHT) {
+            if (z0 + 64 < asked.depth) look_up_places(z0 + 64);
+        } else {
+#pragma unroll
+            for (int j = 0; j < EACH; ++j) {
+                if constexpr (A_ACROSS) a_at[0][j] += size_t(p.K) * 128;
+                else
+#pragma unroll
+                    for (int i = 0; i < AU; ++i) a_at[i][j] += 128;
+#pragma unroll
+                for (int i = 0; i < BU; ++i) b_at[i][j] += 128;
+            }
+        }
+    };
+
+    // ---- a tile after the other
+    const uint32_t a_slot = A_ACROSS ? places_at(lane, false) : fragment_at(q, hk), b_slot = B_ACROSS ? places_at(lane, true) : fragment_at(q, hk);
+    Tile now = next_tile();
+    bool primed = false;                                       // its first chunk has been asked for
+    int stores = 0;                                            // of this wave, behind that request
+    while (now.rows > 0) {
+        const int nchunk = (now.depth + 63) / 64;
+        if (nchunk > 0 && !primed) {
+            look_up_rows(now);
+            open(now);
+#pragma unroll
+            for (int c = 0; c < AHEAD; ++c)
+                if (c < nchunk) {
+                    request(lds + fill, c * 64, 0, REQUESTS);
+                    requested(c * 64);
+                }
+            stores = 0;
+        }
+        Tile then = {};
+        const int blocks = (now.rows + 31) / 32;
+        const int mine = now.c0 + cg * (FA * 32) < cols ? max(0, (blocks - rg + S::RG - 1) / S::RG) : 0;
+        auto arrive = [&](int c) {                             // chunk c is there, and all waves are done with the one before
+            if constexpr (AHEAD == 1) {
+                if (c == 0 && stores > 0) {
+                    if (stores >= 16) answered_but<16>();
+                    else if (stores >= 8) answered_but<8>();
+                    else answered_but<4>();
+                } else answered_but<0>();
+            } else {
+                if (c + 1 < nchunk) answered_but<REQUESTS>();
+                else answered_but<0>();
+            }
+            meet();
+        };
+        auto work = [&](auto nb_const) {
+            constexpr int LIVE = decltype(nb_const)::value;
+            f32x16 acc[FA][LIVE > 0 ? LIVE : 1];
+#pragma unroll
+            for (int a = 0; a < FA; ++a)
+#pragma unroll
+                for (int b = 0; b < LIVE; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.f;
+#pragma unroll 1
+            for (int c = 0; c < nchunk; ++c) {
+                arrive(c);
+                int z_ask = c + AHEAD < nchunk ? (c + AHEAD) * 64 : -1;
+                if (STAYS && c == 0) {
+                    then = next_tile();
+                    if (then.rows > 0 && then.depth > 0) look_up_rows(then);
+                }
+                if (STAYS && c == nchunk - 1 && then.rows > 0 && then.depth > 0) {
+                    open(then);
+                    z_ask = 0;
+                }
+                // (what is read and what is filled are said to be apart: else every transposing read would wait for all requests)
+                auto chunk = [&](const lds_ptr __restrict__ from, const lds_ptr __restrict__ to) {
+                const lds_ptr au = from + (uint32_t((cg * FA / 2) * UA) + a_slot + uint32_t(FA == 1 ? (cg & 1) * (A_ACROSS ? 64 : 512) : 0));
+                const lds_ptr bu = from + (uint32_t(AU * UA) + b_slot);
+                bf16x8 af[2][FA], bf[2][LIVE > 0 ? LIVE : 1];
+                auto read = [&](int ks) {
+#pragma unroll
+                    for (int a = 0; a < FA; ++a) {
+                        if constexpr (A_ACROSS) af[ks & 1][a] = read_across(au + uint32_t(a * 64 + ks * 2 * YBLOCK));
+                        else af[ks & 1][a] = read_along(au + (a * 512 + ks * 32));
+                    }
+#pragma unroll
+                    for (int b = 0; b < LIVE; ++b) {
+                        const lds_ptr at = bu + uint32_t((b * S::RG + rg) / 2 * UB + (b * S::RG + rg) % 2 * (B_ACROSS ? 64 : 512));
+                        if constexpr (B_ACROSS) bf[ks & 1][b] = read_across(at + uint32_t(ks * 2 * YBLOCK));
+                        else bf[ks & 1][b] = read_along(at + ks * 32);
+                    }
+                };
+                auto ask = [&](int ks) {
+                    if (z_ask >= 0 && ks < 2) request(to, z_ask, ks * REQUESTS / 2, (ks + 1) * REQUESTS / 2);
+                    __builtin_amdgcn_sched_barrier(0);
+                };
+                if constexpr (LIVE == 0) { ask(0); ask(1); }
+                else {
+                    if (S::BUFS > 2) { ask(0); ask(1); }       // (a stream of weights: first of all)
+                    read(0);
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+                        for (int b = 0; b < LIVE; ++b) {
+#pragma unroll
+                            for (int a = 0; a < FA; ++a) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(af[ks & 1][a], bf[ks & 1][b], acc[a][b], 0, 0, 0);
+                            __builtin_amdgcn_sched_barrier(0);
+                            if (b == 0 && ks < 3) {
+                                read(ks + 1);
+                                __builtin_amdgcn_sched_barrier(0);
+                            }
+                            if (S::BUFS == 2 && b == LIVE / 2) ask(ks);
+                        }
+                }
+                };
+                chunk(lds + take, lds + fill);
+                if (z_ask >= 0) requested(z_ask);
+                take = take == AHEAD * BUF ? 0 : take + BUF;
+            }
+            // a lane: 16 neighbouring columns of row q of every block
+#pragma unroll
+            for (int b = 0; b < LIVE; ++b) {
+                const int r = (b * S::RG + rg) * 32 + q;
+                if (r >= now.rows) continue;
+                const int c = now.c0 + cg * (FA * 32) + 16 * hk;
+                auto put = [&](auto* to) {
+#pragma unroll
+                    for (int a = 0; a < FA; ++a)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const int at = a * 32 + h * 8;
+                            if (c + at >= cols) continue;
+                            float v[8];
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) v[i] = acc[a][b][8 * h + i];
+                            if (DIR == FORWARD && p.relu)
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) v[i] = v[i] < 0.f ? 0.f : v[i];                  // (a NaN stays one)
+                            if (DIR == GRAD_INPUT && p.act) {
+                                const bf16x8 on = *reinterpret_cast<const bf16x8*>(p.act + int64_t(now.begin + r) * p.act_stride + c + at);
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) v[i] = float(on[i]) > 0.f ? v[i] : 0.f;
+                            }
+                            if constexpr (std::is_same_v<decltype(to), float*>) {
+                                *reinterpret_cast<u32x4*>(to + at) = u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+                                *reinterpret_cast<u32x4*>(to + at + 4) = u32x4{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])};
+                            } else
+                                *reinterpret_cast<u32x4*>(to + at) = u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+                        }
+                };
+                if constexpr (DIR == GRAD_WEIGHT) {
+                    const size_t row = size_t(now.r0 + r) * size_t(p.K) + size_t(c), all = size_t(p.N) * size_t(p.K);
+                    if (now.slot >= 0) put(partial + size_t(now.slot) * all + row);
+                    else put(static_cast<TO*>(p.out) + size_t(now.e) * all + row);
+                } else put(static_cast<TO*>(p.out) + int64_t(now.begin + r) * p.out_stride + c);
+            }
+            // (an end of its own for every size, so that the compiler keeps what is the same for all lanes in scalar registers)
+            asm volatile("; %0" ::"n"(LIVE));
+        };
+        if (mine > NB / 2) work(std::integral_constant<int, NB>{});
+        else if (mine > 0) work(std::integral_constant<int, NB / 2>{});
+        else work(std::integral_constant<int, 0>{});
+        if (!STAYS) return;
+        if (nchunk == 0) then = next_tile();
+        primed = nchunk > 0 && then.depth > 0;
+        // (the fewest that there can have been: none is made for columns beyond the last)
+        stores = now.c0 + cg * (FA * 32) + FA * 32 <= cols ? min(mine, NB) * FA * 2 : 0;
+        now = then;
+    }
+}
+
+// Gradients whose sum a border between two lanes cuts: their parts, in order.  A workgroup looks after a share of the elements for one border, and only for the
+// first one inside a group.
+template <typename TO>
+__global__ __launch_bounds__(256) void k_join(Groups g, Shares s, const float* __restrict__ partial, TO* __restrict__ out, int64_t elements, int per_border)
+{
+    const int border = int(blockIdx.x) / per_border + 1;
+    const int64_t x = s.each * border;
+    const int e = group_at(g, s, x), n = max(g.begin(e + 1) - g.begin(e), 0);
+    const int64_t first = start_of(g, s, e) + s.extra;
+    if (x <= first || x >= first + n || x - s.each > first) return;
+    int last = border;
+    while (last + 1 < s.lanes && s.each * (last + 1) < first + n) ++last;
+    for (int64_t i = (int64_t(blockIdx.x) % per_border * 256 + threadIdx.x) * 4; i < elements; i += int64_t(per_border) * 1024) {
+        f32x4 v = *reinterpret_cast<const f32x4*>(partial + (2 * border - 1) * elements + i);
+#pragma unroll 4
+        for (int j = border; j <= last; ++j) v += *reinterpret_cast<const f32x4*>(partial + 2 * int64_t(j) * elements + i);
+        TO* const to = out + int64_t(e) * elements + i;
+        if constexpr (std::is_same_v<TO, float>) *reinterpret_cast<f32x4*>(to) = v;
+        else *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+    }
+}
+
 int check(const moe_product_shape* s, const std::string& who)
 {
     if (!s) return fail(DYNB_E_INVAL, who + ": NULL shape");
@@ -150,6 +582,7 @@ int check_groups(const moe_product_shape* s, const moe_groups* g, bool gathers, 
     return DYNB_OK;
 }
 int64_t tiles(int n) { return (int64_t(n) + ANY - 1) / ANY; }
+constexpr int CUS = 256;
 constexpr int64_t MOST_GROUPS = (1 << 24) - 1;                 // workgroups of 256 threads in a launch
 bool odd(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 1) != 0; }
 
@@ -158,6 +591,89 @@ int launched(const char* who)
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return fail(DYNB_E_HIP, std::string(who) + ": " + hipGetErrorString(e));
     return DYNB_OK;
+}
+
+bool on_16(std::initializer_list<const void*> pointers)
+{
+    for (const void* p : pointers)
+        if (reinterpret_cast<uintptr_t>(p) & 15) return false;
+    return true;
+}
+
+// us of a pass by kind:
+enum KindOf { BIG, MID, FEW };
+KindOf kind_of(const moe_product_shape* s)
+{
+    const int64_t each = s->M / s->E;
+    return each >= 192 ? BIG : each >= 64 ? MID : FEW;
+}
+
+template <int DIR, typename TO, class S>
+int launch_tiles(const Args& p, int64_t grid, int64_t units, int ct, int rt, const Shares& shares, float* partial, hipStream_t st, const char* who)
+{
+    static std::atomic<uint64_t> attr_set{0};                 // one bit per device: LDS beyond 64 KB
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e == hipSuccess && !(attr_set.load() >> (dev & 63) & 1)) {
+        e = hipFuncSetAttribute(reinterpret_cast<const void*>(k_product<DIR, TO, S>), hipFuncAttributeMaxDynamicSharedMemorySize, int(LDS_BYTES<DIR, S>));
+        if (e == hipSuccess) attr_set.fetch_or(uint64_t(1) << (dev & 63));
+    }
+    if (e != hipSuccess) return fail(DYNB_E_HIP, std::string(who) + ": " + hipGetErrorString(e));
+    hipLaunchKernelGGL((k_product<DIR, TO, S>), dim3(unsigned(grid)), dim3(S::THREADS), (LDS_BYTES<DIR, S>), st, p, int(units), ct, rt, shares, partial);
+    return launched(who);
+}
+
+// forward and the input's gradient
+template <int DIR>
+int launch_rows(const moe_product_shape* s, const Args& p, bool fast, hipStream_t st, const char* who)
+{
+    const int cols = DIR == FORWARD ? s->N : s->K;
+    auto launch = [&](auto kind) {
+        using S = decltype(kind);
+        const int ct = (cols + S::COLS - 1) / S::COLS;
+        const int64_t units = (int64_t(s->M) / S::ROWS + s->E + 1) * ct;
+        if (units > MOST_GROUPS) return fail(DYNB_E_UNSUPPORTED, std::string(who) + ": too many results");
+        return launch_tiles<DIR, bf16_t, S>(p, S::WAVES == 8 ? std::min<int64_t>(units, CUS) : units, units, ct, 1, Shares{}, nullptr, st, who);
+    };
+    if (fast) switch (kind_of(s)) {
+        case BIG: return launch(Big{});
+        case MID: return launch(Mid{});
+        default: return launch(Few{});
+        }
+    const int64_t grid = tiles(cols) * (s->M / ANY + s->E + 1);
+    if (grid > MOST_GROUPS) return fail(DYNB_E_UNSUPPORTED, std::string(who) + ": too many results");
+    hipLaunchKernelGGL((k_product_any<DIR, bf16_t>), dim3(unsigned(grid)), dim3(256), 0, st, p);
+    return launched(who);
+}
+
+// How the weights' gradient runs: the kind of tile, and as many lanes as give the least work to the workgroup that has the most, with what adding up
+// the lanes' parts takes.  In rows' time of a tile, 16 ns: a tile's way to memory is 512 of them, and a lane's two parts move some
+// 2.5 times the gradient's size at 5 TB/s.
+struct WeightPlan {
+    bool big;
+    int ct, rt;
+    Shares shares;
+    size_t bytes;                                              // of partial sums
+};
+WeightPlan weight_plan(const moe_product_shape* s)
+{
+    WeightPlan w = {};
+    w.big = s->K > 128 && s->N > 128;
+    const int side = w.big ? 256 : 128, slots = w.big ? CUS : 2 * CUS;
+    w.ct = (s->K + side - 1) / side;
+    w.rt = (s->N + side - 1) / side;
+    w.shares.extra = 512;
+    const int64_t tiles_ = int64_t(w.ct) * w.rt, all = int64_t(s->M) + int64_t(w.shares.extra) * s->E;
+    const double join = 2.5 * 4.0 * double(s->K) * double(s->N) / 5e6 / 0.016;
+    double best = 0.0;
+    w.shares.lanes = 1;
+    for (int lanes = 1; lanes <= slots && int64_t(lanes) * 256 <= std::max<int64_t>(s->M, 256); ++lanes) {
+        const double cost = double((tiles_ * lanes + slots - 1) / slots) * double(all) / lanes + (lanes - 1) * join;
+        if (lanes == 1 || cost < best) { best = cost; w.shares.lanes = lanes; }
+    }
+    w.shares.each = (all + w.shares.lanes - 1) / w.shares.lanes;
+    w.bytes = w.shares.lanes > 1 ? size_t(w.shares.lanes) * 2 * size_t(s->K) * size_t(s->N) * 4 : 0;
+    return w;
 }
 
 Groups groups_of(const moe_product_shape* s, const moe_groups* g) { return Groups{g->offsets, g->perm, std::max(g->k, 1), g->perm ? g->rows : s->M, s->M, s->E}; }
@@ -174,10 +690,8 @@ extern "C" int moe_product(const moe_product_shape* s, const moe_groups* g, cons
     if (in_stride < s->K || out_stride < s->N) return fail(DYNB_E_INVAL, "moe_product: rows overlap (stride below their length)");
     if (odd(in) || odd(W) || odd(out)) return fail(DYNB_E_INVAL, "moe_product: misaligned pointer");
     const Args p = {groups_of(s, g), static_cast<const bf16_t*>(W), static_cast<const bf16_t*>(in), 0, in_stride, nullptr, 0, out, out_stride, s->K, s->N, int(s->flags & MOE_PRODUCT_RELU)};
-    const int64_t grid = tiles(s->N) * (s->M / ANY + s->E + 1);
-    if (grid > MOST_GROUPS) return fail(DYNB_E_UNSUPPORTED, "moe_product: too many results");
-    hipLaunchKernelGGL((k_product_any<FORWARD, bf16_t>), dim3(unsigned(grid)), dim3(256), 0, static_cast<hipStream_t>(stream), p);
-    return launched("moe_product");
+    const bool fast = s->K % 8 == 0 && s->N % 8 == 0 && in_stride % 8 == 0 && out_stride % 8 == 0 && on_16({in, W, out});
+    return launch_rows<FORWARD>(s, p, fast, static_cast<hipStream_t>(stream), "moe_product");
 }
 
 extern "C" int moe_product_grad_input(const moe_product_shape* s, const moe_groups* g, const void* dout, int64_t dout_stride, const void* W, const void* act, int64_t act_stride,
@@ -191,16 +705,14 @@ extern "C" int moe_product_grad_input(const moe_product_shape* s, const moe_grou
     if (dout_stride < s->N || din_stride < s->K || (act && act_stride < s->K)) return fail(DYNB_E_INVAL, "moe_product_grad_input: rows overlap (stride below their length)");
     if (odd(dout) || odd(W) || odd(act) || odd(din)) return fail(DYNB_E_INVAL, "moe_product_grad_input: misaligned pointer");
     const Args p = {groups_of(s, g), static_cast<const bf16_t*>(W), static_cast<const bf16_t*>(dout), 0, dout_stride, static_cast<const bf16_t*>(act), act_stride, din, din_stride, s->K, s->N, 0};
-    const int64_t grid = tiles(s->K) * (s->M / ANY + s->E + 1);
-    if (grid > MOST_GROUPS) return fail(DYNB_E_UNSUPPORTED, "moe_product_grad_input: too many results");
-    hipLaunchKernelGGL((k_product_any<GRAD_INPUT, bf16_t>), dim3(unsigned(grid)), dim3(256), 0, static_cast<hipStream_t>(stream), p);
-    return launched("moe_product_grad_input");
+    const bool fast = s->K % 8 == 0 && s->N % 8 == 0 && dout_stride % 8 == 0 && act_stride % 8 == 0 && din_stride % 8 == 0 && on_16({dout, W, act, din});
+    return launch_rows<GRAD_INPUT>(s, p, fast, static_cast<hipStream_t>(stream), "moe_product_grad_input");
 }
 
 extern "C" size_t moe_product_grad_weight_workspace_bytes(const moe_product_shape* s)
 {
     if (check(s, "moe_product_grad_weight_workspace_bytes") != DYNB_OK) return 0;
-    return 256;
+    return std::max<size_t>(weight_plan(s).bytes, 256);
 }
 
 extern "C" int moe_product_grad_weight(const moe_product_shape* s, const moe_groups* g, const void* dout, int64_t dout_stride, const void* in, int64_t in_stride, void* dW,
@@ -216,6 +728,23 @@ extern "C" int moe_product_grad_weight(const moe_product_shape* s, const moe_gro
     if (workspace_bytes < moe_product_grad_weight_workspace_bytes(s)) return fail(DYNB_E_WORKSPACE, "moe_product_grad_weight: workspace too small");
     if (reinterpret_cast<uintptr_t>(workspace) & 255) return fail(DYNB_E_INVAL, "moe_product_grad_weight: workspace not 256-byte aligned");
     const Args p = {groups_of(s, g), static_cast<const bf16_t*>(in), static_cast<const bf16_t*>(dout), in_stride, dout_stride, nullptr, 0, dW, 0, s->K, s->N, 0};
+    if (s->K % 8 == 0 && s->N % 8 == 0 && dout_stride % 8 == 0 && in_stride % 8 == 0 && on_16({dout, in, dW})) {
+        const WeightPlan w = weight_plan(s);
+        hipStream_t st = static_cast<hipStream_t>(stream);
+        float* const partial = static_cast<float*>(workspace);
+        const int64_t grid = int64_t(w.ct) * w.rt * w.shares.lanes, elements = int64_t(s->K) * s->N;
+        if (grid > MOST_GROUPS / 2) return fail(DYNB_E_UNSUPPORTED, "moe_product_grad_weight: too many results");
+        auto launch = [&](auto to) {
+            using TO = decltype(to);
+            const int done = w.big ? launch_tiles<GRAD_WEIGHT, TO, Big>(p, grid, 0, w.ct, w.rt, w.shares, partial, st, "moe_product_grad_weight")
+                                   : launch_tiles<GRAD_WEIGHT, TO, Mid>(p, grid, 0, w.ct, w.rt, w.shares, partial, st, "moe_product_grad_weight");
+            if (done != DYNB_OK || w.shares.lanes == 1) return done;
+            const int per_border = int(std::min<int64_t>((elements + 4095) / 4096, 512));
+            hipLaunchKernelGGL((k_join<TO>), dim3(unsigned((w.shares.lanes - 1) * per_border)), dim3(256), 0, st, p.g, w.shares, partial, static_cast<TO*>(dW), elements, per_border);
+            return launched("moe_product_grad_weight");
+        };
+        return grad_dtype == DYNB_BF16 ? launch(bf16_t{}) : launch(float{});
+    }
     const int64_t grid = tiles(s->K) * tiles(s->N) * s->E;
     if (grid > MOST_GROUPS) return fail(DYNB_E_UNSUPPORTED, "moe_product_grad_weight: too many results");
     hipStream_t st = static_cast<hipStream_t>(stream);
