@@ -27,8 +27,13 @@ __device__ __forceinline__ void lds_copy16(const char* base, uint32_t off, uint3
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)(base + off),
                                      (__attribute__((address_space(3))) uint32_t*)(lds_raw + lds_at), 16, 0, ONCE ? 2 : 0);
 }
-// ... from any addresses
 using lds_ptr = __attribute__((address_space(3))) unsigned char*;
+__device__ __forceinline__ void lds_copy16_to(const char* base, uint32_t off, lds_ptr lds)
+{
+    asm volatile("" : "+s"(base), "+v"(off));
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)(base + off), (__attribute__((address_space(3))) uint32_t*)lds, 16, 0, 0);
+}
+// ... from any addresses
 __device__ __forceinline__ void lds_copy16_from(const char* p, lds_ptr lds)
 {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)(p), (__attribute__((address_space(3))) uint32_t*)lds, 16, 0, 0);

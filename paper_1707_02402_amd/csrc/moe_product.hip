@@ -26,7 +26,7 @@ struct Groups {
     int32_t k, rows;          // ... which has `rows` rows
     int32_t M, E;
     __device__ __forceinline__ int begin(int e) const { return e <= 0 ? 0 : e > E ? M : min(max(offsets[e], 0), M); }
-    __device__ __forceinline__ int64_t row_of(int32_t use) const { return min(uint32_t(use) / uint32_t(k), uint32_t(rows - 1)); }
+    __device__ __forceinline__ uint32_t row_of(int32_t use) const { return min(uint32_t(use) / uint32_t(k), uint32_t(rows - 1)); }
     __device__ __forceinline__ int64_t row(int r) const { return perm ? row_of(perm[r]) : r; }
 };
 
@@ -178,6 +178,7 @@ __device__ const u32x4 zeros_16 = {0u, 0u, 0u, 0u};            // what stands be
 // A kind of tile: CG x RG waves, each with FA x 32 columns and NB x 32 rows of the results
 template <int FA_, int NB_, int CG_, int RG_, int BUFS_, int SIMD_>
 struct Kind {
+    static constexpr bool BIG = FA_ * CG_ == 8;
     static constexpr int FA = FA_, NB = NB_, CG = CG_, RG = RG_, BUFS = BUFS_, SIMD = SIMD_, WAVES = CG * RG, THREADS = WAVES * 64, COLS = CG * FA * 32, ROWS = RG * NB * 32;
 };
 using Big = Kind<2, 4, 4, 2, 2, 2>;      // 256 x 256: an operand's bytes are multiplied 256 times
@@ -221,7 +222,7 @@ template <int DIR, typename TO, class S>
 __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int units, int ct, int rt, Shares shares, float* __restrict__ partial)
 {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
-    constexpr bool A_ACROSS = DIR != FORWARD, B_ACROSS = DIR == GRAD_WEIGHT, STAYS = S::BUFS == 2 && (S::WAVES == 8 || DIR == GRAD_WEIGHT);
+    constexpr bool A_ACROSS = DIR != FORWARD, B_ACROSS = DIR == GRAD_WEIGHT, STAYS = S::BUFS == 2 && (S::BIG || DIR == GRAD_WEIGHT);
     constexpr int AU = S::COLS / 64, BU = S::ROWS / 64, UA = A_ACROSS ? YUNIT : XUNIT, UB = B_ACROSS ? YUNIT : XUNIT, EACH = 8 / S::WAVES, REQUESTS = (AU + BU) * EACH;
     constexpr uint32_t BUF = BUF_BYTES<DIR, S>;
     constexpr int AHEAD = S::BUFS - 1, FA = S::FA, NB = S::NB;
@@ -289,12 +290,14 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
         w_e = group_at(p.g, shares, w_from);
     }
 
-    // ---- copying: wave w's blocks are w, w + WAVES ..
+    // ---- copying: wave w's blocks are w, w + WAVES ..; a request is a scalar base, which moves on with the chunks, and a lane's offset, which a tile keeps
+    // (but for gathered rows as places of the sum)
     const uint32_t piece = uint32_t(lane & 7) * 16u;
-    const char* a_at[A_ACROSS ? 1 : AU][EACH];                 // along: a unit's rows; across: its first place
-    const char* b_at[B_ACROSS ? 1 : BU][EACH];
-    uint32_t a_col[AU], b_col[BU];                             // across: bytes from a row's beginning
-    int32_t z_row[EACH];                                       // weights' gradient: `in`'s row of this lane's places in the chunk that is asked for next
+    const char *a_base = nullptr, *b_base = nullptr;
+    uint32_t a_off[AU][EACH], b_off[BU][EACH];
+    const size_t a_step = DIR == FORWARD ? 128 : DIR == GRAD_INPUT ? size_t(p.K) * 128 : p.g.perm ? 0 : size_t(p.a_stride) * 128;
+    const size_t b_step = B_ACROSS ? size_t(p.b_stride) * 128 : 128;
+    int32_t uses[EACH];                                        // weights' gradient: `perm` at this lane's places of the chunk that is asked for next
     int32_t rows_then[BU][EACH];                               // forward: `perm` at the next tile's rows
     Tile asked = {};                                           // the tile that is asked for
     auto look_up_rows = [&](const Tile& t) {
@@ -307,86 +310,63 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
     };
     auto look_up_places = [&](int z0) {
         if constexpr (DIR == GRAD_WEIGHT)
+            if (p.g.perm)
 #pragma unroll
-            for (int j = 0; j < EACH; ++j) {
-                const int r = asked.begin + min(z0 + copied_place(wave + j * S::WAVES, lane), asked.depth - 1);
-                z_row[j] = p.g.perm ? p.g.perm[r] : r;
-            }
+                for (int j = 0; j < EACH; ++j) uses[j] = p.g.perm[asked.begin + min(z0 + copied_place(wave + j * S::WAVES, lane), asked.depth - 1)];
     };
     auto open = [&](const Tile& t) {
         asked = t;
-        if (DIR == GRAD_WEIGHT || A_ACROSS)
+        const size_t w = size_t(t.e) * size_t(p.N) * size_t(p.K);
+        a_base = reinterpret_cast<const char*>(DIR == GRAD_WEIGHT ? p.a + (p.g.perm ? 0 : t.begin * p.a_stride) : DIR == FORWARD ? p.a + w + size_t(t.c0) * size_t(p.K) : p.a + w);
+        b_base = reinterpret_cast<const char*>(DIR == FORWARD && p.g.perm ? p.b : p.b + t.begin * p.b_stride);
 #pragma unroll
-            for (int i = 0; i < AU; ++i) a_col[i] = uint32_t(min(t.c0 + i * 64 + (lane & 7) * 8, cols - 8)) * 2u;
-        if (DIR == GRAD_WEIGHT)
+        for (int j = 0; j < EACH; ++j) {
+            const int block = wave + j * S::WAVES, s_q = copied_row(block, lane), z = copied_place(block, lane);
 #pragma unroll
-            for (int i = 0; i < BU; ++i) b_col[i] = uint32_t(min(t.r0 + i * 64 + (lane & 7) * 8, p.N - 8)) * 2u;
-        if constexpr (DIR != GRAD_WEIGHT) {
-            const char* const w = reinterpret_cast<const char*>(p.a + size_t(t.e) * size_t(p.N) * size_t(p.K));
+            for (int i = 0; i < AU; ++i) {
+                const uint32_t col = uint32_t(min(t.c0 + i * 64 + (lane & 7) * 8, cols - 8)) * 2u;
+                if constexpr (DIR == FORWARD)                  // (the features in the order that gives a lane 16 neighbours)
+                    a_off[i][j] = uint32_t(min(i * 64 + (lane >> 5) * 32 + (s_q >> 2 & 1) * 16 + (s_q >> 3) * 4 + (s_q & 3), cols - 1 - t.c0)) * uint32_t(p.K) * 2u + piece;
+                else if constexpr (DIR == GRAD_INPUT) a_off[i][j] = uint32_t(z) * uint32_t(p.K) * 2u + col;
+                else a_off[i][j] = (p.g.perm ? 0u : uint32_t(z) * uint32_t(p.a_stride) * 2u) + col;
+            }
 #pragma unroll
-            for (int j = 0; j < EACH; ++j) {
-                const int block = wave + j * S::WAVES, s_q = copied_row(block, lane);
-                if constexpr (A_ACROSS) a_at[0][j] = w + size_t(copied_place(block, lane)) * size_t(p.K) * 2;
-                else
-#pragma unroll
-                    for (int i = 0; i < AU; ++i)               // (the features in the order that gives a lane 16 neighbours)
-                        a_at[i][j] = w + size_t(min(t.c0 + i * 64 + (lane >> 5) * 32 + (s_q >> 2 & 1) * 16 + (s_q >> 3) * 4 + (s_q & 3), cols - 1)) * size_t(p.K) * 2 + piece;
-#pragma unroll
-                for (int i = 0; i < BU; ++i) {
-                    int64_t row = t.begin + min(i * 64 + (lane >> 5) * 32 + s_q, t.rows - 1);
+            for (int i = 0; i < BU; ++i) {
+                if constexpr (B_ACROSS) b_off[i][j] = uint32_t(z) * uint32_t(p.b_stride) * 2u + uint32_t(min(t.r0 + i * 64 + (lane & 7) * 8, p.N - 8)) * 2u;
+                else {
+                    uint32_t row = uint32_t(min(i * 64 + (lane >> 5) * 32 + s_q, t.rows - 1));
                     if (DIR == FORWARD && p.g.perm) row = p.g.row_of(rows_then[i][j]);
-                    b_at[i][j] = reinterpret_cast<const char*>(p.b + row * p.b_stride) + piece;
+                    b_off[i][j] = row * uint32_t(p.b_stride) * 2u + piece;
                 }
             }
-        } else look_up_places(0);
+        }
+        look_up_places(0);
     };
     uint32_t fill = 0, take = 0;                               // the chunk's place in LDS that is filled next, and the one that is read
-    const char *w_in[EACH], *w_dout[EACH];
     // requests i0 .. i1 of the chunk that begins at place z0 of the sum
     auto request = [&](lds_ptr to, int z0, int i0, int i1) {
         const bool whole = z0 + 64 <= asked.depth;
-        if (DIR == GRAD_WEIGHT && i0 == 0) {
-#pragma unroll
-            for (int j = 0; j < EACH; ++j) {
-                const int64_t r = asked.begin + min(z0 + copied_place(wave + j * S::WAVES, lane), asked.depth - 1);
-                w_in[j] = reinterpret_cast<const char*>(p.a + (p.g.perm ? p.g.row_of(z_row[j]) : int64_t(z_row[j])) * p.a_stride);
-                w_dout[j] = reinterpret_cast<const char*>(p.b + r * p.b_stride);
-            }
-        }
 #pragma unroll
         for (int n = 0; n < REQUESTS; ++n) {
             if (n < i0 || n >= i1) continue;
             const int i = n / EACH, j = n % EACH, block = wave + j * S::WAVES;
             const bool is_a = i < AU;
-            const char* from;
-            bool there;
-            if (is_a ? A_ACROSS : B_ACROSS) {
-                if constexpr (DIR == GRAD_WEIGHT) from = is_a ? w_in[j] + a_col[i % AU] : w_dout[j] + b_col[(i - AU + BU) % BU];
-                else from = a_at[0][j] + a_col[i % AU];
-                there = whole || z0 + copied_place(block, lane) < asked.depth;
-            } else {
-                from = is_a ? a_at[A_ACROSS ? 0 : i % AU][j] : b_at[B_ACROSS ? 0 : (i - AU + BU) % BU][j];
-                there = whole || z0 + (lane & 7) * 8 < asked.depth;
+            const lds_ptr lds_at = to + uint32_t(is_a ? i * UA + block * (A_ACROSS ? YBLOCK : XBLOCK) : AU * UA + (i - AU) * UB + block * (B_ACROSS ? YBLOCK : XBLOCK));
+            const char* const base = is_a ? a_base : b_base;
+            uint32_t off = is_a ? a_off[i % AU][j] : b_off[(i - AU + BU) % BU][j];
+            if (DIR == GRAD_WEIGHT && is_a && p.g.perm) off += p.g.row_of(uses[j]) * uint32_t(p.a_stride) * 2u;
+            if (whole) lds_copy16_to(base, off, lds_at);
+            else {                                             // (zeros behind the end of the sum)
+                const int z = (is_a ? A_ACROSS : B_ACROSS) ? copied_place(block, lane) : (lane & 7) * 8;
+                lds_copy16_from(z0 + z < asked.depth ? base + off : reinterpret_cast<const char*>(&zeros_16), lds_at);
             }
-            if (!there) from = reinterpret_cast<const char*>(&zeros_16);
-            lds_copy16_from(from, to + uint32_t(is_a ? i * UA + block * (A_ACROSS ? YBLOCK : XBLOCK) : AU * UA + (i - AU) * UB + block * (B_ACROSS ? YBLOCK : XBLOCK)));
         }
     };
     auto requested = [&](int z0) {
         fill = fill == AHEAD * BUF ? 0 : fill + BUF;
-        if constexpr (DIR == GRAD_WEIGHT) {
-            if (z0 + 64 < asked.depth) look_up_places(z0 + 64);
-        } else {
-#pragma unroll
-            for (int j = 0; j < EACH; ++j) {
-                if constexpr (A_ACROSS) a_at[0][j] += size_t(p.K) * 128;
-                else
-#pragma unroll
-                    for (int i = 0; i < AU; ++i) a_at[i][j] += 128;
-#pragma unroll
-                for (int i = 0; i < BU; ++i) b_at[i][j] += 128;
-            }
-        }
+        a_base += a_step;
+        b_base += b_step;
+        if (z0 + 64 < asked.depth) look_up_places(z0 + 64);
     };
 
     // ---- a tile after the other
@@ -452,8 +432,8 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
                 auto read = [&](int ks) {
 #pragma unroll
                     for (int a = 0; a < FA; ++a) {
-                        if constexpr (A_ACROSS) af[ks & 1][a] = read_across(au + uint32_t(a * 64 + ks * 2 * YBLOCK));
-                        else af[ks & 1][a] = read_along(au + (a * 512 + ks * 32));
+                        if constexpr (A_ACROSS) af[ks & 1][a] = read_across(au + uint32_t(a / 2 * UA + a % 2 * 64 + ks * 2 * YBLOCK));
+                        else af[ks & 1][a] = read_along(au + (a / 2 * UA + a % 2 * 512 + ks * 32));
                     }
 #pragma unroll
                     for (int b = 0; b < LIVE; ++b) {
@@ -633,7 +613,7 @@ int launch_rows(const moe_product_shape* s, const Args& p, bool fast, hipStream_
         const int ct = (cols + S::COLS - 1) / S::COLS;
         const int64_t units = (int64_t(s->M) / S::ROWS + s->E + 1) * ct;
         if (units > MOST_GROUPS) return fail(DYNB_E_UNSUPPORTED, std::string(who) + ": too many results");
-        return launch_tiles<DIR, bf16_t, S>(p, S::WAVES == 8 ? std::min<int64_t>(units, CUS) : units, units, ct, 1, Shares{}, nullptr, st, who);
+        return launch_tiles<DIR, bf16_t, S>(p, S::BIG ? std::min<int64_t>(units, CUS) : units, units, ct, 1, Shares{}, nullptr, st, who);
     };
     if (fast) switch (kind_of(s)) {
         case BIG: return launch(Big{});
