@@ -173,7 +173,6 @@ __device__ __forceinline__ bf16x8 read_across(lds_ptr p)
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 __device__ __forceinline__ bf16x8 read_along(lds_ptr p) { return *reinterpret_cast<const __attribute__((address_space(3))) bf16x8*>(p); }
-__device__ const u32x4 zeros_16 = {0u, 0u, 0u, 0u};            // what stands behind the end of a sum
 
 // A kind of tile: CG x RG waves, each with FA x 32 columns and NB x 32 rows of the results
 template <int FA_, int NB_, int CG_, int RG_, int BUFS_, int SIMD_>
@@ -181,7 +180,7 @@ struct Kind {
     static constexpr bool BIG = FA_ * CG_ == 8;
     static constexpr int FA = FA_, NB = NB_, CG = CG_, RG = RG_, BUFS = BUFS_, SIMD = SIMD_, WAVES = CG * RG, THREADS = WAVES * 64, COLS = CG * FA * 32, ROWS = RG * NB * 32;
 };
-using Big = Kind<2, 4, 4, 2, 2, 2>;      // 256 x 256: an operand's bytes are multiplied 256 times
+using Big = Kind<4, 4, 2, 2, 2, 1>;      // 256 x 256: an operand's bytes are multiplied 256 times
 using Mid = Kind<2, 2, 2, 2, 2, 2>;      // 128 x 128, two workgroups a CU
 using Few = Kind<1, 2, 4, 1, 3, 2>;      // 128 columns x 64 rows, two chunks ahead: a stream of weights
 
@@ -218,7 +217,7 @@ struct Tile {
     int slot;                            // of the partial sums, or -1
 };
 
-template <int DIR, typename TO, class S>
+template <int DIR, typename TO, class S, bool FUSED>
 __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int units, int ct, int rt, Shares shares, float* __restrict__ partial)
 {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
@@ -291,34 +290,37 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
     }
 
     // ---- copying: wave w's blocks are w, w + WAVES ..; a request is a scalar base, which moves on with the chunks, and a lane's offset, which a tile keeps
-    // (but for gathered rows as places of the sum)
+    // (but for gathered rows as places of the sum).  Behind the end of a sum the last place that there is is copied again, and cleared in LDS before use.
     const uint32_t piece = uint32_t(lane & 7) * 16u;
     const char *a_base = nullptr, *b_base = nullptr;
-    uint32_t a_off[AU][EACH], b_off[BU][EACH];
-    const size_t a_step = DIR == FORWARD ? 128 : DIR == GRAD_INPUT ? size_t(p.K) * 128 : p.g.perm ? 0 : size_t(p.a_stride) * 128;
+    uint32_t a_off[AU][EACH], b_off[BU][EACH], more[EACH];
+    const bool gathers = DIR != GRAD_INPUT && p.g.perm != nullptr;
+    const size_t a_step = DIR == FORWARD ? 128 : DIR == GRAD_INPUT ? size_t(p.K) * 128 : gathers ? 0 : size_t(p.a_stride) * 128;
     const size_t b_step = B_ACROSS ? size_t(p.b_stride) * 128 : 128;
     int32_t uses[EACH];                                        // weights' gradient: `perm` at this lane's places of the chunk that is asked for next
     int32_t rows_then[BU][EACH];                               // forward: `perm` at the next tile's rows
     Tile asked = {};                                           // the tile that is asked for
+    int z_asked = 0;                                           // ... and the chunk: its first place
     auto look_up_rows = [&](const Tile& t) {
         if constexpr (DIR == FORWARD)
-            if (p.g.perm)
+            if (gathers)
 #pragma unroll
                 for (int i = 0; i < BU; ++i)
 #pragma unroll
                     for (int j = 0; j < EACH; ++j) rows_then[i][j] = p.g.perm[t.begin + min(i * 64 + (lane >> 5) * 32 + copied_row(wave + j * S::WAVES, lane), t.rows - 1)];
     };
-    auto look_up_places = [&](int z0) {
+    auto look_up_places = [&]() {
         if constexpr (DIR == GRAD_WEIGHT)
-            if (p.g.perm)
+            if (gathers)
 #pragma unroll
-                for (int j = 0; j < EACH; ++j) uses[j] = p.g.perm[asked.begin + min(z0 + copied_place(wave + j * S::WAVES, lane), asked.depth - 1)];
+                for (int j = 0; j < EACH; ++j) uses[j] = p.g.perm[asked.begin + min(z_asked + copied_place(wave + j * S::WAVES, lane), asked.depth - 1)];
     };
     auto open = [&](const Tile& t) {
         asked = t;
+        z_asked = 0;
         const size_t w = size_t(t.e) * size_t(p.N) * size_t(p.K);
-        a_base = reinterpret_cast<const char*>(DIR == GRAD_WEIGHT ? p.a + (p.g.perm ? 0 : t.begin * p.a_stride) : DIR == FORWARD ? p.a + w + size_t(t.c0) * size_t(p.K) : p.a + w);
-        b_base = reinterpret_cast<const char*>(DIR == FORWARD && p.g.perm ? p.b : p.b + t.begin * p.b_stride);
+        a_base = reinterpret_cast<const char*>(DIR == GRAD_WEIGHT ? p.a + (gathers ? 0 : t.begin * p.a_stride) : DIR == FORWARD ? p.a + w + size_t(t.c0) * size_t(p.K) : p.a + w);
+        b_base = reinterpret_cast<const char*>(DIR == FORWARD && gathers ? p.b : p.b + t.begin * p.b_stride);
 #pragma unroll
         for (int j = 0; j < EACH; ++j) {
             const int block = wave + j * S::WAVES, s_q = copied_row(block, lane), z = copied_place(block, lane);
@@ -328,46 +330,70 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
                 if constexpr (DIR == FORWARD)                  // (the features in the order that gives a lane 16 neighbours)
                     a_off[i][j] = uint32_t(min(i * 64 + (lane >> 5) * 32 + (s_q >> 2 & 1) * 16 + (s_q >> 3) * 4 + (s_q & 3), cols - 1 - t.c0)) * uint32_t(p.K) * 2u + piece;
                 else if constexpr (DIR == GRAD_INPUT) a_off[i][j] = uint32_t(z) * uint32_t(p.K) * 2u + col;
-                else a_off[i][j] = (p.g.perm ? 0u : uint32_t(z) * uint32_t(p.a_stride) * 2u) + col;
+                else a_off[i][j] = (gathers ? 0u : uint32_t(z) * uint32_t(p.a_stride) * 2u) + col;
             }
 #pragma unroll
             for (int i = 0; i < BU; ++i) {
                 if constexpr (B_ACROSS) b_off[i][j] = uint32_t(z) * uint32_t(p.b_stride) * 2u + uint32_t(min(t.r0 + i * 64 + (lane & 7) * 8, p.N - 8)) * 2u;
                 else {
                     uint32_t row = uint32_t(min(i * 64 + (lane >> 5) * 32 + s_q, t.rows - 1));
-                    if (DIR == FORWARD && p.g.perm) row = p.g.row_of(rows_then[i][j]);
+                    if (DIR == FORWARD && gathers) row = p.g.row_of(rows_then[i][j]);
                     b_off[i][j] = row * uint32_t(p.b_stride) * 2u + piece;
                 }
             }
         }
-        look_up_places(0);
+        look_up_places();
     };
-    uint32_t fill = 0, take = 0;                               // the chunk's place in LDS that is filled next, and the one that is read
-    // requests i0 .. i1 of the chunk that begins at place z0 of the sum
-    auto request = [&](lds_ptr to, int z0, int i0, int i1) {
-        const bool whole = z0 + 64 <= asked.depth;
+    // ahead of a chunk's requests
+    auto prepare = [&]() {
+        const int rest = asked.depth - z_asked;
+        if (rest < 64) {                                       // (the tile's last: its offsets are not used again)
+#pragma unroll
+            for (int j = 0; j < EACH; ++j) {
+                const int z = copied_place(wave + j * S::WAVES, lane);
+                const uint32_t places = uint32_t(max(z - (rest - 1), 0)), pieces = (lane & 7) * 8 >= rest ? piece : 0u;
+#pragma unroll
+                for (int i = 0; i < AU; ++i) a_off[i][j] -= DIR == FORWARD ? pieces : DIR == GRAD_INPUT ? places * uint32_t(p.K) * 2u : gathers ? 0u : places * uint32_t(p.a_stride) * 2u;
+#pragma unroll
+                for (int i = 0; i < BU; ++i) b_off[i][j] -= B_ACROSS ? places * uint32_t(p.b_stride) * 2u : pieces;
+            }
+        }
+        if constexpr (DIR == GRAD_WEIGHT) {
+#pragma unroll
+            for (int j = 0; j < EACH; ++j) more[j] = gathers ? p.g.row_of(uses[j]) * uint32_t(p.a_stride) * 2u : 0u;
+        }
+    };
+    // requests i0 .. i1 of a chunk
+    auto request = [&](lds_ptr to, int i0, int i1) {
 #pragma unroll
         for (int n = 0; n < REQUESTS; ++n) {
             if (n < i0 || n >= i1) continue;
             const int i = n / EACH, j = n % EACH, block = wave + j * S::WAVES;
-            const bool is_a = i < AU;
-            const lds_ptr lds_at = to + uint32_t(is_a ? i * UA + block * (A_ACROSS ? YBLOCK : XBLOCK) : AU * UA + (i - AU) * UB + block * (B_ACROSS ? YBLOCK : XBLOCK));
-            const char* const base = is_a ? a_base : b_base;
-            uint32_t off = is_a ? a_off[i % AU][j] : b_off[(i - AU + BU) % BU][j];
-            if (DIR == GRAD_WEIGHT && is_a && p.g.perm) off += p.g.row_of(uses[j]) * uint32_t(p.a_stride) * 2u;
-            if (whole) lds_copy16_to(base, off, lds_at);
-            else {                                             // (zeros behind the end of the sum)
-                const int z = (is_a ? A_ACROSS : B_ACROSS) ? copied_place(block, lane) : (lane & 7) * 8;
-                lds_copy16_from(z0 + z < asked.depth ? base + off : reinterpret_cast<const char*>(&zeros_16), lds_at);
-            }
+            if (i < AU) lds_copy16_to(a_base, DIR == GRAD_WEIGHT ? a_off[i % AU][j] + more[j] : a_off[i % AU][j], to + uint32_t(i * UA + block * (A_ACROSS ? YBLOCK : XBLOCK)));
+            else lds_copy16_to(b_base, b_off[(i - AU + BU) % BU][j], to + uint32_t(AU * UA + (i - AU) * UB + block * (B_ACROSS ? YBLOCK : XBLOCK)));
         }
     };
-    auto requested = [&](int z0) {
-        fill = fill == AHEAD * BUF ? 0 : fill + BUF;
+    auto requested = [&]() {
+        z_asked += 64;
+        if (z_asked >= asked.depth) return;
         a_base += a_step;
         b_base += b_step;
-        if (z0 + 64 < asked.depth) look_up_places(z0 + 64);
+        look_up_places();
     };
+    // zeros behind the end of the sum, each wave in what it has copied
+    auto clear = [&](lds_ptr at, int rest) {
+#pragma unroll
+        for (int n = 0; n < REQUESTS; ++n) {
+            const int i = n / EACH, j = n % EACH, block = wave + j * S::WAVES;
+            const bool is_a = i < AU;
+            if (((is_a ? A_ACROSS : B_ACROSS) ? copied_place(block, lane) : (lane & 7) * 8) >= rest)
+                *(__attribute__((address_space(3))) u32x4*)(at + uint32_t((is_a ? i * UA : AU * UA + (i - AU) * UB) + block * ((is_a ? A_ACROSS : B_ACROSS) ? YBLOCK : XBLOCK) + lane * 16)) =
+                    u32x4{0u, 0u, 0u, 0u};
+        }
+        meet();
+    };
+    uint32_t fill = 0, take = 0;                               // the chunk's place in LDS that is filled next, and the one that is read
+    auto next_place = [&](uint32_t at) { return at == AHEAD * BUF ? 0 : at + BUF; };
 
     // ---- a tile after the other
     const uint32_t a_slot = A_ACROSS ? places_at(lane, false) : fragment_at(q, hk), b_slot = B_ACROSS ? places_at(lane, true) : fragment_at(q, hk);
@@ -379,11 +405,14 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
         if (nchunk > 0 && !primed) {
             look_up_rows(now);
             open(now);
+            fill = take;                                       // (what was asked for behind the last tile is overwritten)
 #pragma unroll
             for (int c = 0; c < AHEAD; ++c)
                 if (c < nchunk) {
-                    request(lds + fill, c * 64, 0, REQUESTS);
-                    requested(c * 64);
+                    prepare();
+                    request(lds + fill, 0, REQUESTS);
+                    requested();
+                    fill = next_place(fill);
                 }
             stores = 0;
         }
@@ -412,64 +441,93 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
                 for (int b = 0; b < LIVE; ++b)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.f;
-#pragma unroll 1
-            for (int c = 0; c < nchunk; ++c) {
-                arrive(c);
-                int z_ask = c + AHEAD < nchunk ? (c + AHEAD) * 64 : -1;
-                if (STAYS && c == 0) {
-                    then = next_tile();
-                    if (then.rows > 0 && then.depth > 0) look_up_rows(then);
-                }
-                if (STAYS && c == nchunk - 1 && then.rows > 0 && then.depth > 0) {
-                    open(then);
-                    z_ask = 0;
-                }
-                // (what is read and what is filled are said to be apart: else every transposing read would wait for all requests)
-                auto chunk = [&](const lds_ptr __restrict__ from, const lds_ptr __restrict__ to) {
+            // The last K-step of a chunk is multiplied behind the next one's arrival: under it the next chunk's first fragments come from LDS, and the requests are
+            // made, one of each a product.  (Ahead of the first chunk, zeros.)  Nothing in a chunk branches.
+            bf16x8 af[2][FA], bf[2][LIVE > 0 ? LIVE : 1];
+#pragma unroll
+            for (int a = 0; a < FA; ++a) af[1][a] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
+#pragma unroll
+            for (int b = 0; b < LIVE; ++b) bf[1][b] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
+            // (what is read and what is filled are said to be apart: else every transposing read would wait for all requests)
+            auto chunk = [&](const lds_ptr __restrict__ from, const lds_ptr __restrict__ to, auto asks) {
+                constexpr int ASKS = decltype(asks)::value ? REQUESTS : 0;
                 const lds_ptr au = from + (uint32_t((cg * FA / 2) * UA) + a_slot + uint32_t(FA == 1 ? (cg & 1) * (A_ACROSS ? 64 : 512) : 0));
                 const lds_ptr bu = from + (uint32_t(AU * UA) + b_slot);
-                bf16x8 af[2][FA], bf[2][LIVE > 0 ? LIVE : 1];
-                auto read = [&](int ks) {
+                // fragments i0 .. i1 of K-step ks
+                auto read = [&](int ks, int i0, int i1) {
 #pragma unroll
-                    for (int a = 0; a < FA; ++a) {
-                        if constexpr (A_ACROSS) af[ks & 1][a] = read_across(au + uint32_t(a / 2 * UA + a % 2 * 64 + ks * 2 * YBLOCK));
-                        else af[ks & 1][a] = read_along(au + (a / 2 * UA + a % 2 * 512 + ks * 32));
-                    }
-#pragma unroll
-                    for (int b = 0; b < LIVE; ++b) {
-                        const lds_ptr at = bu + uint32_t((b * S::RG + rg) / 2 * UB + (b * S::RG + rg) % 2 * (B_ACROSS ? 64 : 512));
-                        if constexpr (B_ACROSS) bf[ks & 1][b] = read_across(at + uint32_t(ks * 2 * YBLOCK));
-                        else bf[ks & 1][b] = read_along(at + ks * 32);
-                    }
-                };
-                auto ask = [&](int ks) {
-                    if (z_ask >= 0 && ks < 2) request(to, z_ask, ks * REQUESTS / 2, (ks + 1) * REQUESTS / 2);
-                    __builtin_amdgcn_sched_barrier(0);
-                };
-                if constexpr (LIVE == 0) { ask(0); ask(1); }
-                else {
-                    if (S::BUFS > 2) { ask(0); ask(1); }       // (a stream of weights: first of all)
-                    read(0);
-                    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                    for (int ks = 0; ks < 4; ++ks)
-#pragma unroll
-                        for (int b = 0; b < LIVE; ++b) {
-#pragma unroll
-                            for (int a = 0; a < FA; ++a) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(af[ks & 1][a], bf[ks & 1][b], acc[a][b], 0, 0, 0);
-                            __builtin_amdgcn_sched_barrier(0);
-                            if (b == 0 && ks < 3) {
-                                read(ks + 1);
-                                __builtin_amdgcn_sched_barrier(0);
-                            }
-                            if (S::BUFS == 2 && b == LIVE / 2) ask(ks);
+                    for (int a = 0; a < FA; ++a)
+                        if (a >= i0 && a < i1) {
+                            if constexpr (A_ACROSS) af[ks & 1][a] = read_across(au + uint32_t(a / 2 * UA + a % 2 * 64 + ks * 2 * YBLOCK));
+                            else af[ks & 1][a] = read_along(au + (a / 2 * UA + a % 2 * 512 + ks * 32));
                         }
-                }
+#pragma unroll
+                    for (int b = 0; b < LIVE; ++b)
+                        if (FA + b >= i0 && FA + b < i1) {
+                            const lds_ptr at = bu + uint32_t((b * S::RG + rg) / 2 * UB + (b * S::RG + rg) % 2 * (B_ACROSS ? 64 : 512));
+                            if constexpr (B_ACROSS) bf[ks & 1][b] = read_across(at + uint32_t(ks * 2 * YBLOCK));
+                            else bf[ks & 1][b] = read_along(at + ks * 32);
+                        }
+                    __builtin_amdgcn_sched_barrier(0);
                 };
-                chunk(lds + take, lds + fill);
-                if (z_ask >= 0) requested(z_ask);
-                take = take == AHEAD * BUF ? 0 : take + BUF;
+                // the products of K-step ks (-1: the chunk before's last); in the first half of them K-step ks + 1 is read, and with the first ones requests are made
+                auto step = [&](int ks, int asks_before, int asks_behind) {
+                    constexpr int PRODUCTS = FA * LIVE, FRAGMENTS = FA + LIVE;
+#pragma unroll
+                    for (int m = 0; m < PRODUCTS; ++m) {
+                        const int a = m % FA, b = m / FA;
+                        acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(af[ks & 1][a], bf[ks & 1][b], acc[a][b], 0, 0, 0);
+                        __builtin_amdgcn_sched_barrier(0);
+                        if (ks < 3) read(ks + 1, min(FRAGMENTS, m * FRAGMENTS * 2 / PRODUCTS), min(FRAGMENTS, (m + 1) * FRAGMENTS * 2 / PRODUCTS));
+                        request(to, asks_before + m * (asks_behind - asks_before) / PRODUCTS, asks_before + (m + 1) * (asks_behind - asks_before) / PRODUCTS);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                };
+                if constexpr (LIVE == 0) request(to, 0, ASKS);
+                else {
+                    // (the last step's fragments are here, all waves have met behind their reads: said so, or they would be waited for behind the next ones)
+#pragma unroll
+                    for (int a = 0; a < FA; ++a) asm volatile("" : "+v"(af[1][a]));
+#pragma unroll
+                    for (int b = 0; b < LIVE; ++b) asm volatile("" : "+v"(bf[1][b]));
+                    constexpr int FIRST = S::BUFS > 2 ? ASKS : ASKS / 2;       // (a stream of weights: all at once)
+                    step(-1, 0, FIRST);
+                    step(0, FIRST, ASKS);
+                    step(1, ASKS, ASKS);
+                    step(2, ASKS, ASKS);
+                }
+            };
+            int c = 0;
+            auto through = [&](int end, auto asks) {
+#pragma unroll 1
+                for (; c < end; ++c) {
+                    arrive(c);
+                    if (c == nchunk - 1 && now.depth % 64 != 0) clear(lds + take, now.depth - c * 64);
+                    if constexpr (STAYS) {
+                        if (c == 0) {
+                            then = next_tile();
+                            if (then.depth > 0) look_up_rows(then);
+                        }
+                        // (behind the last tile the last chunk is asked for again)
+                        if (c == nchunk - 1 && then.depth > 0) open(then);
+                    }
+                    if constexpr (decltype(asks)::value) {
+                        if (z_asked < asked.depth) prepare();
+                        chunk(lds + take, lds + fill, asks);
+                        requested();
+                        fill = next_place(fill);
+                    } else chunk(lds + take, lds + fill, asks);
+                    take = next_place(take);
+                }
+            };
+            if constexpr (STAYS) through(nchunk, std::true_type{});
+            else {
+                through(nchunk - AHEAD, std::true_type{});
+                through(nchunk, std::false_type{});
             }
+            if (nchunk > 0)
+#pragma unroll
+                for (int m = 0; m < FA * LIVE; ++m) acc[m % FA][m / FA] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(af[1][m % FA], bf[1][m / FA], acc[m % FA][m / FA], 0, 0, 0);
             // a lane: 16 neighbouring columns of row q of every block
 #pragma unroll
             for (int b = 0; b < LIVE; ++b) {
@@ -486,10 +544,10 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
                             float v[8];
 #pragma unroll
                             for (int i = 0; i < 8; ++i) v[i] = acc[a][b][8 * h + i];
-                            if (DIR == FORWARD && p.relu)
+                            if (DIR == FORWARD && FUSED)
 #pragma unroll
                                 for (int i = 0; i < 8; ++i) v[i] = v[i] < 0.f ? 0.f : v[i];                  // (a NaN stays one)
-                            if (DIR == GRAD_INPUT && p.act) {
+                            if constexpr (DIR == GRAD_INPUT && FUSED) {
                                 const bf16x8 on = *reinterpret_cast<const bf16x8*>(p.act + int64_t(now.begin + r) * p.act_stride + c + at);
 #pragma unroll
                                 for (int i = 0; i < 8; ++i) v[i] = float(on[i]) > 0.f ? v[i] : 0.f;
@@ -520,6 +578,7 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
         stores = now.c0 + cg * (FA * 32) + FA * 32 <= cols ? min(mine, NB) * FA * 2 : 0;
         now = then;
     }
+    answered_but<0>();                                         // (nothing is on its way to LDS that another workgroup may have next)
 }
 
 // Gradients whose sum a border between two lanes cuts: their parts, in order.  A workgroup looks after a share of the elements for one border, and only for the
@@ -588,18 +647,18 @@ KindOf kind_of(const moe_product_shape* s)
     return each >= 192 ? BIG : each >= 64 ? MID : FEW;
 }
 
-template <int DIR, typename TO, class S>
+template <int DIR, typename TO, class S, bool FUSED = false>
 int launch_tiles(const Args& p, int64_t grid, int64_t units, int ct, int rt, const Shares& shares, float* partial, hipStream_t st, const char* who)
 {
     static std::atomic<uint64_t> attr_set{0};                 // one bit per device: LDS beyond 64 KB
     int dev = 0;
     hipError_t e = hipGetDevice(&dev);
     if (e == hipSuccess && !(attr_set.load() >> (dev & 63) & 1)) {
-        e = hipFuncSetAttribute(reinterpret_cast<const void*>(k_product<DIR, TO, S>), hipFuncAttributeMaxDynamicSharedMemorySize, int(LDS_BYTES<DIR, S>));
+        e = hipFuncSetAttribute(reinterpret_cast<const void*>(k_product<DIR, TO, S, FUSED>), hipFuncAttributeMaxDynamicSharedMemorySize, int(LDS_BYTES<DIR, S>));
         if (e == hipSuccess) attr_set.fetch_or(uint64_t(1) << (dev & 63));
     }
     if (e != hipSuccess) return fail(DYNB_E_HIP, std::string(who) + ": " + hipGetErrorString(e));
-    hipLaunchKernelGGL((k_product<DIR, TO, S>), dim3(unsigned(grid)), dim3(S::THREADS), (LDS_BYTES<DIR, S>), st, p, int(units), ct, rt, shares, partial);
+    hipLaunchKernelGGL((k_product<DIR, TO, S, FUSED>), dim3(unsigned(grid)), dim3(S::THREADS), (LDS_BYTES<DIR, S>), st, p, int(units), ct, rt, shares, partial);
     return launched(who);
 }
 
@@ -613,7 +672,8 @@ int launch_rows(const moe_product_shape* s, const Args& p, bool fast, hipStream_
         const int ct = (cols + S::COLS - 1) / S::COLS;
         const int64_t units = (int64_t(s->M) / S::ROWS + s->E + 1) * ct;
         if (units > MOST_GROUPS) return fail(DYNB_E_UNSUPPORTED, std::string(who) + ": too many results");
-        return launch_tiles<DIR, bf16_t, S>(p, S::BIG ? std::min<int64_t>(units, CUS) : units, units, ct, 1, Shares{}, nullptr, st, who);
+        const auto run = p.relu || p.act ? launch_tiles<DIR, bf16_t, S, true> : launch_tiles<DIR, bf16_t, S, false>;
+        return run(p, S::BIG ? std::min<int64_t>(units, CUS) : units, units, ct, 1, Shares{}, nullptr, st, who);
     };
     if (fast) switch (kind_of(s)) {
         case BIG: return launch(Big{});
