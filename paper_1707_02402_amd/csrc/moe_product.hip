@@ -174,6 +174,13 @@ __device__ __forceinline__ bf16x8 read_across(lds_ptr p)
 }
 __device__ __forceinline__ bf16x8 read_along(lds_ptr p) { return *reinterpret_cast<const __attribute__((address_space(3))) bf16x8*>(p); }
 
+// what this wave's lanes wrote to LDS is there for its other lanes
+__device__ __forceinline__ void wave_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // A kind of tile: CG x RG waves, each with FA x 32 columns and NB x 32 rows of the results
 template <int FA_, int NB_, int CG_, int RG_, int BUFS_, int SIMD_>
 struct Kind {
@@ -217,6 +224,17 @@ struct Tile {
     int slot;                            // of the partial sums, or -1
 };
 
+// Unit u of rows x ct tiles: TALL rows walk the columns together.  Four for Big, so that the workgroups of a die, which run 32 neighbours at a time, share both
+// operands in its L2 (8 columns and 4 rows instead of 32 and 1; 8192 rows, channels and features, one expert: forward 1264 -> 805 us).  One for the others, whose rows
+// are of different experts (1024 experts of 64 rows: 888 us, four 1049).
+struct Place { int row, col; };
+template <int TALL>
+__device__ __forceinline__ Place walk(int u, int rows, int ct)
+{
+    const int group = u / (TALL * ct), in = u - group * TALL * ct, tall = min(TALL, rows - group * TALL);
+    return Place{group * TALL + in % tall, in / tall};
+}
+
 template <int DIR, typename TO, class S, bool FUSED>
 __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int units, int ct, int rt, Shares shares, float* __restrict__ partial)
 {
@@ -239,7 +257,8 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
     const int count = DIR == GRAD_WEIGHT ? 0 : STAYS ? (units - place + int(gridDim.x) - 1) / int(gridDim.x) : 1;
     int at_unit = -1;
     // weights' gradient: a lane's groups
-    const int w_tile = place % (ct * rt), w_lane = place / (ct * rt);
+    const int w_lane = place / (ct * rt);
+    const Place w_tile = walk<4>(place % (ct * rt), rt, ct);
     const int64_t w_from = shares.each * w_lane, w_to = w_from + shares.each;
     int w_e = 0;
     auto tile_of = [&](const Piece& at, int col) {
@@ -249,8 +268,9 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
         meet();
         if (tid < LIST && from + tid < count) {
             const int unit = place + (from + tid) * int(gridDim.x);
-            const Piece at = find_piece_alone(p.g, S::ROWS, unit / ct);
-            *reinterpret_cast<u32x4*>(lds_raw + BUF * S::BUFS + tid * 16) = u32x4{uint32_t(at.e), uint32_t(at.begin), uint32_t(at.rows), uint32_t(unit % ct)};
+            const Place w = walk<4>(unit, units / ct, ct);
+            const Piece at = find_piece_alone(p.g, S::ROWS, w.row);
+            *reinterpret_cast<u32x4*>(lds_raw + BUF * S::BUFS + tid * 16) = u32x4{uint32_t(at.e), uint32_t(at.begin), uint32_t(at.rows), uint32_t(w.col)};
         }
         meet();
     };
@@ -264,7 +284,7 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
                 if (s >= w_to) break;
                 const int lo = int(min(max(w_from - first, int64_t(0)), int64_t(n))), hi = int(min(max(w_to - first, int64_t(0)), int64_t(n)));
                 if (n == 0 ? s < w_from : hi <= lo) continue;
-                t = Tile{w_e, a + lo, p.N - w_tile / ct * S::ROWS, w_tile % ct * S::COLS, w_tile / ct * S::ROWS, hi - lo, hi - lo == n ? -1 : 2 * w_lane + (lo > 0 ? 0 : 1)};
+                t = Tile{w_e, a + lo, p.N - w_tile.row * S::ROWS, w_tile.col * S::COLS, w_tile.row * S::ROWS, hi - lo, hi - lo == n ? -1 : 2 * w_lane + (lo > 0 ? 0 : 1)};
                 t.rows = min(t.rows, S::ROWS);
                 ++w_e;
                 break;
@@ -280,7 +300,8 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
                 if (at.rows > 0) { t = tile_of(at, __builtin_amdgcn_readfirstlane(v.w)); break; }
             }
         } else if (++at_unit == 0) {
-            t = tile_of(find_piece(p.g, S::ROWS, place / ct), place % ct);
+            const Place w = walk<1>(place, units / ct, ct);
+            t = tile_of(find_piece(p.g, S::ROWS, w.row), w.col);
         }
         return t;
     };
@@ -422,7 +443,9 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
         auto arrive = [&](int c) {                             // chunk c is there, and all waves are done with the one before
             if constexpr (AHEAD == 1) {
                 if (c == 0 && stores > 0) {
-                    if (stores >= 16) answered_but<16>();
+                    if (stores >= 60) answered_but<60>();
+                    else if (stores >= 32) answered_but<32>();
+                    else if (stores >= 16) answered_but<16>();
                     else if (stores >= 8) answered_but<8>();
                     else answered_but<4>();
                 } else answered_but<0>();
@@ -498,6 +521,7 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
                 }
             };
             int c = 0;
+            uint32_t last = take;                              // the last chunk's place
             auto through = [&](int end, auto asks) {
 #pragma unroll 1
                 for (; c < end; ++c) {
@@ -517,6 +541,7 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
                         requested();
                         fill = next_place(fill);
                     } else chunk(lds + take, lds + fill, asks);
+                    last = take;
                     take = next_place(take);
                 }
             };
@@ -525,46 +550,95 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
                 through(nchunk - AHEAD, std::true_type{});
                 through(nchunk, std::false_type{});
             }
-            if (nchunk > 0)
+            // (without a chunk, zeros: a branch around this would have the accumulators copied)
 #pragma unroll
-                for (int m = 0; m < FA * LIVE; ++m) acc[m % FA][m / FA] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(af[1][m % FA], bf[1][m / FA], acc[m % FA][m / FA], 0, 0, 0);
-            // a lane: 16 neighbouring columns of row q of every block
+            for (int m = 0; m < FA * LIVE; ++m) acc[m % FA][m / FA] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(af[1][m % FA], bf[1][m / FA], acc[m % FA][m / FA], 0, 0, 0);
+            // A lane has 16 neighbouring columns of row q of every block.  They go by way of LDS, each wave its own share of the last chunk's place, and leave with all
+            // lanes of a store side by side: 16 bytes of every row a lane took the stores' address unit 64 clocks each, 8 us of a tile's 37 (forward, 1024 channels).
+            if (nchunk > 0) meet();                            // (all waves are done with that chunk)
+            const lds_ptr mine_at = lds + last + uint32_t(wave) * (BUF / S::WAVES / 16 * 16);
+            auto put = [&](auto* to, int64_t pitch) {          // to: row 0 of the tile, this wave's first column
+                using T = std::remove_pointer_t<decltype(to)>;
+                constexpr int P = 16 / int(sizeof(T)), LANES = FA * 32 / P, AT_ONCE = 64 / LANES, PITCH = FA * 32 * int(sizeof(T)) + 16;
+                static_assert(32 * PITCH <= int(BUF / S::WAVES), "room");
+                const int col = lane % LANES * P, row = lane / LANES;
+                const bool on = now.c0 + cg * (FA * 32) + col < cols;
+                // (one address each, the steps are constants or scalars: an address a store was one too many to keep)
+                const lds_ptr in_at = mine_at + uint32_t(q * PITCH + 16 * hk * int(sizeof(T))), out_at = mine_at + uint32_t(row * PITCH + col * int(sizeof(T)));
+                char* lane_to = reinterpret_cast<char*>(to + int64_t(rg * 32 + row) * pitch + col);
+                const int64_t step = AT_ONCE * pitch * int(sizeof(T)), to_next = S::RG * 32 * pitch * int(sizeof(T));
+                const char* act_at = nullptr;
+                int64_t act_step = 0, act_next = 0;
+                if constexpr (DIR == GRAD_INPUT && FUSED) {
+                    act_at = reinterpret_cast<const char*>(p.act + (now.begin + rg * 32 + row) * p.act_stride + now.c0 + cg * (FA * 32) + col);
+                    act_step = AT_ONCE * p.act_stride * 2;
+                    act_next = S::RG * 32 * p.act_stride * 2;
+                }
 #pragma unroll
-            for (int b = 0; b < LIVE; ++b) {
-                const int r = (b * S::RG + rg) * 32 + q;
-                if (r >= now.rows) continue;
-                const int c = now.c0 + cg * (FA * 32) + 16 * hk;
-                auto put = [&](auto* to) {
+                for (int b = 0; b < LIVE; ++b) {
 #pragma unroll
-                    for (int a = 0; a < FA; ++a)
+                    for (int a = 0; a < FA; ++a) {
+                        if (nchunk == 0) break;                // (zeros, and LDS is the next tile's)
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
-                            const int at = a * 32 + h * 8;
-                            if (c + at >= cols) continue;
                             float v[8];
 #pragma unroll
                             for (int i = 0; i < 8; ++i) v[i] = acc[a][b][8 * h + i];
                             if (DIR == FORWARD && FUSED)
 #pragma unroll
                                 for (int i = 0; i < 8; ++i) v[i] = v[i] < 0.f ? 0.f : v[i];                  // (a NaN stays one)
-                            if constexpr (DIR == GRAD_INPUT && FUSED) {
-                                const bf16x8 on = *reinterpret_cast<const bf16x8*>(p.act + int64_t(now.begin + r) * p.act_stride + c + at);
-#pragma unroll
-                                for (int i = 0; i < 8; ++i) v[i] = float(on[i]) > 0.f ? v[i] : 0.f;
-                            }
-                            if constexpr (std::is_same_v<decltype(to), float*>) {
-                                *reinterpret_cast<u32x4*>(to + at) = u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
-                                *reinterpret_cast<u32x4*>(to + at + 4) = u32x4{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])};
+                            const lds_ptr at = in_at + (a * 32 + 8 * h) * int(sizeof(T));
+                            using lds_u32x4 = __attribute__((address_space(3))) u32x4;
+                            if constexpr (sizeof(T) == 4) {
+                                *(lds_u32x4*)at = u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+                                *(lds_u32x4*)(at + 16) = u32x4{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])};
                             } else
-                                *reinterpret_cast<u32x4*>(to + at) = u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+                                *(lds_u32x4*)at = u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
                         }
-                };
-                if constexpr (DIR == GRAD_WEIGHT) {
-                    const size_t row = size_t(now.r0 + r) * size_t(p.K) + size_t(c), all = size_t(p.N) * size_t(p.K);
-                    if (now.slot >= 0) put(partial + size_t(now.slot) * all + row);
-                    else put(static_cast<TO*>(p.out) + size_t(now.e) * all + row);
-                } else put(static_cast<TO*>(p.out) + int64_t(now.begin + r) * p.out_stride + c);
-            }
+                        __builtin_amdgcn_sched_barrier(0);     // (all accumulators at once in other registers would have no room)
+                    }
+                    wave_sync();
+                    constexpr int STORES = 32 / AT_ONCE;
+                    u32x4 v[STORES], act[STORES];
+#pragma unroll
+                    for (int i = 0; i < STORES; ++i) v[i] = *(const __attribute__((address_space(3))) u32x4*)(out_at + i * AT_ONCE * PITCH);
+                    if (nchunk == 0)
+#pragma unroll
+                        for (int i = 0; i < STORES; ++i) v[i] = u32x4{0u, 0u, 0u, 0u};
+                    auto one = [&](int i) {
+                        if constexpr (DIR == GRAD_INPUT && FUSED)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                v[i][j] = (__uint_as_float(act[i][j] << 16) > 0.f ? v[i][j] & 0xffffu : 0u) | (__uint_as_float(act[i][j] & 0xffff0000u) > 0.f ? v[i][j] & 0xffff0000u : 0u);
+                        *reinterpret_cast<u32x4*>(lane_to + i * step) = v[i];
+                    };
+                    const int left = now.rows - (b * S::RG + rg) * 32;
+                    if (left >= 32 && now.c0 + cg * (FA * 32) + FA * 32 <= cols) {
+                        if constexpr (DIR == GRAD_INPUT && FUSED)
+#pragma unroll
+                            for (int i = 0; i < STORES; ++i) act[i] = *reinterpret_cast<const u32x4*>(act_at + i * act_step);
+#pragma unroll
+                        for (int i = 0; i < STORES; ++i) one(i);
+                    } else
+#pragma unroll
+                        for (int i = 0; i < STORES; ++i)
+                            if (row + i * AT_ONCE < left && on) {
+                                if constexpr (DIR == GRAD_INPUT && FUSED) act[i] = *reinterpret_cast<const u32x4*>(act_at + i * act_step);
+                                one(i);
+                            }
+                    lane_to += to_next;
+                    act_at += act_next;
+                    wave_sync();
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            };
+            const int first_col = now.c0 + cg * (FA * 32);
+            if constexpr (DIR == GRAD_WEIGHT) {
+                const size_t row = size_t(now.r0) * size_t(p.K) + size_t(first_col), all = size_t(p.N) * size_t(p.K);
+                if constexpr (std::is_same_v<TO, float>) put((now.slot >= 0 ? partial + size_t(now.slot) * all : static_cast<float*>(p.out) + size_t(now.e) * all) + row, p.K);
+                else if (now.slot >= 0) put(partial + size_t(now.slot) * all + row, p.K);
+                else put(static_cast<TO*>(p.out) + size_t(now.e) * all + row, p.K);
+            } else put(static_cast<TO*>(p.out) + int64_t(now.begin) * p.out_stride + first_col, p.out_stride);
             // (an end of its own for every size, so that the compiler keeps what is the same for all lanes in scalar registers)
             asm volatile("; %0" ::"n"(LIVE));
         };
@@ -574,8 +648,8 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
         if (!STAYS) return;
         if (nchunk == 0) then = next_tile();
         primed = nchunk > 0 && then.depth > 0;
-        // (the fewest that there can have been: none is made for columns beyond the last)
-        stores = now.c0 + cg * (FA * 32) + FA * 32 <= cols ? min(mine, NB) * FA * 2 : 0;
+        // (the fewest that there can have been: of the blocks that are whole)
+        stores = now.c0 + cg * (FA * 32) + FA * 32 <= cols ? max(0, (now.rows / 32 - rg + S::RG - 1) / S::RG) * FA * (DIR == GRAD_WEIGHT ? int(sizeof(TO)) : 2) : 0;
         now = then;
     }
     answered_but<0>();                                         // (nothing is on its way to LDS that another workgroup may have next)
