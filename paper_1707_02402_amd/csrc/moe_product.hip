@@ -193,7 +193,7 @@ using Few = Kind<1, 2, 4, 1, 3, 2>;      // 128 columns x 64 rows, two chunks ah
 
 constexpr int LIST = 256;                // tiles that a staying workgroup looks up at once
 template <int DIR, class S> constexpr uint32_t BUF_BYTES = uint32_t((S::COLS / 64) * (DIR == FORWARD ? XUNIT : YUNIT) + (S::ROWS / 64) * (DIR == GRAD_WEIGHT ? YUNIT : XUNIT));
-template <int DIR, class S> constexpr uint32_t LDS_BYTES = BUF_BYTES<DIR, S> * S::BUFS + (DIR != GRAD_WEIGHT ? LIST * 16 : 0);
+template <int DIR, class S> constexpr uint32_t LDS_BYTES = BUF_BYTES<DIR, S> * S::BUFS + (DIR != GRAD_WEIGHT && S::BIG ? LIST * 16 + S::ROWS * 4 : 0);
 
 // How the weights' gradient is shared out.  The sums run over the rows of a group; every tile of W_e's gradient is the work of one workgroup, or, where there are
 // fewer tiles than CUs, of several ("lanes") that take a share of all rows each.  A group counts as its rows and `extra` more for its tile's way to memory;
@@ -243,6 +243,7 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
     constexpr int AU = S::COLS / 64, BU = S::ROWS / 64, UA = A_ACROSS ? YUNIT : XUNIT, UB = B_ACROSS ? YUNIT : XUNIT, EACH = 8 / S::WAVES, REQUESTS = (AU + BU) * EACH;
     constexpr uint32_t BUF = BUF_BYTES<DIR, S>;
     constexpr int AHEAD = S::BUFS - 1, FA = S::FA, NB = S::NB;
+    static_assert(DIR != FORWARD || !STAYS || S::ROWS == S::THREADS, "a thread a row looks up");
     static_assert(AHEAD == 1 || !STAYS, "a tile's first chunk is asked for under the last one's last chunk");
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, q = lane & 31, hk = lane >> 5;
     const int cg = wave % S::CG, rg = wave / S::CG;
@@ -319,16 +320,21 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
     const size_t a_step = DIR == FORWARD ? 128 : DIR == GRAD_INPUT ? size_t(p.K) * 128 : gathers ? 0 : size_t(p.a_stride) * 128;
     const size_t b_step = B_ACROSS ? size_t(p.b_stride) * 128 : 128;
     int32_t uses[EACH];                                        // weights' gradient: `perm` at this lane's places of the chunk that is asked for next
-    int32_t rows_then[BU][EACH];                               // forward: `perm` at the next tile's rows
     Tile asked = {};                                           // the tile that is asked for
     int z_asked = 0;                                           // ... and the chunk: its first place
+    // forward: `perm` at the next tile's rows, into LDS (registers that a load is on its way to would be waited for under the next chunk's requests)
+    constexpr uint32_t ROWS_AT = BUF * S::BUFS + LIST * 16;
     auto look_up_rows = [&](const Tile& t) {
-        if constexpr (DIR == FORWARD)
+        if constexpr (DIR == FORWARD && STAYS)
             if (gathers)
-#pragma unroll
-                for (int i = 0; i < BU; ++i)
-#pragma unroll
-                    for (int j = 0; j < EACH; ++j) rows_then[i][j] = p.g.perm[t.begin + min(i * 64 + (lane >> 5) * 32 + copied_row(wave + j * S::WAVES, lane), t.rows - 1)];
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)(p.g.perm + t.begin + min(wave * 64 + lane, t.rows - 1)),
+                                                 (__attribute__((address_space(3))) uint32_t*)(lds + ROWS_AT + wave * 256), 4, 0, 0);
+    };
+    auto rows_looked_up = [&]() {
+        if (DIR == FORWARD && STAYS && gathers) {
+            answered_but<0>();
+            meet();
+        }
     };
     auto look_up_places = [&]() {
         if constexpr (DIR == GRAD_WEIGHT)
@@ -358,7 +364,7 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
                 if constexpr (B_ACROSS) b_off[i][j] = uint32_t(z) * uint32_t(p.b_stride) * 2u + uint32_t(min(t.r0 + i * 64 + (lane & 7) * 8, p.N - 8)) * 2u;
                 else {
                     uint32_t row = uint32_t(min(i * 64 + (lane >> 5) * 32 + s_q, t.rows - 1));
-                    if (DIR == FORWARD && gathers) row = p.g.row_of(rows_then[i][j]);
+                    if (DIR == FORWARD && gathers) row = p.g.row_of(STAYS ? *(const __attribute__((address_space(3))) int32_t*)(lds + ROWS_AT + row * 4) : p.g.perm[t.begin + int(row)]);
                     b_off[i][j] = row * uint32_t(p.b_stride) * 2u + piece;
                 }
             }
@@ -425,6 +431,7 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
         const int nchunk = (now.depth + 63) / 64;
         if (nchunk > 0 && !primed) {
             look_up_rows(now);
+            rows_looked_up();
             open(now);
             fill = take;                                       // (what was asked for behind the last tile is overwritten)
 #pragma unroll
@@ -533,6 +540,7 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
                             if (then.depth > 0) look_up_rows(then);
                         }
                         // (behind the last tile the last chunk is asked for again)
+                        if (nchunk == 1 && then.depth > 0) rows_looked_up();
                         if (c == nchunk - 1 && then.depth > 0) open(then);
                     }
                     if constexpr (decltype(asks)::value) {
@@ -781,7 +789,7 @@ WeightPlan weight_plan(const moe_product_shape* s)
     const double join = 2.5 * 4.0 * double(s->K) * double(s->N) / 5e6 / 0.016;
     double best = 0.0;
     w.shares.lanes = 1;
-    for (int lanes = 1; lanes <= slots && int64_t(lanes) * 256 <= std::max<int64_t>(s->M, 256); ++lanes) {
+    for (int lanes = 1; lanes <= slots && int64_t(lanes) * 256 <= all; ++lanes) {
         const double cost = double((tiles_ * lanes + slots - 1) / slots) * double(all) / lanes + (lanes - 1) * join;
         if (lanes == 1 || cost < best) { best = cost; w.shares.lanes = lanes; }
     }
