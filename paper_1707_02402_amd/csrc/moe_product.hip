@@ -192,6 +192,7 @@ using Mid = Kind<2, 2, 2, 2, 2, 2>;      // 128 x 128, two workgroups a CU
 using Few = Kind<1, 2, 4, 1, 3, 2>;      // 128 columns x 64 rows, two chunks ahead: a stream of weights
 
 constexpr int LIST = 256;                // tiles that a staying workgroup looks up at once
+constexpr int SORTED = 8192;             // groups whose counts fit where chunks go
 template <int DIR, class S> constexpr uint32_t BUF_BYTES = uint32_t((S::COLS / 64) * (DIR == FORWARD ? XUNIT : YUNIT) + (S::ROWS / 64) * (DIR == GRAD_WEIGHT ? YUNIT : XUNIT));
 template <int DIR, class S> constexpr uint32_t LDS_BYTES = BUF_BYTES<DIR, S> * S::BUFS + (DIR != GRAD_WEIGHT && S::BIG ? LIST * 16 + S::ROWS * 4 : 0);
 
@@ -254,8 +255,12 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
     const int per_die = int(gridDim.x) / 8, place = int(blockIdx.x) < per_die * 8 ? int(blockIdx.x & 7) * per_die + int(blockIdx.x >> 3) : int(blockIdx.x);
 
     // ---- the tiles
-    // forward, input's gradient: unit = piece of rows * ct + column; a workgroup that stays takes every gridDim.x-th unit, by the list
-    const int count = DIR == GRAD_WEIGHT ? 0 : STAYS ? (units - place + int(gridDim.x) - 1) / int(gridDim.x) : 1;
+    // forward, input's gradient: unit = piece of rows * ct + column; a workgroup that stays takes every gridDim.x-th unit, by the list.
+    // Up to SORTED groups and LIST units a workgroup, the units are the pieces that there are, those of more than half of a tile's rows first: rests of up to
+    // 128 rows, which take half as long, even out what is left over (65536 rows, 64 experts by Zipf's law, 8 columns of tiles: 8.6 tiles' time a workgroup on average,
+    // 10 for the longest without, 9.1 so).  Beyond, find_piece's units.
+    int count = DIR == GRAD_WEIGHT ? 0 : STAYS ? (units - place + int(gridDim.x) - 1) / int(gridDim.x) : 1;
+    const bool sorted = DIR != GRAD_WEIGHT && STAYS && p.g.E < SORTED && count <= LIST;
     int at_unit = -1;
     // weights' gradient: a lane's groups
     const int w_lane = place / (ct * rt);
@@ -265,13 +270,74 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
     auto tile_of = [&](const Piece& at, int col) {
         return Tile{at.e, at.begin, at.rows, col * S::COLS, 0, at.e < p.g.E ? (DIR == FORWARD ? p.K : p.N) : 0, -1};
     };
+    auto put_unit = [&](int i, const Piece& at, int col) {
+        *reinterpret_cast<u32x4*>(lds_raw + BUF * S::BUFS + i * 16) = u32x4{uint32_t(at.e), uint32_t(at.begin), uint32_t(at.rows), uint32_t(col)};
+    };
     auto list_units = [&](int from) {
         meet();
         if (tid < LIST && from + tid < count) {
-            const int unit = place + (from + tid) * int(gridDim.x);
-            const Place w = walk<4>(unit, units / ct, ct);
-            const Piece at = find_piece_alone(p.g, S::ROWS, w.row);
-            *reinterpret_cast<u32x4*>(lds_raw + BUF * S::BUFS + tid * 16) = u32x4{uint32_t(at.e), uint32_t(at.begin), uint32_t(at.rows), uint32_t(w.col)};
+            const Place w = walk<4>(place + (from + tid) * int(gridDim.x), units / ct, ct);
+            put_unit(tid, find_piece_alone(p.g, S::ROWS, w.row), w.col);
+        }
+        meet();
+    };
+    auto list_sorted = [&]() {
+        // how many large and small pieces there are ahead of every group, where the first chunks will be; what lies behind the groups counts as small
+        int2* const ahead = reinterpret_cast<int2*>(lds_raw);
+        int* const sums = reinterpret_cast<int*>(lds_raw + BUF * S::BUFS);
+        auto pieces = [&](int e) {
+            const int n = max(p.g.begin(e + 1) - p.g.begin(e), 0), rest = n % S::ROWS;
+            return e == p.g.E ? int2{0, (n + S::ROWS - 1) / S::ROWS} : int2{n / S::ROWS + (rest > S::ROWS / 2), rest > 0 && rest <= S::ROWS / 2};
+        };
+        const int per = (p.g.E + S::THREADS) / S::THREADS, e0 = min(tid * per, p.g.E + 1), e1 = min(e0 + per, p.g.E + 1);
+        int2 mine = {0, 0};
+        for (int e = e0; e < e1; ++e) {
+            const int2 n = pieces(e);
+            mine.x += n.x;
+            mine.y += n.y;
+        }
+        int2 at = mine;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int x = __shfl_up(at.x, o), y = __shfl_up(at.y, o);
+            at.x += lane >= o ? x : 0;
+            at.y += lane >= o ? y : 0;
+        }
+        if (lane == 63) { sums[wave * 2] = at.x; sums[wave * 2 + 1] = at.y; }
+        meet();
+        int2 all = {0, 0};
+        at.x -= mine.x;
+        at.y -= mine.y;
+#pragma unroll
+        for (int w = 0; w < S::WAVES; ++w) {
+            at.x += w < wave ? sums[w * 2] : 0;
+            at.y += w < wave ? sums[w * 2 + 1] : 0;
+            all.x += sums[w * 2];
+            all.y += sums[w * 2 + 1];
+        }
+        for (int e = e0; e < e1; ++e) {
+            ahead[e] = at;
+            const int2 n = pieces(e);
+            at.x += n.x;
+            at.y += n.y;
+        }
+        meet();
+        count = min(((all.x + all.y) * ct - place + int(gridDim.x) - 1) / int(gridDim.x), LIST);
+        if (tid < count) {
+            const int unit = place + tid * int(gridDim.x);
+            const bool large = unit < all.x * ct;
+            const Place w = walk<4>(large ? unit : unit - all.x * ct, large ? all.x : all.y, ct);
+            int lo = 0, n = p.g.E + 1;                         // the last group with no more pieces ahead of it than w.row (those without pieces stand ahead of it)
+            while (n > 1) {
+                const int half = n >> 1;
+                const int2 v = ahead[lo + half];
+                if ((large ? v.x : v.y) <= w.row) { lo += half; n -= half; }
+                else n = half;
+            }
+            const int a = p.g.begin(lo), rows = max(p.g.begin(lo + 1) - a, 0);
+            const int part = large ? w.row - ahead[lo].x : lo == p.g.E ? w.row - ahead[lo].y : rows / S::ROWS;
+            const bool there = part >= 0 && part <= (rows - 1) / S::ROWS && rows > 0;    // (else the offsets fall)
+            put_unit(tid, there ? Piece{lo, a + part * S::ROWS, min(S::ROWS, rows - part * S::ROWS)} : Piece{lo, a, 0}, w.col);
         }
         meet();
     };
@@ -292,7 +358,7 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
             }
         } else if constexpr (STAYS) {
             while (++at_unit < count) {
-                if (at_unit % LIST == 0) list_units(at_unit);
+                if (!sorted && at_unit % LIST == 0) list_units(at_unit);
                 const u32x4 v = *reinterpret_cast<const u32x4*>(lds_raw + BUF * S::BUFS + at_unit % LIST * 16);
                 Piece at;
                 at.e = __builtin_amdgcn_readfirstlane(v.x);
@@ -309,7 +375,7 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
     if constexpr (DIR == GRAD_WEIGHT) {
         if (w_lane >= shares.lanes) return;
         w_e = group_at(p.g, shares, w_from);
-    }
+    } else if (sorted) list_sorted();
 
     // ---- copying: wave w's blocks are w, w + WAVES ..; a request is a scalar base, which moves on with the chunks, and a lane's offset, which a tile keeps
     // (but for gathered rows as places of the sum).  Behind the end of a sum the last place that there is is copied again, and cleared in LDS before use.
@@ -664,24 +730,45 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
 }
 
 // Gradients whose sum a border between two lanes cuts: their parts, in order.  A workgroup looks after a share of the elements for one border, and only for the
-// first one inside a group.
+// first one inside a group.  Few parts: a wave adds up all parts of 256 elements; many (one crowded expert, small matrices): a quarter of the parts each, or the
+// loads' chain is what it takes (65536 rows, 256 x 256: 128 parts, 59 us a pass with a wave for all parts, 40 so).
+constexpr int JOIN_FEW = 8;
 template <typename TO>
 __global__ __launch_bounds__(256) void k_join(Groups g, Shares s, const float* __restrict__ partial, TO* __restrict__ out, int64_t elements, int per_border)
 {
-    const int border = int(blockIdx.x) / per_border + 1;
+    __shared__ f32x4 room[3][64];
+    const int border = int(blockIdx.x) / per_border + 1, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t x = s.each * border;
     const int e = group_at(g, s, x), n = max(g.begin(e + 1) - g.begin(e), 0);
     const int64_t first = start_of(g, s, e) + s.extra;
     if (x <= first || x >= first + n || x - s.each > first) return;
     int last = border;
     while (last + 1 < s.lanes && s.each * (last + 1) < first + n) ++last;
-    for (int64_t i = (int64_t(blockIdx.x) % per_border * 256 + threadIdx.x) * 4; i < elements; i += int64_t(per_border) * 1024) {
-        f32x4 v = *reinterpret_cast<const f32x4*>(partial + (2 * border - 1) * elements + i);
-#pragma unroll 4
-        for (int j = border; j <= last; ++j) v += *reinterpret_cast<const f32x4*>(partial + 2 * int64_t(j) * elements + i);
+    const int parts = last - border + 2;                       // slot 2 * border - 1, then 2 * border, 2 * border + 2 ..
+    auto sum = [&](int64_t i, int from, int to) {
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+        for (int j = from; j < to; ++j) v += *reinterpret_cast<const f32x4*>(partial + int64_t(j == 0 ? 2 * border - 1 : 2 * (border + j - 1)) * elements + i);
+        return v;
+    };
+    auto put = [&](int64_t i, const f32x4& v) {
         TO* const to = out + int64_t(e) * elements + i;
         if constexpr (std::is_same_v<TO, float>) *reinterpret_cast<f32x4*>(to) = v;
         else *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+    };
+    const int64_t share = int64_t(blockIdx.x) % per_border;
+    if (parts <= JOIN_FEW) {
+        for (int64_t i = (share * 256 + threadIdx.x) * 4; i < elements; i += int64_t(per_border) * 1024) put(i, sum(i, 0, parts));
+        return;
+    }
+    for (int64_t i0 = share * 256; i0 < elements; i0 += int64_t(per_border) * 256) {
+        const int64_t i = i0 + lane * 4;
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+        if (i < elements) v = sum(i, parts * wave / 4, parts * (wave + 1) / 4);
+        if (wave > 0) room[wave - 1][lane] = v;
+        __syncthreads();
+        if (wave == 0 && i < elements) put(i, ((v + room[0][lane]) + room[1][lane]) + room[2][lane]);
+        __syncthreads();
     }
 }
 
@@ -721,12 +808,30 @@ bool on_16(std::initializer_list<const void*> pointers)
     return true;
 }
 
-// us of a pass by kind:
+// Few: rows that leave most of a larger tile empty, or too few tiles of 128 x 128 for the chip.  Big: where its tiles are many and long enough.  us, forward / the
+// input's gradient, by rows, K, N, experts, Zipf exponent:
+//                                   Big          Mid          Few
+//   74 x 512 x 1024, 256, 1.1       18 / 24      18 / 16      13 / 13
+//   1000 x 1024 x 1024, 8, 0.5      27 / 27      14 / 14      11 / 10
+//   3000 x 2048 x 2048, 1           47 / 45      29 / 29      34 / 36
+//   4096 x 2048 x 1024, 16, 0.6     49 / 35      28 / 31      35 / 34
+//   8192 x 512 x 1024, 256, 1.1     81 / 88      56 / 57      52 / 53
+//   8192 x 512 x 1024, 64, 0.8      35 / 32      21 / 18      22 / 22
+//   16384 x 512 x 1024, 256, 0.8    88 / 94      66 / 65      62 / 62
+//   16384 x 1024 x 2048, 64, 0.8   122 / 116    116 / 113    133 / 126
+//   16384 x 2048 x 2048, 16, 0.6   144 / 142    143 / 142    192 / 206
+//   32768 x 1024 x 2048, 32, 0.6   153 / 157    192 / 176    226 / 198
+//   65536 x 512 x 1024, 64, 0.6     86 / 84      81 / 78     115 / 95
+//   65536 x 512 x 2048, 16, 0.6    165 / 158    220 / 179    263 / 203
+//   65536 x 1024 x 2048, 256, 0.6  421 / 390    434 / 411    506 / 484
+//   65536 x 1024 x 2048, 512, 0.6  606 / 579    562 / 554    614 / 627
+//   8192 x 8192 x 8192, 1          782 / 768   1319 / 1402  2367 / 2516
 enum KindOf { BIG, MID, FEW };
-KindOf kind_of(const moe_product_shape* s)
+KindOf kind_of(const moe_product_shape* s, int cols, int depth)
 {
-    const int64_t each = s->M / s->E;
-    return each >= 192 ? BIG : each >= 64 ? MID : FEW;
+    const int64_t each = s->M / s->E, chunks = (depth + 63) / 64;
+    if (each >= 192 && s->M / 256 * ((cols + 255) / 256) * chunks >= 12288) return BIG;
+    return each > 64 && (int64_t(s->M) + 127) / 128 * ((cols + 127) / 128) >= 256 ? MID : FEW;
 }
 
 template <int DIR, typename TO, class S, bool FUSED = false>
@@ -757,7 +862,7 @@ int launch_rows(const moe_product_shape* s, const Args& p, bool fast, hipStream_
         const auto run = p.relu || p.act ? launch_tiles<DIR, bf16_t, S, true> : launch_tiles<DIR, bf16_t, S, false>;
         return run(p, S::BIG ? std::min<int64_t>(units, CUS) : units, units, ct, 1, Shares{}, nullptr, st, who);
     };
-    if (fast) switch (kind_of(s)) {
+    if (fast) switch (kind_of(s, cols, DIR == FORWARD ? s->K : s->N)) {
         case BIG: return launch(Big{});
         case MID: return launch(Mid{});
         default: return launch(Few{});
@@ -780,7 +885,9 @@ struct WeightPlan {
 WeightPlan weight_plan(const moe_product_shape* s)
 {
     WeightPlan w = {};
-    w.big = s->K > 128 && s->N > 128;
+    // us, Big / Mid, by rows, K, N, experts: 65536 x 1024 x 2048, 64 421 / 480, 256 756 / 890; 65536 x 512 x 1024, 64 134 / 139; 65536 x 512 x 512, 64 92 / 60;
+    // 8192 x 4096 x 4096, 1 240 / 267; 3000 x 2048 x 2048, 1 52 / 44; 16384 x 512 x 1024, 256 160 / 157; 74 x 512 x 1024, 256 109 / 100
+    w.big = int64_t(s->M) / 64 * ((s->K + 255) / 256) * ((s->N + 255) / 256) >= 8192;
     const int side = w.big ? 256 : 128, slots = w.big ? CUS : 2 * CUS;
     w.ct = (s->K + side - 1) / side;
     w.rt = (s->N + side - 1) / side;
@@ -861,7 +968,7 @@ extern "C" int moe_product_grad_weight(const moe_product_shape* s, const moe_gro
             const int done = w.big ? launch_tiles<GRAD_WEIGHT, TO, Big>(p, grid, 0, w.ct, w.rt, w.shares, partial, st, "moe_product_grad_weight")
                                    : launch_tiles<GRAD_WEIGHT, TO, Mid>(p, grid, 0, w.ct, w.rt, w.shares, partial, st, "moe_product_grad_weight");
             if (done != DYNB_OK || w.shares.lanes == 1) return done;
-            const int per_border = int(std::min<int64_t>((elements + 4095) / 4096, 512));
+            const int per_border = int(std::min<int64_t>((elements + 255) / 256, std::max(64, 2048 / (w.shares.lanes - 1))));
             hipLaunchKernelGGL((k_join<TO>), dim3(unsigned((w.shares.lanes - 1) * per_border)), dim3(256), 0, st, p.g, w.shares, partial, static_cast<TO*>(dW), elements, per_border);
             return launched("moe_product_grad_weight");
         };
