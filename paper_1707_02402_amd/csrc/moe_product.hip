@@ -7,14 +7,17 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <atomic>
 #include <initializer_list>
+#include <mutex>
+#include <set>
 #include <string>
+#include <utility>
 #include <type_traits>
 
 #include "device_utils.h"
 #include "lds_copy.h"
 #include "plan_internal.h"
+#include "rows.h"
 
 using dynb::fail;
 
@@ -79,71 +82,6 @@ struct Args {
 };
 
 enum { FORWARD, GRAD_INPUT, GRAD_WEIGHT };
-
-// Any size, stride and address: tiles of 64 x 64 results, sums in pieces of 32 elements that are loaded one element at a time (the direction in memory
-// goes over the lanes) and multiplied by 32x32x16 MFMAs from LDS.
-constexpr int ANY = 64, ANY_C = 32, ANY_P = ANY_C + 8;
-
-template <int DIR, typename TO>
-__global__ __launch_bounds__(256) void k_product_any(Args p)
-{
-    __shared__ __attribute__((aligned(16))) bf16_t tile[2][ANY * ANY_P];
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, q = lane & 31, hk = lane >> 5;
-    const int cols = DIR == FORWARD ? p.N : p.K, ct = (cols + ANY - 1) / ANY, rt = DIR == GRAD_WEIGHT ? (p.N + ANY - 1) / ANY : 1;
-    const int c0 = int(blockIdx.x) % ct * ANY, r0 = int(blockIdx.x) / ct % rt * ANY, unit = int(blockIdx.x) / ct / rt;
-    const Piece at = find_piece(p.g, DIR == GRAD_WEIGHT ? 0x7fffffff : ANY, unit);
-    if (DIR == GRAD_WEIGHT ? at.e >= p.g.E : at.rows == 0) return;
-    const int rows = DIR == GRAD_WEIGHT ? p.N : at.rows;
-    const int depth = DIR == FORWARD ? p.K : DIR == GRAD_INPUT ? p.N : at.rows;
-    f32x16 acc;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) acc[i] = 0.f;
-    const size_t w = size_t(at.e) * size_t(p.N) * size_t(p.K);
-    // element (index i of the results' side, place z of the sum)
-    auto col_at = [&](int i, int z) -> bf16_t {
-        if (i >= cols || z >= depth) return 0;
-        if (DIR == FORWARD) return p.a[w + size_t(i) * p.K + z];
-        if (DIR == GRAD_INPUT) return p.a[w + size_t(z) * p.K + i];
-        return p.a[p.g.row(at.begin + z) * p.a_stride + i];
-    };
-    auto row_at = [&](int i, int z) -> bf16_t {
-        if (i >= rows || z >= depth) return 0;
-        if (DIR == FORWARD) return p.b[p.g.row(at.begin + i) * p.b_stride + z];
-        if (DIR == GRAD_INPUT) return p.b[int64_t(at.begin + i) * p.b_stride + z];
-        return p.b[int64_t(at.begin + z) * p.b_stride + i];
-    };
-    if (at.e < p.g.E)
-        for (int z0 = 0; z0 < depth; z0 += ANY_C) {
-            __syncthreads();
-#pragma unroll
-            for (int j = 0; j < ANY * ANY_C / 256; ++j) {
-                const int v = tid + j * 256, along_i = v % ANY, along_z = v / ANY, z = v % ANY_C, i = v / ANY_C;
-                if (DIR == FORWARD) tile[0][i * ANY_P + z] = col_at(c0 + i, z0 + z);
-                else tile[0][along_i * ANY_P + along_z] = col_at(c0 + along_i, z0 + along_z);
-                if (DIR == GRAD_WEIGHT) tile[1][along_i * ANY_P + along_z] = row_at(r0 + along_i, z0 + along_z);
-                else tile[1][i * ANY_P + z] = row_at(r0 + i, z0 + z);
-            }
-            __syncthreads();
-#pragma unroll
-            for (int ks = 0; ks < ANY_C; ks += 16) {
-                const bf16x8 a = *reinterpret_cast<const bf16x8*>(&tile[0][((wave & 1) * 32 + q) * ANY_P + ks + 8 * hk]);
-                const bf16x8 b = *reinterpret_cast<const bf16x8*>(&tile[1][((wave >> 1) * 32 + q) * ANY_P + ks + 8 * hk]);
-                acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, acc, 0, 0, 0);
-            }
-        }
-    const int r = r0 + (wave >> 1) * 32 + q;
-    if (r >= rows) return;
-    TO* const to = static_cast<TO*>(p.out) + (DIR == GRAD_WEIGHT ? int64_t(w) + int64_t(r) * p.K : int64_t(at.begin + r) * p.out_stride);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const int c = c0 + (wave & 1) * 32 + (i >> 2) * 8 + hk * 4 + (i & 3);
-        if (c >= cols) continue;
-        float v = acc[i];
-        if (DIR == FORWARD && p.relu) v = v < 0.f ? 0.f : v;   // (a NaN stays one)
-        if (DIR == GRAD_INPUT && p.act && !(bf16_to_f32(p.act[int64_t(at.begin + r) * p.act_stride + c]) > 0.f)) v = 0.f;
-        store_f32(to + c, v);
-    }
-}
 
 // ------------------------------------------------------------------------------------------ K and N multiples of 8, rows on 16-byte borders
 // Tiles of results whose operands go straight from memory into LDS, a chunk of 64 places of the sum at a time and at least one chunk ahead, and
@@ -568,7 +506,7 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
                 };
                 // the products of K-step ks (-1: the chunk before's last); in the first half of them K-step ks + 1 is read, and with the first ones requests are made
                 auto step = [&](int ks, int asks_before, int asks_behind) {
-                    constexpr int PRODUCTS = FA * LIVE, FRAGMENTS = FA + LIVE;
+                    constexpr int PRODUCTS = FA * (LIVE > 0 ? LIVE : 1), FRAGMENTS = FA + LIVE;
 #pragma unroll
                     for (int m = 0; m < PRODUCTS; ++m) {
                         const int a = m % FA, b = m / FA;
@@ -729,6 +667,147 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
     answered_but<0>();                                         // (nothing is on its way to LDS that another workgroup may have next)
 }
 
+// ------------------------------------------------------------------------------------------ any size, stride and address
+// Mid's tiles and its places in LDS, by way of registers: pieces of 16 bytes are loaded from wherever they lie (rows of odd length lie between the borders that a copy
+// straight into LDS keeps to), the last of a row element by element, a chunk ahead.
+template <int DIR, typename TO>
+__global__ __launch_bounds__(256, 2) void k_product_any(Args p, int units, int ct, int rt, Shares shares, float* __restrict__ partial)
+{
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
+    using S = Mid;
+    constexpr bool A_ACROSS = DIR != FORWARD, B_ACROSS = DIR == GRAD_WEIGHT;
+    constexpr int U = 2, EACH = 2, UA = A_ACROSS ? YUNIT : XUNIT, UB = B_ACROSS ? YUNIT : XUNIT;
+    constexpr uint32_t BUF = BUF_BYTES<DIR, S>;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, q = lane & 31, hk = lane >> 5, cg = wave % 2, rg = wave / 2;
+    const int cols = DIR == FORWARD ? p.N : p.K;
+    const lds_ptr lds = (lds_ptr)lds_raw;
+    using lds_u32x4 = __attribute__((address_space(3))) u32x4;
+
+    u32x4 a_piece[U][EACH], b_piece[U][EACH];
+    auto load = [&](const Tile& t, int z0) {
+        const u32x4 none = {0u, 0u, 0u, 0u};
+        const size_t w = size_t(t.e) * size_t(p.N) * size_t(p.K);
+#pragma unroll
+        for (int j = 0; j < EACH; ++j) {
+            const int block = wave + j * S::WAVES, s_q = copied_row(block, lane), z = z0 + copied_place(block, lane), along = z0 + (lane & 7) * 8, rest = t.depth - along;
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const int a_col = t.c0 + i * 64 + (lane & 7) * 8, row = i * 64 + (lane >> 5) * 32 + s_q;
+                if constexpr (DIR == FORWARD) {                // (the features in the order that gives a lane 16 neighbours)
+                    const int feature = t.c0 + i * 64 + (lane >> 5) * 32 + (s_q >> 2 & 1) * 16 + (s_q >> 3) * 4 + (s_q & 3);
+                    a_piece[i][j] = feature < cols && rest > 0 ? load_piece(p.a + w + size_t(feature) * size_t(p.K) + along, rest) : none;
+                    b_piece[i][j] = row < t.rows && rest > 0 ? load_piece(p.b + p.g.row(t.begin + row) * p.b_stride + along, rest) : none;
+                } else if constexpr (DIR == GRAD_INPUT) {
+                    a_piece[i][j] = z < t.depth && a_col < cols ? load_piece(p.a + w + size_t(z) * size_t(p.K) + a_col, cols - a_col) : none;
+                    b_piece[i][j] = row < t.rows && rest > 0 ? load_piece(p.b + int64_t(t.begin + row) * p.b_stride + along, rest) : none;
+                } else {
+                    const int b_col = t.r0 + i * 64 + (lane & 7) * 8;
+                    a_piece[i][j] = z < t.depth && a_col < cols ? load_piece(p.a + p.g.row(t.begin + z) * p.a_stride + a_col, cols - a_col) : none;
+                    b_piece[i][j] = z < t.depth && b_col < p.N ? load_piece(p.b + int64_t(t.begin + z) * p.b_stride + b_col, p.N - b_col) : none;
+                }
+            }
+        }
+    };
+    auto write = [&](lds_ptr to) {
+#pragma unroll
+        for (int j = 0; j < EACH; ++j)
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const int block = wave + j * S::WAVES;
+                *(lds_u32x4*)(to + uint32_t(i * UA + block * (A_ACROSS ? YBLOCK : XBLOCK) + lane * 16)) = a_piece[i][j];
+                *(lds_u32x4*)(to + uint32_t(U * UA + i * UB + block * (B_ACROSS ? YBLOCK : XBLOCK) + lane * 16)) = b_piece[i][j];
+            }
+    };
+    const uint32_t a_slot = uint32_t(cg * UA) + (A_ACROSS ? places_at(lane, false) : fragment_at(q, hk));
+    const uint32_t b_slot = uint32_t(U * UA) + uint32_t(rg * (B_ACROSS ? 64 : 512)) + (B_ACROSS ? places_at(lane, true) : fragment_at(q, hk));
+
+    auto work = [&](const Tile& t) {
+        f32x16 acc[2][2];
+#pragma unroll
+        for (int i = 0; i < 64; ++i) acc[i >> 5][i >> 4 & 1][i & 15] = 0.f;
+        if (t.depth > 0) load(t, 0);
+        uint32_t at = 0;
+        for (int z0 = 0; z0 < t.depth; z0 += 64) {
+            write(lds + at);
+            __syncthreads();                                   // (who is still at the other place's chunk has not written this one's successor)
+            if (z0 + 64 < t.depth) load(t, z0 + 64);
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) {
+                bf16x8 af[2], bf[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    // (rows: block i of this wave is the i-th unit's fragment rg)
+                    if constexpr (A_ACROSS) af[i] = read_across(lds + at + a_slot + uint32_t(i * 64 + ks * 2 * YBLOCK));
+                    else af[i] = read_along(lds + at + a_slot + uint32_t(i * 512 + ks * 32));
+                    if constexpr (B_ACROSS) bf[i] = read_across(lds + at + b_slot + uint32_t(i * UB + ks * 2 * YBLOCK));
+                    else bf[i] = read_along(lds + at + b_slot + uint32_t(i * UB + ks * 32));
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[i & 1][i >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(af[i & 1], bf[i >> 1], acc[i & 1][i >> 1], 0, 0, 0);
+            }
+            at = BUF - at;
+        }
+        __syncthreads();
+        const lds_ptr mine_at = lds + uint32_t(wave) * (2 * BUF / S::WAVES / 16 * 16);
+        auto put = [&](auto* to, int64_t pitch) {
+            using T = std::remove_pointer_t<decltype(to)>;
+            constexpr int P = PIECE<T>, LANES = 64 / P, AT_ONCE = 64 / LANES, PITCH = 64 * int(sizeof(T)) + 16;
+            static_assert(32 * PITCH <= int(2 * BUF / S::WAVES), "room");
+            const int col = lane % LANES * P, row = lane / LANES, first = t.c0 + cg * 64, left = cols - first - col;
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                    float v = acc[i >> 4][b][i & 15];
+                    if (DIR == FORWARD && p.relu) v = v < 0.f ? 0.f : v;                                     // (a NaN stays one)
+                    const lds_ptr here = mine_at + uint32_t(q * PITCH + ((i >> 4) * 32 + 16 * hk + (i & 15)) * int(sizeof(T)));
+                    if constexpr (sizeof(T) == 4) *(__attribute__((address_space(3))) float*)here = v;
+                    else *(__attribute__((address_space(3))) bf16_t*)here = f32_to_bf16(v);
+                }
+                wave_sync();
+                for (int i = 0; i < 32; i += AT_ONCE) {
+                    const int r = (b * 2 + rg) * 32 + row + i;
+                    if (r >= t.rows || left <= 0) continue;
+                    const u32x4 v = *(const lds_u32x4*)(mine_at + uint32_t((row + i) * PITCH + col * int(sizeof(T))));
+                    u32x4 act;
+                    const bool masked = DIR == GRAD_INPUT && p.act;
+                    if (masked) act = load_piece(p.act + int64_t(t.begin + r) * p.act_stride + first + col, left);
+                    float w[P];
+#pragma unroll
+                    for (int j = 0; j < P; ++j) {
+                        w[j] = element<T>(v, j);
+                        if (masked && !(element<bf16_t>(act, j) > 0.f)) w[j] = 0.f;
+                    }
+                    store_piece<P>(to + int64_t(r) * pitch + first + col, left, w);
+                }
+                wave_sync();
+            }
+        };
+        if constexpr (DIR == GRAD_WEIGHT) {
+            const size_t all = size_t(p.N) * size_t(p.K), row = size_t(t.r0) * size_t(p.K);
+            if (t.slot >= 0) put(partial + size_t(t.slot) * all + row, p.K);
+            else put(static_cast<TO*>(p.out) + size_t(t.e) * all + row, p.K);
+        } else put(static_cast<TO*>(p.out) + int64_t(t.begin) * p.out_stride, p.out_stride);
+        __syncthreads();
+    };
+    if constexpr (DIR == GRAD_WEIGHT) {
+        const int w_lane = int(blockIdx.x) / (ct * rt);
+        const Place at = walk<4>(int(blockIdx.x) % (ct * rt), rt, ct);
+        const int64_t from = shares.each * w_lane, to = from + shares.each;
+        for (int e = group_at(p.g, shares, from); e < p.g.E && start_of(p.g, shares, e) < to; ++e) {
+            const int a = p.g.begin(e), n = max(p.g.begin(e + 1) - a, 0);
+            const int64_t s = start_of(p.g, shares, e), first = s + shares.extra;
+            const int lo = int(min(max(from - first, int64_t(0)), int64_t(n))), hi = int(min(max(to - first, int64_t(0)), int64_t(n)));
+            if (n == 0 ? s < from : hi <= lo) continue;
+            work(Tile{e, a + lo, min(p.N - at.row * S::ROWS, S::ROWS), at.col * S::COLS, at.row * S::ROWS, hi - lo, hi - lo == n ? -1 : 2 * w_lane + (lo > 0 ? 0 : 1)});
+        }
+    } else {
+        const Place w = walk<1>(int(blockIdx.x), units / ct, ct);
+        const Piece at = find_piece(p.g, S::ROWS, w.row);
+        if (at.rows > 0) work(Tile{at.e, at.begin, at.rows, w.col * S::COLS, 0, at.e < p.g.E ? (DIR == FORWARD ? p.K : p.N) : 0, -1});
+    }
+}
+
 // Gradients whose sum a border between two lanes cuts: their parts, in order.  A workgroup looks after a share of the elements for one border, and only for the
 // first one inside a group.  Few parts: a wave adds up all parts of 256 elements; many (one crowded expert, small matrices): a quarter of the parts each, or the
 // loads' chain is what it takes (65536 rows, 256 x 256: 128 parts, 59 us a pass with a wave for all parts, 40 so).
@@ -748,13 +827,12 @@ __global__ __launch_bounds__(256) void k_join(Groups g, Shares s, const float* _
     auto sum = [&](int64_t i, int from, int to) {
         f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
-        for (int j = from; j < to; ++j) v += *reinterpret_cast<const f32x4*>(partial + int64_t(j == 0 ? 2 * border - 1 : 2 * (border + j - 1)) * elements + i);
+        for (int j = from; j < to; ++j) v += __builtin_bit_cast(f32x4, load_piece(partial + int64_t(j == 0 ? 2 * border - 1 : 2 * (border + j - 1)) * elements + i, int(min(elements - i, int64_t(4)))));
         return v;
     };
     auto put = [&](int64_t i, const f32x4& v) {
-        TO* const to = out + int64_t(e) * elements + i;
-        if constexpr (std::is_same_v<TO, float>) *reinterpret_cast<f32x4*>(to) = v;
-        else *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+        const float w[4] = {v[0], v[1], v[2], v[3]};
+        store_piece<4>(out + int64_t(e) * elements + i, int(min(elements - i, int64_t(4))), w);
     };
     const int64_t share = int64_t(blockIdx.x) % per_border;
     if (parts <= JOIN_FEW) {
@@ -789,7 +867,6 @@ int check_groups(const moe_product_shape* s, const moe_groups* g, bool gathers, 
     if ((reinterpret_cast<uintptr_t>(g->offsets) | reinterpret_cast<uintptr_t>(g->perm)) & 3) return fail(DYNB_E_INVAL, who + ": misaligned pointer");
     return DYNB_OK;
 }
-int64_t tiles(int n) { return (int64_t(n) + ANY - 1) / ANY; }
 constexpr int CUS = 256;
 constexpr int64_t MOST_GROUPS = (1 << 24) - 1;                 // workgroups of 256 threads in a launch
 bool odd(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 1) != 0; }
@@ -834,18 +911,24 @@ KindOf kind_of(const moe_product_shape* s, int cols, int depth)
     return each > 64 && (int64_t(s->M) + 127) / 128 * ((cols + 127) / 128) >= 256 ? MID : FEW;
 }
 
-template <int DIR, typename TO, class S, bool FUSED = false>
-int launch_tiles(const Args& p, int64_t grid, int64_t units, int ct, int rt, const Shares& shares, float* partial, hipStream_t st, const char* who)
+using Kernel = void (*)(Args, int, int, int, Shares, float*);
+template <int DIR, class S>
+int launch_kernel(Kernel kernel, const Args& p, int64_t grid, int64_t units, int ct, int rt, const Shares& shares, float* partial, hipStream_t st, const char* who)
 {
-    static std::atomic<uint64_t> attr_set{0};                 // one bit per device: LDS beyond 64 KB
-    int dev = 0;
-    hipError_t e = hipGetDevice(&dev);
-    if (e == hipSuccess && !(attr_set.load() >> (dev & 63) & 1)) {
-        e = hipFuncSetAttribute(reinterpret_cast<const void*>(k_product<DIR, TO, S, FUSED>), hipFuncAttributeMaxDynamicSharedMemorySize, int(LDS_BYTES<DIR, S>));
-        if (e == hipSuccess) attr_set.fetch_or(uint64_t(1) << (dev & 63));
+    // LDS beyond 64 KB has to be asked for; a kernel is asked for once on every device
+    static std::mutex lock;
+    static std::set<std::pair<int, Kernel>> asked;
+    {
+        int dev = 0;
+        hipError_t e = hipGetDevice(&dev);
+        std::lock_guard<std::mutex> guard(lock);
+        if (e == hipSuccess && !asked.count({dev, kernel})) {
+            e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, int(LDS_BYTES<DIR, S>));
+            if (e == hipSuccess) asked.insert({dev, kernel});
+        }
+        if (e != hipSuccess) return fail(DYNB_E_HIP, std::string(who) + ": " + hipGetErrorString(e));
     }
-    if (e != hipSuccess) return fail(DYNB_E_HIP, std::string(who) + ": " + hipGetErrorString(e));
-    hipLaunchKernelGGL((k_product<DIR, TO, S, FUSED>), dim3(unsigned(grid)), dim3(S::THREADS), (LDS_BYTES<DIR, S>), st, p, int(units), ct, rt, shares, partial);
+    hipLaunchKernelGGL(kernel, dim3(unsigned(grid)), dim3(S::THREADS), (LDS_BYTES<DIR, S>), st, p, int(units), ct, rt, shares, partial);
     return launched(who);
 }
 
@@ -859,18 +942,18 @@ int launch_rows(const moe_product_shape* s, const Args& p, bool fast, hipStream_
         const int ct = (cols + S::COLS - 1) / S::COLS;
         const int64_t units = (int64_t(s->M) / S::ROWS + s->E + 1) * ct;
         if (units > MOST_GROUPS) return fail(DYNB_E_UNSUPPORTED, std::string(who) + ": too many results");
-        const auto run = p.relu || p.act ? launch_tiles<DIR, bf16_t, S, true> : launch_tiles<DIR, bf16_t, S, false>;
-        return run(p, S::BIG ? std::min<int64_t>(units, CUS) : units, units, ct, 1, Shares{}, nullptr, st, who);
+        return launch_kernel<DIR, S>(p.relu || p.act ? k_product<DIR, bf16_t, S, true> : k_product<DIR, bf16_t, S, false>, p, S::BIG ? std::min<int64_t>(units, CUS) : units, units, ct, 1,
+                                     Shares{}, nullptr, st, who);
     };
     if (fast) switch (kind_of(s, cols, DIR == FORWARD ? s->K : s->N)) {
         case BIG: return launch(Big{});
         case MID: return launch(Mid{});
         default: return launch(Few{});
         }
-    const int64_t grid = tiles(cols) * (s->M / ANY + s->E + 1);
-    if (grid > MOST_GROUPS) return fail(DYNB_E_UNSUPPORTED, std::string(who) + ": too many results");
-    hipLaunchKernelGGL((k_product_any<DIR, bf16_t>), dim3(unsigned(grid)), dim3(256), 0, st, p);
-    return launched(who);
+    const int ct = (cols + Mid::COLS - 1) / Mid::COLS;
+    const int64_t units = (int64_t(s->M) / Mid::ROWS + s->E + 1) * ct;
+    if (units > MOST_GROUPS) return fail(DYNB_E_UNSUPPORTED, std::string(who) + ": too many results");
+    return launch_kernel<DIR, Mid>(k_product_any<DIR, bf16_t>, p, units, units, ct, 1, Shares{}, nullptr, st, who);
 }
 
 // How the weights' gradient runs: the kind of tile, and as many lanes as give the least work to the workgroup that has the most, with what adding up
@@ -882,12 +965,12 @@ struct WeightPlan {
     Shares shares;
     size_t bytes;                                              // of partial sums
 };
-WeightPlan weight_plan(const moe_product_shape* s)
+WeightPlan weight_plan(const moe_product_shape* s, bool fast)
 {
     WeightPlan w = {};
     // us, Big / Mid, by rows, K, N, experts: 65536 x 1024 x 2048, 64 421 / 480, 256 756 / 890; 65536 x 512 x 1024, 64 134 / 139; 65536 x 512 x 512, 64 92 / 60;
     // 8192 x 4096 x 4096, 1 240 / 267; 3000 x 2048 x 2048, 1 52 / 44; 16384 x 512 x 1024, 256 160 / 157; 74 x 512 x 1024, 256 109 / 100
-    w.big = int64_t(s->M) / 64 * ((s->K + 255) / 256) * ((s->N + 255) / 256) >= 8192;
+    w.big = fast && int64_t(s->M) / 64 * ((s->K + 255) / 256) * ((s->N + 255) / 256) >= 8192;
     const int side = w.big ? 256 : 128, slots = w.big ? CUS : 2 * CUS;
     w.ct = (s->K + side - 1) / side;
     w.rt = (s->N + side - 1) / side;
@@ -941,7 +1024,8 @@ extern "C" int moe_product_grad_input(const moe_product_shape* s, const moe_grou
 extern "C" size_t moe_product_grad_weight_workspace_bytes(const moe_product_shape* s)
 {
     if (check(s, "moe_product_grad_weight_workspace_bytes") != DYNB_OK) return 0;
-    return std::max<size_t>(weight_plan(s).bytes, 256);
+    // (which of the two runs depends on addresses, too)
+    return std::max<size_t>({weight_plan(s, true).bytes, weight_plan(s, false).bytes, 256});
 }
 
 extern "C" int moe_product_grad_weight(const moe_product_shape* s, const moe_groups* g, const void* dout, int64_t dout_stride, const void* in, int64_t in_stride, void* dW,
@@ -957,27 +1041,21 @@ extern "C" int moe_product_grad_weight(const moe_product_shape* s, const moe_gro
     if (workspace_bytes < moe_product_grad_weight_workspace_bytes(s)) return fail(DYNB_E_WORKSPACE, "moe_product_grad_weight: workspace too small");
     if (reinterpret_cast<uintptr_t>(workspace) & 255) return fail(DYNB_E_INVAL, "moe_product_grad_weight: workspace not 256-byte aligned");
     const Args p = {groups_of(s, g), static_cast<const bf16_t*>(in), static_cast<const bf16_t*>(dout), in_stride, dout_stride, nullptr, 0, dW, 0, s->K, s->N, 0};
-    if (s->K % 8 == 0 && s->N % 8 == 0 && dout_stride % 8 == 0 && in_stride % 8 == 0 && on_16({dout, in, dW})) {
-        const WeightPlan w = weight_plan(s);
-        hipStream_t st = static_cast<hipStream_t>(stream);
-        float* const partial = static_cast<float*>(workspace);
-        const int64_t grid = int64_t(w.ct) * w.rt * w.shares.lanes, elements = int64_t(s->K) * s->N;
-        if (grid > MOST_GROUPS / 2) return fail(DYNB_E_UNSUPPORTED, "moe_product_grad_weight: too many results");
-        auto launch = [&](auto to) {
-            using TO = decltype(to);
-            const int done = w.big ? launch_tiles<GRAD_WEIGHT, TO, Big>(p, grid, 0, w.ct, w.rt, w.shares, partial, st, "moe_product_grad_weight")
-                                   : launch_tiles<GRAD_WEIGHT, TO, Mid>(p, grid, 0, w.ct, w.rt, w.shares, partial, st, "moe_product_grad_weight");
-            if (done != DYNB_OK || w.shares.lanes == 1) return done;
-            const int per_border = int(std::min<int64_t>((elements + 255) / 256, std::max(64, 2048 / (w.shares.lanes - 1))));
-            hipLaunchKernelGGL((k_join<TO>), dim3(unsigned((w.shares.lanes - 1) * per_border)), dim3(256), 0, st, p.g, w.shares, partial, static_cast<TO*>(dW), elements, per_border);
-            return launched("moe_product_grad_weight");
-        };
-        return grad_dtype == DYNB_BF16 ? launch(bf16_t{}) : launch(float{});
-    }
-    const int64_t grid = tiles(s->K) * tiles(s->N) * s->E;
-    if (grid > MOST_GROUPS) return fail(DYNB_E_UNSUPPORTED, "moe_product_grad_weight: too many results");
+    const bool fast = s->K % 8 == 0 && s->N % 8 == 0 && dout_stride % 8 == 0 && in_stride % 8 == 0 && on_16({dout, in, dW});
+    const WeightPlan w = weight_plan(s, fast);
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (grad_dtype == DYNB_BF16) hipLaunchKernelGGL((k_product_any<GRAD_WEIGHT, bf16_t>), dim3(unsigned(grid)), dim3(256), 0, st, p);
-    else hipLaunchKernelGGL((k_product_any<GRAD_WEIGHT, float>), dim3(unsigned(grid)), dim3(256), 0, st, p);
-    return launched("moe_product_grad_weight");
+    float* const partial = static_cast<float*>(workspace);
+    const int64_t grid = int64_t(w.ct) * w.rt * w.shares.lanes, elements = int64_t(s->K) * s->N;
+    if (grid > MOST_GROUPS / 2) return fail(DYNB_E_UNSUPPORTED, "moe_product_grad_weight: too many results");
+    auto launch = [&](auto to) {
+        using TO = decltype(to);
+        const char* const who = "moe_product_grad_weight";
+        const int done = w.big ? launch_kernel<GRAD_WEIGHT, Big>(k_product<GRAD_WEIGHT, TO, Big, false>, p, grid, 0, w.ct, w.rt, w.shares, partial, st, who)
+                               : launch_kernel<GRAD_WEIGHT, Mid>(fast ? k_product<GRAD_WEIGHT, TO, Mid, false> : k_product_any<GRAD_WEIGHT, TO>, p, grid, 0, w.ct, w.rt, w.shares, partial, st, who);
+        if (done != DYNB_OK || w.shares.lanes == 1) return done;
+        const int per_border = int(std::min<int64_t>((elements + 255) / 256, std::max(64, 2048 / (w.shares.lanes - 1))));
+        hipLaunchKernelGGL((k_join<TO>), dim3(unsigned((w.shares.lanes - 1) * per_border)), dim3(256), 0, st, p.g, w.shares, partial, static_cast<TO*>(dW), elements, per_border);
+        return launched(who);
+    };
+    return grad_dtype == DYNB_BF16 ? launch(bf16_t{}) : launch(float{});
 }
