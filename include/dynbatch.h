@@ -491,7 +491,7 @@ typedef struct {
  *   in    [M or groups->rows][K] bf16     W [E][N][K] bf16, dense     out, dout [M][N] bf16
  *   act, din [M][K] bf16                  dW [E][N][K] grad_dtype (DYNB_F32 or DYNB_BF16), dense
  * Results may not overlap with what is read.  Any sizes and addresses are accepted; K and N that are multiples of 8 with
- * rows on 16-byte borders run the fast kernels.  Nothing is read back and nothing waits on the host.  Sums are in a fixed order: equal calls
+ * rows on 16-byte borders, at most 2^22 elements apart and (gathered ones) within 4 GB, are copied straight into LDS, others by way of registers.  Nothing is read back and nothing waits on the host.  Sums are in a fixed order: equal calls
  * give equal bits.
  * Errors: DYNB_E_INVAL (NULL, sizes <= 0, strides below a row's length, misaligned), DYNB_E_UNSUPPORTED (dtype, flag, more
  * than 2^30 rows, 2^22 channels, 2^20 experts or 2^24 tiles of results), DYNB_E_WORKSPACE, DYNB_E_HIP.  */
@@ -517,8 +517,8 @@ typedef struct {
 } dynb_embed_shape;
 
 /*   tokens device [T]   table device [V][d] dtype, dense   out device [T][d] dtype, rows out_stride elements apart
- * Errors: DYNB_E_INVAL (NULL, sizes <= 0, out_stride < d, misaligned), DYNB_E_UNSUPPORTED (dtype, more than 2^25 tokens or 2^27
- * rows), DYNB_E_HIP.                                                                             */
+ * Errors: DYNB_E_INVAL (NULL, sizes <= 0, out_stride < d, misaligned), DYNB_E_UNSUPPORTED (dtype, more than 2^25 tokens, 2^27
+ * rows or 2^28 columns), DYNB_E_HIP.                                                             */
 int dynb_embed(const dynb_embed_shape* shape, const int32_t* tokens, const void* table, void* out, int64_t out_stride,
                void* stream);
 /*   dout device [T][d] dtype, rows dout_stride elements apart; dtable device [V][d] grad_dtype (DYNB_F32 or DYNB_BF16), dense: every
@@ -544,8 +544,8 @@ typedef struct {
  *   mean, rstd  device [T] fp32: what the backward pass wants (moments of x); dynb_layer_norm: may be NULL
  *   dx, dgamma, dbeta  may be NULL where they are not wanted; dgamma, dbeta device [d] fp32
  *   workspace   device, >= dynb_layer_norm_backward_workspace_bytes, 256-byte aligned, scratch
- * Errors: DYNB_E_INVAL (NULL, sizes <= 0, negative eps, strides below d, misaligned), DYNB_E_UNSUPPORTED (dtype),
- * DYNB_E_WORKSPACE, DYNB_E_HIP.                                                                  */
+ * Errors: DYNB_E_INVAL (NULL, sizes <= 0, negative eps, strides below d, misaligned), DYNB_E_UNSUPPORTED (dtype, more than 2^28
+ * columns), DYNB_E_WORKSPACE, DYNB_E_HIP.                                                        */
 int dynb_layer_norm(const dynb_norm_shape* shape, const void* x, int64_t x_stride, const float* gamma, const float* beta,
                     void* y, int64_t y_stride, float* mean, float* rstd, void* stream);
 size_t dynb_layer_norm_backward_workspace_bytes(const dynb_norm_shape* shape);
@@ -567,7 +567,7 @@ typedef struct {
 /*   tensors  host [n], read before the call returns
  *   norm     device, one float
  *   workspace device, >= dynb_clip_workspace_bytes, 256-byte aligned, scratch
- * Errors: DYNB_E_INVAL (NULL, negative sizes, max_norm not positive, misaligned), DYNB_E_UNSUPPORTED (dtype),
+ * Errors: DYNB_E_INVAL (NULL, negative sizes, max_norm not positive, misaligned), DYNB_E_UNSUPPORTED (dtype, more than 2^42 elements),
  * DYNB_E_WORKSPACE, DYNB_E_HIP.                                                                  */
 size_t dynb_clip_workspace_bytes(void);
 int dynb_clip_gradients(const dynb_grad_tensor* tensors, int32_t n, float max_norm, float* norm, void* workspace,

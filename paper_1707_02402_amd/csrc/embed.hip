@@ -475,7 +475,7 @@ int check(const dynb_embed_shape* s, const std::string& who)
     if (!s) return fail(DYNB_E_INVAL, who + ": NULL shape");
     if (s->T < 0 || s->V <= 0 || s->d <= 0) return fail(DYNB_E_INVAL, who + ": sizes must be positive");
     if (s->dtype != DYNB_F32 && s->dtype != DYNB_BF16) return fail(DYNB_E_UNSUPPORTED, who + ": unknown dtype");
-    if (s->T > 1 << 25 || s->V > 1 << 27) return fail(DYNB_E_UNSUPPORTED, who + ": more than 2^25 tokens or 2^27 rows");   // (a launch has room for 2^32 threads)
+    if (s->T > 1 << 25 || s->V > 1 << 27 || s->d > 1 << 28) return fail(DYNB_E_UNSUPPORTED, who + ": more than 2^25 tokens, 2^27 rows or 2^28 columns");   // (a launch has room for 2^32 threads)
     return DYNB_OK;
 }
 bool misaligned(const void* p, int dtype) { return (reinterpret_cast<uintptr_t>(p) & (dtype == DYNB_BF16 ? 1 : 3)) != 0; }

@@ -878,6 +878,11 @@ int launched(const char* who)
     return DYNB_OK;
 }
 
+// what k_product's 32-bit offsets reach: 255 rows from a tile's first, and gathered rows from the first of all
+bool reached(const moe_groups* g, int64_t in_stride, int64_t other_stride)
+{
+    return in_stride <= 1 << 22 && other_stride <= 1 << 22 && (!g->perm || int64_t(g->rows) * in_stride * 2 < int64_t(1) << 32);
+}
 bool on_16(std::initializer_list<const void*> pointers)
 {
     for (const void* p : pointers)
@@ -1002,7 +1007,7 @@ extern "C" int moe_product(const moe_product_shape* s, const moe_groups* g, cons
     if (in_stride < s->K || out_stride < s->N) return fail(DYNB_E_INVAL, "moe_product: rows overlap (stride below their length)");
     if (odd(in) || odd(W) || odd(out)) return fail(DYNB_E_INVAL, "moe_product: misaligned pointer");
     const Args p = {groups_of(s, g), static_cast<const bf16_t*>(W), static_cast<const bf16_t*>(in), 0, in_stride, nullptr, 0, out, out_stride, s->K, s->N, int(s->flags & MOE_PRODUCT_RELU)};
-    const bool fast = s->K % 8 == 0 && s->N % 8 == 0 && in_stride % 8 == 0 && out_stride % 8 == 0 && on_16({in, W, out});
+    const bool fast = s->K % 8 == 0 && s->N % 8 == 0 && in_stride % 8 == 0 && out_stride % 8 == 0 && on_16({in, W, out}) && reached(g, in_stride, 0);
     return launch_rows<FORWARD>(s, p, fast, static_cast<hipStream_t>(stream), "moe_product");
 }
 
@@ -1017,7 +1022,7 @@ extern "C" int moe_product_grad_input(const moe_product_shape* s, const moe_grou
     if (dout_stride < s->N || din_stride < s->K || (act && act_stride < s->K)) return fail(DYNB_E_INVAL, "moe_product_grad_input: rows overlap (stride below their length)");
     if (odd(dout) || odd(W) || odd(act) || odd(din)) return fail(DYNB_E_INVAL, "moe_product_grad_input: misaligned pointer");
     const Args p = {groups_of(s, g), static_cast<const bf16_t*>(W), static_cast<const bf16_t*>(dout), 0, dout_stride, static_cast<const bf16_t*>(act), act_stride, din, din_stride, s->K, s->N, 0};
-    const bool fast = s->K % 8 == 0 && s->N % 8 == 0 && dout_stride % 8 == 0 && act_stride % 8 == 0 && din_stride % 8 == 0 && on_16({dout, W, act, din});
+    const bool fast = s->K % 8 == 0 && s->N % 8 == 0 && dout_stride % 8 == 0 && act_stride % 8 == 0 && din_stride % 8 == 0 && on_16({dout, W, act, din}) && reached(g, 0, dout_stride);
     return launch_rows<GRAD_INPUT>(s, p, fast, static_cast<hipStream_t>(stream), "moe_product_grad_input");
 }
 
@@ -1041,7 +1046,7 @@ extern "C" int moe_product_grad_weight(const moe_product_shape* s, const moe_gro
     if (workspace_bytes < moe_product_grad_weight_workspace_bytes(s)) return fail(DYNB_E_WORKSPACE, "moe_product_grad_weight: workspace too small");
     if (reinterpret_cast<uintptr_t>(workspace) & 255) return fail(DYNB_E_INVAL, "moe_product_grad_weight: workspace not 256-byte aligned");
     const Args p = {groups_of(s, g), static_cast<const bf16_t*>(in), static_cast<const bf16_t*>(dout), in_stride, dout_stride, nullptr, 0, dW, 0, s->K, s->N, 0};
-    const bool fast = s->K % 8 == 0 && s->N % 8 == 0 && dout_stride % 8 == 0 && in_stride % 8 == 0 && on_16({dout, in, dW});
+    const bool fast = s->K % 8 == 0 && s->N % 8 == 0 && dout_stride % 8 == 0 && in_stride % 8 == 0 && on_16({dout, in, dW}) && reached(g, in_stride, dout_stride);
     const WeightPlan w = weight_plan(s, fast);
     hipStream_t st = static_cast<hipStream_t>(stream);
     float* const partial = static_cast<float*>(workspace);

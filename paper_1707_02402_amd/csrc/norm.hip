@@ -303,6 +303,7 @@ int check(const dynb_norm_shape* s, const std::string& who)
     if (s->T < 0 || s->d <= 0) return fail(DYNB_E_INVAL, who + ": sizes must be positive");
     if (!(s->eps >= 0.f)) return fail(DYNB_E_INVAL, who + ": eps must not be negative");
     if (s->dtype != DYNB_F32 && s->dtype != DYNB_BF16) return fail(DYNB_E_UNSUPPORTED, who + ": unknown dtype");
+    if (s->d > 1 << 28) return fail(DYNB_E_UNSUPPORTED, who + ": more than 2^28 columns");
     return DYNB_OK;
 }
 constexpr int64_t MOST_ROWS = 1 << 21;                         // of a launch (which has room for 2^32 threads)

@@ -252,3 +252,61 @@ def test_other_streams_and_graphs(dyn):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(ref, (out, din, dW)))
+
+
+def test_rows_beyond_four_gigabytes(dyn):
+    """Rows a megaelement apart: offsets into x, dout and the results pass 32 bits, whether rows are gathered or not."""
+    g = torch.Generator().manual_seed(12)
+    M, K, N, E, pitch = 2100, 64, 72, 3, 1 << 20
+    off = torch.tensor([0, 700, 701, M], dtype=torch.int32).cuda()
+    buf = torch.empty(M * pitch, dtype=BF, device="cuda")
+    wide = buf.view(M, pitch)
+    x, dout, W = dev(bf(g, M, K)), dev(bf(g, M, N)), dev(bf(g, E, N, K))
+    perm = torch.randperm(2 * M, generator=g).int().cuda()
+    off2 = (off * 2).contiguous()
+    wide[:, 128:128 + K], wide[:, 256:256 + N] = x, dout
+    xv, dv = wide[:, 128:128 + K], wide[:, 256:256 + N]
+    # (the dense tensors run another kernel where the offsets decide; products of the same numbers, rounded once each)
+    close = lambda a, b: torch.allclose(a.float(), b.float(), rtol=2.0 ** -7, atol=1e-3)
+    assert close(dyn.moe_product(xv, W, off), dyn.moe_product(x, W, off))
+    assert close(dyn.moe_product(xv, W, off2, perm=perm, k=2), dyn.moe_product(x, W, off2, perm=perm, k=2))
+    assert close(dyn.moe_product_grad_input(dv, W, off, act=xv), dyn.moe_product_grad_input(dout, W, off, act=x))
+    assert torch.allclose(dyn.moe_product_grad_weight(dv, xv, off), dyn.moe_product_grad_weight(dout, x, off), rtol=1e-4, atol=1e-2)
+    d2 = dev(bf(g, 2 * M, N))
+    assert torch.allclose(dyn.moe_product_grad_weight(d2, xv, off2, perm=perm, k=2), dyn.moe_product_grad_weight(d2, x, off2, perm=perm, k=2), rtol=1e-4, atol=1e-2)
+    out = wide[:, 512:512 + N]
+    dyn.moe_product(x, W, off, out=out)
+    assert close(out, dyn.moe_product(x, W, off))
+
+
+@pytest.mark.parametrize("M,K,N,E,loads", [(16384, 2048, 1928, 20, "skew"), (20001, 2056, 2048, 30, "holes"), (16384, 1024, 1024, 20, "skew"), (13000, 2048, 1032, 30, "holes"), (9000, 136, 200, 400, "skew"), (30000, 264, 72, 2, "tail")])
+def test_many_rows_of_every_kind_of_tile(dyn, M, K, N, E, loads):
+    """Sizes at which every kind of tile runs (crowded experts on the largest), against products in 64 bits on the GPU."""
+    g = torch.Generator().manual_seed(M)
+    r = np.random.Generator(np.random.Philox(key=[M, K]))
+    share = r.random(E) ** 3
+    if loads == "holes":
+        share[::3] = 0
+    counts = np.bincount(r.choice(E, M - M // 3 if loads == "tail" else M, p=share / share.sum()), minlength=E)
+    off = torch.from_numpy(np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)).cuda()
+    at = off.tolist()
+    x, W, dout = dev(bf(g, (M + 1) // 2, K)), dev(bf(g, E, N, K, std=K ** -0.5)), dev(bf(g, M, N, std=N ** -0.5))
+    perm, act = torch.randperm(M, generator=g).int().cuda(), dev(bf(g, M, K))
+    rows = x.double()[perm.long() // 2]
+    fwd, gin = torch.zeros(M, N, dtype=torch.float64, device="cuda"), torch.zeros(M, K, dtype=torch.float64, device="cuda")
+    bf_, bi = torch.zeros_like(fwd), torch.zeros_like(gin)
+    gw, bw = torch.zeros(E, N, K, dtype=torch.float64, device="cuda"), torch.zeros(E, N, K, dtype=torch.float64, device="cuda")
+    for e in range(E):
+        a, b, w, d = at[e], at[e + 1], W[e].double(), dout[at[e]:at[e + 1]].double()
+        fwd[a:b], bf_[a:b] = rows[a:b] @ w.t(), K * 2.0 ** -23 * (rows[a:b].abs() @ w.abs().t())
+        gin[a:b], bi[a:b] = (d @ w) * (act[a:b] > 0), N * 2.0 ** -23 * (d.abs() @ w.abs())
+        gw[e], bw[e] = d.t() @ rows[a:b], (b - a) * 2.0 ** -23 * (d.abs().t() @ rows[a:b].abs())
+    cpu = lambda t: t.cpu()
+    got = dyn.moe_product(x, W, off, perm=perm, k=2, relu=True, out=torch.full((M, N), float("nan"), dtype=BF, device="cuda"))
+    within(got, cpu(fwd.clamp(min=0)), cpu(stored(fwd.clamp(min=0), bf_, BF)), "forward")
+    got = dyn.moe_product_grad_input(dout, W, off, act=act, out=torch.full((M, K), float("nan"), dtype=BF, device="cuda"))
+    within(got, cpu(gin), cpu(stored(gin, bi, BF)), "input's gradient")
+    for dt in (torch.float32, BF):
+        got = dyn.moe_product_grad_weight(dout, x, off, perm=perm, k=2, dW=torch.full((E, N, K), float("nan"), dtype=dt, device="cuda"))
+        within(got, cpu(gw), cpu(stored(gw, bw, dt)), "weights' gradient")
+        assert torch.equal(got, dyn.moe_product_grad_weight(dout, x, off, perm=perm, k=2, dW=torch.empty_like(got)))

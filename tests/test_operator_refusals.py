@@ -58,6 +58,7 @@ def test_embeddings():
         for kw in (dict(T=-1), dict(V=0), dict(d=0), dict(tokens=None), dict(tokens=P + 2)):
             assert call(**kw) == "DYNB_E_INVAL", kw
         assert call(dtype=3) == "DYNB_E_UNSUPPORTED"
+        assert call(T=(1 << 25) + 1) == call(V=(1 << 27) + 1) == call(d=(1 << 28) + 1) == "DYNB_E_UNSUPPORTED"
     for kw in (dict(table=None), dict(out=None), dict(os_=7), dict(table=P + 2), dict(out=P + 1)):
         assert look(**kw) == "DYNB_E_INVAL", kw
     for kw in (dict(dout=None), dict(dt=None), dict(ws=None), dict(ds=7), dict(dout=P + 2), dict(dt=P + 2), dict(ws=P + 8)):
@@ -76,7 +77,7 @@ def test_layer_norm():
     for call in (fwd, bwd):
         for kw in (dict(T=-1), dict(d=0), dict(eps=-1.0), dict(eps=float("nan")), dict(x=None), dict(xs=7), dict(x=P + 2), dict(gamma=P + 1), dict(mean=P + 2)):
             assert call(**kw) == "DYNB_E_INVAL", kw
-        assert call(dtype=2) == "DYNB_E_UNSUPPORTED"
+        assert call(dtype=2) == call(d=(1 << 28) + 1) == "DYNB_E_UNSUPPORTED"
     for kw in (dict(y=None), dict(ys=7), dict(beta=P + 2), dict(rstd=P + 1)):
         assert fwd(**kw) == "DYNB_E_INVAL", kw
     for kw in (dict(dy=None), dict(mean=None), dict(rstd=None), dict(ws=None), dict(ds=7), dict(dxs=7), dict(dg=P + 2), dict(db=P + 1), dict(ws=P + 64)):
@@ -93,5 +94,6 @@ def test_clipping():
     for kw in (dict(n=-1), dict(norm=None), dict(ws=None), dict(ws=P + 8), dict(max_norm=0.0), dict(max_norm=-1.0), dict(max_norm=float("nan")),
                dict(tensors=((None, P, 8, 0),)), dict(tensors=((P, P, -1, 0),)), dict(tensors=((P + 2, P, 8, 0),)), dict(tensors=((P, P, 8, 0), (P, P + 1, 8, 1)))):
         assert clip(**kw) == "DYNB_E_INVAL", kw
+    assert clip(tensors=((P, P, (1 << 42) + 1, 1),)) == "DYNB_E_UNSUPPORTED"
     assert clip(wb=8) == "DYNB_E_WORKSPACE" and clip(tensors=((P, P, 8, 4),)) == "DYNB_E_UNSUPPORTED"
     assert code(L.dynb_clip_gradients(None, 1, 1.0, P, P, 1 << 40, None)) == "DYNB_E_INVAL"
