@@ -35,11 +35,11 @@ struct Groups {
 
 struct Piece { int e, begin, rows; };                          // rows begin .. of group e (E: what lies behind the last group)
 
-__device__ __forceinline__ Piece piece_of(const Groups& g, int P, int unit, int e)
+__device__ __forceinline__ Piece piece_of(int P, int unit, int e, int a, int b)
 {
     Piece p;
     p.e = e;
-    const int a = g.begin(e), rows = g.begin(e + 1) - a, part = unit - (a / P + e);
+    const int rows = b - a, part = unit - (a / P + e);
     p.begin = a + part * P;
     p.rows = rows > 0 && part <= (rows - 1) / P ? min(P, rows - part * P) : 0;
     return p;
@@ -49,14 +49,17 @@ __device__ __forceinline__ Piece find_piece(const Groups& g, int P, int unit)
 {
     const int lane = threadIdx.x & 63;
     int lo = 0, n = g.E + 1;                                   // the group is one of lo .. lo + n - 1
-    while (n > 1) {
+    while (n > 63) {
         const int step = (n + 63) / 64, e = lo + lane * step;
         const bool here = lane * step < n && g.begin(e) / P + e <= unit;
         const int last = 63 - __builtin_clzll(__ballot(here) | 1ull);
         lo += last * step;
         n = min(step, n - last * step);
     }
-    return piece_of(g, P, unit, __builtin_amdgcn_readfirstlane(lo));
+    // (a lane a group, and one behind them: the group's borders need no further load)
+    const int e = lo + lane, begin = g.begin(min(e, g.E + 1));
+    const int last = 63 - __builtin_clzll(__ballot(lane < n && begin / P + e <= unit) | 1ull);
+    return piece_of(P, unit, lo + last, __builtin_amdgcn_readlane(begin, last), __builtin_amdgcn_readlane(begin, last + 1));
 }
 // ... for every lane its own
 __device__ __forceinline__ Piece find_piece_alone(const Groups& g, int P, int unit)
@@ -67,7 +70,7 @@ __device__ __forceinline__ Piece find_piece_alone(const Groups& g, int P, int un
         if (g.begin(lo + half) / P + lo + half <= unit) { lo += half; n -= half; }
         else n = half;
     }
-    return piece_of(g, P, unit, lo);
+    return piece_of(P, unit, lo, g.begin(lo), g.begin(lo + 1));
 }
 
 struct Args {
@@ -346,12 +349,11 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
 #pragma unroll
                 for (int j = 0; j < EACH; ++j) uses[j] = p.g.perm[asked.begin + min(z_asked + copied_place(wave + j * S::WAVES, lane), asked.depth - 1)];
     };
-    auto open = [&](const Tile& t) {
+    auto open_a = [&](const Tile& t) {
         asked = t;
         z_asked = 0;
         const size_t w = size_t(t.e) * size_t(p.N) * size_t(p.K);
         a_base = reinterpret_cast<const char*>(DIR == GRAD_WEIGHT ? p.a + (gathers ? 0 : t.begin * p.a_stride) : DIR == FORWARD ? p.a + w + size_t(t.c0) * size_t(p.K) : p.a + w);
-        b_base = reinterpret_cast<const char*>(DIR == FORWARD && gathers ? p.b : p.b + t.begin * p.b_stride);
 #pragma unroll
         for (int j = 0; j < EACH; ++j) {
             const int block = wave + j * S::WAVES, s_q = copied_row(block, lane), z = copied_place(block, lane);
@@ -363,6 +365,13 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
                 else if constexpr (DIR == GRAD_INPUT) a_off[i][j] = uint32_t(z) * uint32_t(p.K) * 2u + col;
                 else a_off[i][j] = (gathers ? 0u : uint32_t(z) * uint32_t(p.a_stride) * 2u) + col;
             }
+        }
+    };
+    auto open_b = [&](const Tile& t) {
+        b_base = reinterpret_cast<const char*>(DIR == FORWARD && gathers ? p.b : p.b + t.begin * p.b_stride);
+#pragma unroll
+        for (int j = 0; j < EACH; ++j) {
+            const int block = wave + j * S::WAVES, s_q = copied_row(block, lane), z = copied_place(block, lane);
 #pragma unroll
             for (int i = 0; i < BU; ++i) {
                 if constexpr (B_ACROSS) b_off[i][j] = uint32_t(z) * uint32_t(p.b_stride) * 2u + uint32_t(min(t.r0 + i * 64 + (lane & 7) * 8, p.N - 8)) * 2u;
@@ -373,10 +382,14 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
                 }
             }
         }
+    };
+    auto open = [&](const Tile& t) {
+        open_a(t);
+        open_b(t);
         look_up_places();
     };
     // ahead of a chunk's requests
-    auto prepare = [&]() {
+    auto prepare = [&](bool a_too = true, bool b_too = true) {
         const int rest = asked.depth - z_asked;
         if (rest < 64) {                                       // (the tile's last: its offsets are not used again)
 #pragma unroll
@@ -384,9 +397,9 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
                 const int z = copied_place(wave + j * S::WAVES, lane);
                 const uint32_t places = uint32_t(max(z - (rest - 1), 0)), pieces = (lane & 7) * 8 >= rest ? piece : 0u;
 #pragma unroll
-                for (int i = 0; i < AU; ++i) a_off[i][j] -= DIR == FORWARD ? pieces : DIR == GRAD_INPUT ? places * uint32_t(p.K) * 2u : gathers ? 0u : places * uint32_t(p.a_stride) * 2u;
+                for (int i = 0; i < AU; ++i) if (a_too) a_off[i][j] -= DIR == FORWARD ? pieces : DIR == GRAD_INPUT ? places * uint32_t(p.K) * 2u : gathers ? 0u : places * uint32_t(p.a_stride) * 2u;
 #pragma unroll
-                for (int i = 0; i < BU; ++i) b_off[i][j] -= B_ACROSS ? places * uint32_t(p.b_stride) * 2u : pieces;
+                for (int i = 0; i < BU; ++i) if (b_too) b_off[i][j] -= B_ACROSS ? places * uint32_t(p.b_stride) * 2u : pieces;
             }
         }
         if constexpr (DIR == GRAD_WEIGHT) {
@@ -435,17 +448,32 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
         const int nchunk = (now.depth + 63) / 64;
         if (nchunk > 0 && !primed) {
             look_up_rows(now);
-            rows_looked_up();
-            open(now);
             fill = take;                                       // (what was asked for behind the last tile is overwritten)
+            if constexpr (STAYS) {
+                rows_looked_up();
+                open(now);
+                prepare();
+                request(lds + fill, 0, REQUESTS);
+                requested();
+                fill = next_place(fill);
+            } else {
+                // the columns' pieces first, which need no look at `perm`
+                open_a(now);
 #pragma unroll
-            for (int c = 0; c < AHEAD; ++c)
-                if (c < nchunk) {
-                    prepare();
-                    request(lds + fill, 0, REQUESTS);
-                    requested();
-                    fill = next_place(fill);
+                for (int half = 0; half < 2; ++half) {
+                    if (half == 1) open_b(now);
+#pragma unroll
+                    for (int c = 0; c < AHEAD; ++c)
+                        if (c < nchunk) {
+                            z_asked = c * 64;
+                            prepare(half == 0, half == 1);
+                            request(lds + c * BUF, half ? AU * EACH : 0, half ? REQUESTS : AU * EACH);
+                            (half ? b_base : a_base) += half ? b_step : a_step;
+                        }
                 }
+                z_asked = min(AHEAD, nchunk) * 64;
+                fill = uint32_t(min(AHEAD, nchunk)) % uint32_t(S::BUFS) * BUF;
+            }
             stores = 0;
         }
         Tile then = {};
@@ -461,7 +489,8 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
                     else answered_but<4>();
                 } else answered_but<0>();
             } else {
-                if (c + 1 < nchunk) answered_but<REQUESTS>();
+                if (c == 0 && nchunk > 1) answered_but<BU * EACH>();       // (both chunks' columns were asked for ahead of the rows)
+                else if (c + 1 < nchunk) answered_but<REQUESTS>();
                 else answered_but<0>();
             }
             meet();
