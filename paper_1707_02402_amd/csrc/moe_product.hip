@@ -73,6 +73,45 @@ __device__ __forceinline__ Piece find_piece_alone(const Groups& g, int P, int un
     return piece_of(P, unit, lo, g.begin(lo), g.begin(lo + 1));
 }
 
+// Fewer rows than groups: most groups are empty, and a launch with room for them all would be workgroups with nothing to do for the most part (74 rows, 256
+// experts, K 512: 13.3 us, COUNTED with room for as many groups as rows).  The unit counts pieces then: every workgroup of 256 threads adds them up.
+constexpr int COUNTED = 2048;            // most groups, eight a thread
+__host__ __device__ __forceinline__ bool counted(int M, int E) { return M < E && E < COUNTED; }
+__host__ __device__ __forceinline__ int64_t most_pieces(int M, int E, int P) { return int64_t(M) / P + (counted(M, E) ? M : E) + 1; }
+// All 256 threads call it; room: 7 ints of LDS
+__device__ __forceinline__ Piece count_pieces(const Groups& g, int P, int unit, int* room)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, per = (g.E + 256) / 256, e0 = min(tid * per, g.E + 1), e1 = min(e0 + per, g.E + 1);
+    int mine = 0;
+    for (int e = e0; e < e1; ++e) mine += (max(g.begin(e + 1) - g.begin(e), 0) + P - 1) / P;
+    int ahead = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int v = __shfl_up(ahead, o);
+        ahead += lane >= o ? v : 0;
+    }
+    if (lane == 63) room[wave] = ahead;
+    if (tid == 0) room[6] = 0;
+    __syncthreads();
+    ahead -= mine;
+    for (int w = 0; w < wave; ++w) ahead += room[w];
+    if (unit >= ahead && unit < ahead + mine)
+        for (int e = e0; e < e1; ++e) {
+            const int a = g.begin(e), n = max(g.begin(e + 1) - a, 0), pieces = (n + P - 1) / P;
+            if (unit < ahead + pieces) {
+                room[4] = e;
+                room[5] = a + (unit - ahead) * P;
+                room[6] = min(P, n - (unit - ahead) * P);
+                break;
+            }
+            ahead += pieces;
+        }
+    __syncthreads();
+    const Piece p = {__builtin_amdgcn_readfirstlane(room[4]), __builtin_amdgcn_readfirstlane(room[5]), __builtin_amdgcn_readfirstlane(room[6])};
+    __syncthreads();
+    return p;
+}
+
 struct Args {
     Groups g;
     const bf16_t *a, *b;      // what gives the results' columns, and their rows
@@ -193,7 +232,9 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
     const lds_ptr lds = (lds_ptr)lds_raw;
 
     // workgroups of a die (every eighth) are neighbours among the units: they share weights and rows in its L2
-    const int per_die = int(gridDim.x) / 8, place = int(blockIdx.x) < per_die * 8 ? int(blockIdx.x & 7) * per_die + int(blockIdx.x >> 3) : int(blockIdx.x);
+    // (counted units: those that there are come first, and go to all dies)
+    const bool counts = !STAYS && counted(p.g.M, p.g.E);
+    const int per_die = int(gridDim.x) / 8, place = !counts && int(blockIdx.x) < per_die * 8 ? int(blockIdx.x & 7) * per_die + int(blockIdx.x >> 3) : int(blockIdx.x);
 
     // ---- the tiles
     // forward, input's gradient: unit = piece of rows * ct + column; a workgroup that stays takes every gridDim.x-th unit, by the list.
@@ -309,7 +350,7 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
             }
         } else if (++at_unit == 0) {
             const Place w = walk<1>(place, units / ct, ct);
-            t = tile_of(find_piece(p.g, S::ROWS, w.row), w.col);
+            t = tile_of(counts ? count_pieces(p.g, S::ROWS, w.row, reinterpret_cast<int*>(lds_raw)) : find_piece(p.g, S::ROWS, w.row), w.col);
         }
         return t;
     };
@@ -832,7 +873,7 @@ __global__ __launch_bounds__(256, 2) void k_product_any(Args p, int units, int c
         }
     } else {
         const Place w = walk<1>(int(blockIdx.x), units / ct, ct);
-        const Piece at = find_piece(p.g, S::ROWS, w.row);
+        const Piece at = counted(p.g.M, p.g.E) ? count_pieces(p.g, S::ROWS, w.row, reinterpret_cast<int*>(lds_raw)) : find_piece(p.g, S::ROWS, w.row);
         if (at.rows > 0) work(Tile{at.e, at.begin, at.rows, w.col * S::COLS, 0, at.e < p.g.E ? (DIR == FORWARD ? p.K : p.N) : 0, -1});
     }
 }
@@ -974,7 +1015,7 @@ int launch_rows(const moe_product_shape* s, const Args& p, bool fast, hipStream_
     auto launch = [&](auto kind) {
         using S = decltype(kind);
         const int ct = (cols + S::COLS - 1) / S::COLS;
-        const int64_t units = (int64_t(s->M) / S::ROWS + s->E + 1) * ct;
+        const int64_t units = (S::BIG ? int64_t(s->M) / S::ROWS + s->E + 1 : most_pieces(s->M, s->E, S::ROWS)) * ct;
         if (units > MOST_GROUPS) return fail(DYNB_E_UNSUPPORTED, std::string(who) + ": too many results");
         return launch_kernel<DIR, S>(p.relu || p.act ? k_product<DIR, bf16_t, S, true> : k_product<DIR, bf16_t, S, false>, p, S::BIG ? std::min<int64_t>(units, CUS) : units, units, ct, 1,
                                      Shares{}, nullptr, st, who);
@@ -985,7 +1026,7 @@ int launch_rows(const moe_product_shape* s, const Args& p, bool fast, hipStream_
         default: return launch(Few{});
         }
     const int ct = (cols + Mid::COLS - 1) / Mid::COLS;
-    const int64_t units = (int64_t(s->M) / Mid::ROWS + s->E + 1) * ct;
+    const int64_t units = most_pieces(s->M, s->E, Mid::ROWS) * ct;
     if (units > MOST_GROUPS) return fail(DYNB_E_UNSUPPORTED, std::string(who) + ": too many results");
     return launch_kernel<DIR, Mid>(k_product_any<DIR, bf16_t>, p, units, units, ct, 1, Shares{}, nullptr, st, who);
 }
