@@ -74,7 +74,7 @@ __device__ __forceinline__ Piece find_piece_alone(const Groups& g, int P, int un
 }
 
 // Fewer rows than groups: most groups are empty, and a launch with room for them all would be workgroups with nothing to do for the most part (74 rows, 256
-// experts, K 512: 13.3 us, COUNTED with room for as many groups as rows).  The unit counts pieces then: every workgroup of 256 threads adds them up.
+// experts, K 512: 13.3 us, 9.8 with room for as many groups as rows).  The unit counts pieces then: every workgroup of 256 threads adds them up.
 constexpr int COUNTED = 2048;            // most groups, eight a thread
 __host__ __device__ __forceinline__ bool counted(int M, int E) { return M < E && E < COUNTED; }
 __host__ __device__ __forceinline__ int64_t most_pieces(int M, int E, int P) { return int64_t(M) / P + (counted(M, E) ? M : E) + 1; }
@@ -487,6 +487,22 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
     int stores = 0;                                            // of this wave, behind that request
     while (now.rows > 0) {
         const int nchunk = (now.depth + 63) / 64;
+        // The mask's pieces, as the results will leave, ahead of everything (Big has no registers for them and loads them with the results).  8192 rows of 256 experts,
+        // 512 features, 1024 channels: 65 us with loads at the end, 64 so, 57 without a mask.
+        constexpr bool ACT_AHEAD = DIR == GRAD_INPUT && FUSED && !STAYS;
+        constexpr int ACT_STORES = ACT_AHEAD ? FA * 2 : 1;     // pieces of a block of 32 rows
+        u32x4 act_ahead[ACT_AHEAD ? NB : 1][ACT_STORES];
+        if constexpr (ACT_AHEAD) {
+            constexpr int LANES = FA * 4;
+            const int col = min(now.c0 + cg * (FA * 32) + lane % LANES * 8, cols - 8);
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int i = 0; i < ACT_STORES; ++i) {
+                    const int r = min((b * S::RG + rg) * 32 + lane / LANES + i * (64 / LANES), now.rows - 1);
+                    act_ahead[b][i] = *reinterpret_cast<const u32x4*>(p.act + int64_t(now.begin + r) * p.act_stride + col);
+                }
+        }
         if (nchunk > 0 && !primed) {
             look_up_rows(now);
             fill = take;                                       // (what was asked for behind the last tile is overwritten)
@@ -682,6 +698,11 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
                     wave_sync();
                     constexpr int STORES = 32 / AT_ONCE;
                     u32x4 v[STORES], act[STORES];
+                    if constexpr (ACT_AHEAD) {
+                        static_assert(STORES == ACT_STORES, "the pieces that were loaded");
+#pragma unroll
+                        for (int i = 0; i < STORES; ++i) act[i] = act_ahead[b][i];
+                    }
 #pragma unroll
                     for (int i = 0; i < STORES; ++i) v[i] = *(const __attribute__((address_space(3))) u32x4*)(out_at + i * AT_ONCE * PITCH);
                     if (nchunk == 0)
@@ -696,7 +717,7 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
                     };
                     const int left = now.rows - (b * S::RG + rg) * 32;
                     if (left >= 32 && now.c0 + cg * (FA * 32) + FA * 32 <= cols) {
-                        if constexpr (DIR == GRAD_INPUT && FUSED)
+                        if constexpr (DIR == GRAD_INPUT && FUSED && !ACT_AHEAD)
 #pragma unroll
                             for (int i = 0; i < STORES; ++i) act[i] = *reinterpret_cast<const u32x4*>(act_at + i * act_step);
 #pragma unroll
@@ -705,7 +726,7 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
 #pragma unroll
                         for (int i = 0; i < STORES; ++i)
                             if (row + i * AT_ONCE < left && on) {
-                                if constexpr (DIR == GRAD_INPUT && FUSED) act[i] = *reinterpret_cast<const u32x4*>(act_at + i * act_step);
+                                if constexpr (DIR == GRAD_INPUT && FUSED && !ACT_AHEAD) act[i] = *reinterpret_cast<const u32x4*>(act_at + i * act_step);
                                 one(i);
                             }
                     lane_to += to_next;
