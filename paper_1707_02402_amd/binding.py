@@ -180,14 +180,14 @@ lib = _load()
 
 
 def _check(rc: int):
-    if rc != 0:
+    if rc:
         raise DynbError(rc, lib.dynb_last_error().decode())
 
 
 def _stream(stream=None):
-    import torch
     if stream is None:                           # (current_stream() builds an object: 2.6 us, more than the smallest kernels take)
-        return ct.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
+        import torch
+        return ct.c_void_p(torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()))
     return ct.c_void_p(stream.cuda_stream)
 
 
@@ -538,17 +538,19 @@ MOE_PRODUCT_RELU = 1
 
 def _dtype_code(t) -> int:
     import torch
-    if t.dtype == torch.float32:
+    dtype = t.dtype
+    if dtype is torch.float32:
         return DYNB_F32
-    assert t.dtype == torch.bfloat16, t.dtype
+    assert dtype is torch.bfloat16, dtype
     return DYNB_BF16
 
 
 def _rows(t, n: int, width: int, like=None) -> int:
     """Checks a tensor of n rows of `width` neighbouring elements; returns the elements from a row to the next."""
-    assert t.is_cuda and t.dim() == 2 and t.shape[0] == n and t.shape[1] == width and (width == 1 or t.stride(1) == 1), (t.shape, t.stride())
-    assert like is None or t.dtype == like.dtype
-    return t.stride(0) if n > 1 else max(t.stride(0), width)
+    stride = t.stride()
+    assert t.is_cuda and t.shape == (n, width) and (width == 1 or stride[1] == 1), (t.shape, stride)
+    assert like is None or t.dtype is like.dtype
+    return stride[0] if n > 1 else max(stride[0], width)
 
 
 def _new(stream, *shape, like, dtype=None):
@@ -668,9 +670,11 @@ def dynb_embed_backward(tokens, dout, V: int, scale: float = 1.0, dtable=None, g
 
 # ------------------------------------------------------------------------------------------ layer norm
 def _fp32(t, n: int):
+    if t is None:
+        return None
     import torch
-    assert t is None or (t.is_cuda and t.is_contiguous() and t.dtype == torch.float32 and t.shape == (n,))
-    return None if t is None else t.data_ptr()
+    assert t.is_cuda and t.dtype is torch.float32 and t.shape == (n,) and t.is_contiguous()
+    return t.data_ptr()
 
 
 def dynb_layer_norm(x, gamma=None, beta=None, eps: float = 1e-5, out=None, want_stats: bool = False, stream=None):
@@ -682,12 +686,14 @@ def dynb_layer_norm(x, gamma=None, beta=None, eps: float = 1e-5, out=None, want_
     if out is None:
         out = _new(stream, T, d, like=x)
     ys = _rows(out, T, d, x)
-    mean = _new(stream, T, like=x, dtype=torch.float32) if want_stats else None
-    rstd = _new(stream, T, like=x, dtype=torch.float32) if want_stats else None
     shape = _NormShape(T, d, _dtype_code(x), eps)
-    _check(lib.dynb_layer_norm(ct.byref(shape), x.data_ptr(), xs, _fp32(gamma, d), _fp32(beta, d), out.data_ptr(), ys, _fp32(mean, T), _fp32(rstd, T),
+    if not want_stats:
+        _check(lib.dynb_layer_norm(ct.byref(shape), x.data_ptr(), xs, _fp32(gamma, d), _fp32(beta, d), out.data_ptr(), ys, None, None, _stream(stream)))
+        return out
+    mean, rstd = _new(stream, T, like=x, dtype=torch.float32), _new(stream, T, like=x, dtype=torch.float32)
+    _check(lib.dynb_layer_norm(ct.byref(shape), x.data_ptr(), xs, _fp32(gamma, d), _fp32(beta, d), out.data_ptr(), ys, mean.data_ptr(), rstd.data_ptr(),
                                _stream(stream)))
-    return (out, mean, rstd) if want_stats else out
+    return out, mean, rstd
 
 
 def dynb_layer_norm_backward_workspace_bytes(T: int, d: int, dtype: int) -> int:
