@@ -64,3 +64,13 @@ __device__ __forceinline__ void wait_for_stores()
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");    // (the compiler, too, keeps earlier stores ahead of what follows)
     __builtin_amdgcn_s_waitcnt(0x0f70);                       // vmcnt(0)
 }
+
+// What this workgroup stored (each wave behind wait_for_stores and a barrier) is in memory, where every CU can see it: one thread calls this, then raises
+// the flag.  The wait is written out, because an atomic with a release of its own does without it here: the compiler finds no load or store between the
+// wait above and the atomic, does not count the write-back as one, and leaves out the wait behind it, so that the flag could be seen while the write-back was
+// under way, and other L2s' workgroups read what memory held before.
+__device__ __forceinline__ void release_to_chip()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");        // writes the L2's dirty lines back
+    __builtin_amdgcn_s_waitcnt(0x0f70);                       // vmcnt(0): it has been answered
+}

@@ -470,12 +470,14 @@ __global__ __launch_bounds__(256, 1) void k_module_persist(MfArgs a, PersistArgs
         else module_body<2>(b, part - 1);
         // Publish: every wave waits until its stores of the result have reached the L2 (all waves of a
         // workgroup sit behind the same one), then one thread writes that L2's dirty lines back to memory,
-        // where every CU can see them, and raises the flag (the agent-scope release does both).
+        // where every CU can see them, waits until that is done, and raises the flag.
         wait_for_stores();
         __syncthreads();                                      // also frees the LDS tile for the next unit
         const int32_t dst = b.items[0].dst;
-        if (threadIdx.x == 0 && dst >= 0)
-            __hip_atomic_fetch_add(q.ready + dst, part == 0 ? 2 : 1, __ATOMIC_RELEASE, __HIP_MEMORY_SCOPE_AGENT);
+        if (threadIdx.x == 0 && dst >= 0) {
+            release_to_chip();
+            __hip_atomic_fetch_add(q.ready + dst, part == 0 ? 2 : 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
     }
 }
 

@@ -907,7 +907,10 @@ __global__ __launch_bounds__(256) void k_topk_group(const float* __restrict__ lo
     // last one sees what all others have made visible
     wait_for_stores();
     __syncthreads();
-    if (tid == 0) s_last = __hip_atomic_fetch_add(done, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == int(gridDim.x) - 1;
+    if (tid == 0) {
+        release_to_chip();
+        s_last = __hip_atomic_fetch_add(done, 1, __ATOMIC_ACQUIRE, __HIP_MEMORY_SCOPE_AGENT) == int(gridDim.x) - 1;
+    }
     __syncthreads();
     if (!s_last) return;
     const int A = T * k, stride = mid_stride(E);
