@@ -41,8 +41,6 @@ __global__ __launch_bounds__(256) void k_embed(const int32_t* __restrict__ token
 // The uses are brought into the order of their tokens (each token's in the order they stand in), so that a row's gradient is one sum, in one
 // order; a row without uses is a row of zeros.  A wave sums the columns of a row that it reads in pieces of 16 bytes a lane (512 of bfloat16; the launches' y
 // runs over the columns), and a workgroup's waves share the uses of a row that has many.
-constexpr int MANY = 64;                                       // uses of a row that are one wave's
-constexpr int AHEAD = 8;                                       // rows a wave has under way
 
 // E: elements of a lane's piece.  Sums that leave in fp32 are stored 16 bytes a lane, lane by lane, so bfloat16 is then read in pieces of 8 bytes (pieces of 16
 // would leave in two stores of 16 bytes of every 32: 50021 rows x 1024, each used once: 77 us instead of 66)
@@ -74,15 +72,15 @@ struct Sums {
 #pragma unroll
                 for (int j = 0; j < E; ++j) v[i][j] += element<T>(raw[k][i], j);
     }
-    // this lane's columns, c .. and STEP further, of the rows at(0) .. at(n - 1)
-    template <typename At>
+    // this lane's columns, c .. and STEP further, of the rows at(0) .. at(n - 1), AHEAD (up to 8) of them under way
+    template <int AHEAD, typename At>
     __device__ __forceinline__ void add(const T* rows, int64_t stride, int c, int d, int n, At&& at)
     {
         int u = 0;
         for (; u + AHEAD <= n; u += AHEAD) add_some<AHEAD>(rows, stride, c, d, u, at);
-        if (u + AHEAD / 2 <= n) {
-            add_some<AHEAD / 2>(rows, stride, c, d, u, at);
-            u += AHEAD / 2;
+        if (u + 4 <= n) {
+            add_some<4>(rows, stride, c, d, u, at);
+            u += 4;
         }
         if (u + 2 <= n) {
             add_some<2>(rows, stride, c, d, u, at);
@@ -122,6 +120,21 @@ struct Sums {
         }
         __syncthreads();
     }
+    // a row without uses.  PAST: past the caches, where it is whole pieces
+    template <bool PAST, typename TG>
+    static __device__ __forceinline__ void store_zeros(TG* row, int c, int d)
+    {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int left = d - c - i * STEP;
+            if (PAST && sizeof(TG) * E == 16 && left >= E)
+                __builtin_nontemporal_store(u32x4{0u, 0u, 0u, 0u}, reinterpret_cast<std::conditional_t<sizeof(TG) == 2, u32x4_at2, u32x4_at4>*>(row + c + i * STEP));
+            else {
+                const float w[E] = {};
+                store_piece<E>(row + c + i * STEP, left, w);
+            }
+        }
+    }
     template <typename TG>
     __device__ __forceinline__ void store(TG* row, int c, int d, float scale)
     {
@@ -144,18 +157,32 @@ __device__ __forceinline__ void wave_sync()
 }
 __device__ __forceinline__ int lanes_below(uint64_t who) { return __popcll(who & ((1ull << (threadIdx.x & 63)) - 1)); }
 
+// the first i of [from, n) with is(i), or n: 64 candidates at a time (one by one they took 40 ns each)
+template <typename Is>
+__device__ __forceinline__ int next_of(int from, int n, Is&& is)
+{
+    const int lane = threadIdx.x & 63;
+    for (; from < n; from += 64) {
+        const uint64_t who = __ballot(from + lane < n && is(from + lane));
+        if (who) return from + __builtin_ctzll(who);
+    }
+    return n;
+}
+
 // Up to FEW tokens, one launch: every workgroup picks the uses of its rows (up to FEW_ROWS) from all tokens, whose 32 KB it reads in less than the launches of a
 // sort would take.
-constexpr int FEW = 8192, FEW_WAVES = 16, FEW_ROWS = 128, FEW_STEPS = FEW / (FEW_WAVES * 64);
+// FEW_MANY: uses of a row from which all waves share them (4095 Zipf tokens, 20011 x 512: 1.9 us of 17 less than from 64).
+constexpr int FEW = 8192, FEW_WAVES = 16, FEW_ROWS = 256, FEW_MANY = 24, FEW_STEPS = FEW / (FEW_WAVES * 64);
 
-template <typename T, typename TG>
+template <typename T, typename TG, bool PAST>
 __global__ __launch_bounds__(FEW_WAVES * 64, 8) void k_embed_grad_few(const int32_t* __restrict__ tokens, const T* __restrict__ dout, TG* __restrict__ dtable, int n, int V, int d,
                                                                       int64_t dout_stride, float scale, int rows_each)
 {
     __shared__ uint32_t uses[FEW];                             // place of the token * FEW_ROWS + row, in the tokens' order
     __shared__ int32_t found[FEW_WAVES], count[FEW_ROWS];
-    __shared__ uint32_t mine[FEW_WAVES][MANY];
+    __shared__ uint32_t mine[FEW_WAVES][64];
     using S = SumsTo<T, TG>;
+    constexpr int AHEAD = sizeof(T) == 2 ? 6 : 8;              // (what 64 registers hold; two rows more of bfloat16 spilled: 21.5 us for 18.4, 4095 tokens, 20011 x 512)
     __shared__ float room[FEW_WAVES / 2][S::COLS];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int v0 = int(blockIdx.x) * rows_each, rows = min(rows_each, V - v0);
@@ -194,7 +221,12 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 8) void k_embed_grad_few(const int3
     // rows with few uses: a wave's each
     for (int r = wave; r < rows; r += FEW_WAVES) {
         const int k = __builtin_amdgcn_readfirstlane(count[r]);
-        if (k > MANY) continue;
+        if (k > FEW_MANY) continue;
+        if (k == 0) {
+            for (int c = int(blockIdx.y) * S::COLS + lane * S::STEP / 64; c - lane * S::STEP / 64 < d; c += int(gridDim.y) * S::COLS)
+                S::template store_zeros<PAST>(dtable + size_t(v0 + r) * size_t(d), c, d);
+            continue;
+        }
         for (int u = 0, seen = 0; seen < k; u += 64) {
             const uint32_t use = u + lane < all ? uses[u + lane] : NONE;
             const bool on = u + lane < all && use % FEW_ROWS == uint32_t(r);
@@ -206,15 +238,16 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 8) void k_embed_grad_few(const int3
         for (int c = int(blockIdx.y) * S::COLS + lane * S::STEP / 64; c - lane * S::STEP / 64 < d; c += int(gridDim.y) * S::COLS) {
             S s;
             s.clear();
-            s.add(dout, dout_stride, c, d, k, [&](int u) { return __builtin_amdgcn_readfirstlane(mine[wave][u]); });
+            s.template add<AHEAD>(dout, dout_stride, c, d, k, [&](int u) { return __builtin_amdgcn_readfirstlane(mine[wave][u]); });
             s.store(dtable + size_t(v0 + r) * size_t(d), c, d, scale);
         }
         wave_sync();
     }
     // rows with many: all waves', a sixteenth of the list each
-    for (int r = 0; r < rows; ++r) {
-        if (count[r] <= MANY) continue;
-        const int from = all * wave / FEW_WAVES, to = all * (wave + 1) / FEW_WAVES;
+    const int from = all * wave / FEW_WAVES, to = all * (wave + 1) / FEW_WAVES;
+    for (int r = -1;;) {
+        r = next_of(r + 1, rows, [&](int i) { return count[i] > FEW_MANY; });
+        if (r >= rows) break;
         for (int c = int(blockIdx.y) * S::COLS + lane * S::STEP / 64; c - lane * S::STEP / 64 < d; c += int(gridDim.y) * S::COLS) {
             S s;
             s.clear();
@@ -224,7 +257,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 8) void k_embed_grad_few(const int3
                 const uint64_t who = __ballot(on);
                 if (on) mine[wave][lanes_below(who)] = use / FEW_ROWS;
                 wave_sync();
-                s.add(dout, dout_stride, c, d, __popcll(who), [&](int i) { return __builtin_amdgcn_readfirstlane(mine[wave][i]); });
+                s.template add<AHEAD>(dout, dout_stride, c, d, __popcll(who), [&](int i) { return __builtin_amdgcn_readfirstlane(mine[wave][i]); });
                 wave_sync();
             }
             s.template join<FEW_WAVES>(room, wave);
@@ -390,35 +423,42 @@ __global__ __launch_bounds__(256) void k_embed_chunks(const uint32_t* __restrict
     for (int c = int(blockIdx.y) * S::COLS + lane * S::STEP / 64; c - lane * S::STEP / 64 < d; c += int(gridDim.y) * S::COLS) {
         S s;
         s.clear();
-        s.add(dout, dout_stride, c, d, CHUNK / 4, [&](int i) { return __builtin_amdgcn_readlane(mine, i); });
+        s.template add<8>(dout, dout_stride, c, d, CHUNK / 4, [&](int i) { return __builtin_amdgcn_readlane(mine, i); });
         s.template join<4>(room, wave);
         if (wave == 0) s.store(sums + size_t(blockIdx.x) * size_t(d), c, d, 1.f);
     }
 }
 
-constexpr int GRAD_ROWS = 16;                                  // rows of the table of a workgroup
+// Tiles of columns are neighbours in the launch, so that the chip writes one part of the table at a time (50021 rows x 1024, 65536 tokens: 123 us with all rows'
+// first tiles ahead of the second, 106 so; workgroups of 8 rows: 105, of 4: 110).
+constexpr int GRAD_ROWS = 8;                                   // rows of the table of a workgroup
+constexpr int MANY = 64;                                       // uses of a row that are one wave's (at least a chunk, so that more of them hold one's border)
 
-template <typename T, typename TG>
+template <typename T, typename TG, bool PAST>
 __global__ __launch_bounds__(256) void k_embed_grad(const Range* __restrict__ ranges, const int32_t* __restrict__ places, const T* __restrict__ dout,
-                                                    const float* __restrict__ sums, TG* __restrict__ dtable, int V, int d, int64_t dout_stride, float scale)
+                                                    const float* __restrict__ sums, TG* __restrict__ dtable, int V, int d, int64_t dout_stride, float scale, int tiles)
 {
     using S = SumsTo<T, TG>;
     __shared__ float room[2][S::COLS];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int v0 = int(blockIdx.x) * GRAD_ROWS, rows = min(GRAD_ROWS, V - v0);
+    const int tile = int(blockIdx.x % unsigned(tiles)), v0 = int(blockIdx.x / unsigned(tiles)) * GRAD_ROWS, rows = min(GRAD_ROWS, V - v0);
     const Range mine = ranges[v0 + min(lane, rows - 1)];
     const int k_mine = mine.end - mine.begin;
-    // rows with few uses: four neighbours a wave
+    // rows with few uses: neighbours a wave
 #pragma unroll
     for (int i = 0; i < GRAD_ROWS / 4; ++i) {
         const int r = wave * (GRAD_ROWS / 4) + i;
         const int from = __builtin_amdgcn_readlane(mine.begin, r), k = __builtin_amdgcn_readlane(k_mine, r);
         if (r >= rows || k > MANY) continue;
+        if (k == 0) {
+            for (int c = tile * S::COLS + lane * S::STEP / 64; c - lane * S::STEP / 64 < d; c += tiles * S::COLS) S::template store_zeros<PAST>(dtable + size_t(v0 + r) * size_t(d), c, d);
+            continue;
+        }
         const int32_t use = lane < k ? places[from + lane] : 0;
-        for (int c = int(blockIdx.y) * S::COLS + lane * S::STEP / 64; c - lane * S::STEP / 64 < d; c += int(gridDim.y) * S::COLS) {
+        for (int c = tile * S::COLS + lane * S::STEP / 64; c - lane * S::STEP / 64 < d; c += tiles * S::COLS) {
             S s;
             s.clear();
-            s.add(dout, dout_stride, c, d, k, [&](int u) { return __builtin_amdgcn_readlane(use, u); });
+            s.template add<8>(dout, dout_stride, c, d, k, [&](int u) { return __builtin_amdgcn_readlane(use, u); });
             s.store(dtable + size_t(v0 + r) * size_t(d), c, d, scale);
         }
     }
@@ -430,11 +470,11 @@ __global__ __launch_bounds__(256) void k_embed_grad(const Range* __restrict__ ra
         const int at = loose * wave / 4, k = loose * (wave + 1) / 4 - at, at_c = int(int64_t(chunks) * wave / 4), k_c = int(int64_t(chunks) * (wave + 1) / 4) - at_c;
         const int i = at + lane;
         const int32_t use = lane < k ? places[i < ahead ? from + i : to - to % CHUNK + i - ahead] : 0;
-        for (int c = int(blockIdx.y) * S::COLS + lane * S::STEP / 64; c - lane * S::STEP / 64 < d; c += int(gridDim.y) * S::COLS) {
+        for (int c = tile * S::COLS + lane * S::STEP / 64; c - lane * S::STEP / 64 < d; c += tiles * S::COLS) {
             S s;
             s.clear();
             s.add_sums(sums + size_t(c_from + at_c) * size_t(d), c, d, k_c);
-            s.add(dout, dout_stride, c, d, k, [&](int u) { return __builtin_amdgcn_readlane(use, u); });
+            s.template add<8>(dout, dout_stride, c, d, k, [&](int u) { return __builtin_amdgcn_readlane(use, u); });
             s.template join<4>(room, wave);
             if (wave == 0) s.store(dtable + size_t(v0 + r) * size_t(d), c, d, scale);
         }
@@ -536,22 +576,32 @@ extern "C" int dynb_embed_backward(const dynb_embed_shape* s, const int32_t* tok
         keys = to;
         places = places_to;
     }
-    auto launch = [&](auto in, auto grad) {
+    auto launch_as = [&](auto in, auto grad, auto past) {
         using T = decltype(in);
         using TG = decltype(grad);
+        constexpr bool PAST = decltype(past)::value;
         const T* const from = static_cast<const T*>(dout);
         TG* const to = static_cast<TG*>(dtable);
         const unsigned tiles = unsigned(std::min((s->d - 1) / SumsTo<T, TG>::COLS + 1, 64));
         if (L.passes == 0) {
-            // two workgroups a CU, if the rows are not too many for that
-            const int rows = int(std::min<int64_t>(std::max<int64_t>((int64_t(s->V) * tiles + 511) / 512, 16), FEW_ROWS));
-            hipLaunchKernelGGL((k_embed_grad_few<T, TG>), dim3(unsigned((s->V + rows - 1) / rows), tiles), dim3(FEW_WAVES * 64), 0, st, tokens, from, to, s->T, s->V, s->d, dout_stride,
+            // two workgroups a CU, if the rows are not too many for that, nor too few (8192 tokens, 777 x 64: 42 us with 16 rows, 30 with 4; 512 tokens,
+            // 2000 x 512: 6.9 with 8)
+            const int rows = int(std::min<int64_t>(std::max<int64_t>((int64_t(s->V) * tiles + 511) / 512, 4), FEW_ROWS));
+            hipLaunchKernelGGL((k_embed_grad_few<T, TG, PAST>), dim3(unsigned((s->V + rows - 1) / rows), tiles), dim3(FEW_WAVES * 64), 0, st, tokens, from, to, s->T, s->V, s->d, dout_stride,
                                s->scale, rows);
             return;
         }
         float* const sums = reinterpret_cast<float*>(ws + L.sums);
         hipLaunchKernelGGL((k_embed_chunks<T>), dim3(unsigned((s->T + CHUNK - 1) / CHUNK), tiles), dim3(256), 0, st, keys, places, from, sums, ranges, s->T, s->V, s->d, dout_stride);
-        hipLaunchKernelGGL((k_embed_grad<T, TG>), dim3(unsigned((s->V + GRAD_ROWS - 1) / GRAD_ROWS), tiles), dim3(256), 0, st, ranges, places, from, sums, to, s->V, s->d, dout_stride, s->scale);
+        const unsigned groups = unsigned((s->V + GRAD_ROWS - 1) / GRAD_ROWS), grad_tiles = std::min(tiles, 0xffffffffu / 256u / groups);      // (threads of a launch)
+        hipLaunchKernelGGL((k_embed_grad<T, TG, PAST>), dim3(groups * grad_tiles), dim3(256), 0, st, ranges, places, from, sums, to, s->V, s->d, dout_stride, s->scale, int(grad_tiles));
+    };
+    // Rows without uses are most of a large table.  Where the gradient is larger than the 256 MB behind the L2s, they are written past the caches, and what is read,
+    // or will be, stays (8192 tokens, 128000 rows x 1024 in fp32, with the gradients' norm taken behind it: 427 us through them, 377 past them); a smaller one is
+    // left for the norm to find there (50021 rows: 126 us, 140 past them).
+    auto launch = [&](auto in, auto grad) {
+        if (size_t(s->V) * size_t(s->d) * sizeof(grad) > size_t(256) << 20) launch_as(in, grad, std::true_type{});
+        else launch_as(in, grad, std::false_type{});
     };
     if (s->dtype == DYNB_BF16 && grad_dtype == DYNB_BF16) launch(bf16_t{}, bf16_t{});
     else if (s->dtype == DYNB_BF16) launch(bf16_t{}, float{});

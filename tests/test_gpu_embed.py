@@ -89,6 +89,24 @@ def test_strides_and_addresses(dyn, dtype, T, V, d, gap, offset):
     assert torch.allclose(dyn.dynb_embed_backward(tokens, dv, V, dtable=odd_grad), b, rtol=1e-4, atol=1e-4)
 
 
+@pytest.mark.parametrize("T", [300, 9000])
+@pytest.mark.parametrize("V,d", [(70001, 1024), (66003, 1029)])
+def test_gradient_beyond_the_caches(dyn, T, V, d):
+    """More than 256 MB of gradient: the rows without uses are stored another way."""
+    g = torch.Generator().manual_seed(T + V)
+    tokens = draw(T, V, "zipf", g).cuda()
+    dout = torch.randn(T, d, generator=g).cuda()
+    used, at = torch.unique(tokens, return_inverse=True)
+    ref = torch.zeros(len(used), d, dtype=torch.float64).index_add_(0, at.cpu(), dout.double().cpu()) * 0.75
+    mag = torch.zeros(len(used), d, dtype=torch.float64).index_add_(0, at.cpu(), dout.double().abs().cpu()) * 0.75
+    n = torch.bincount(at.cpu()).double()[:, None]
+    got = dyn.dynb_embed_backward(tokens, dout, V, scale=0.75, dtable=torch.full((V, d), float("nan"), device="cuda"))
+    within(got[used.long()], ref, stored(ref, (n + 1) * 2.0 ** -23 * mag, torch.float32))
+    unused = torch.ones(V, dtype=torch.bool, device="cuda")
+    unused[used.long()] = False
+    assert (got[unused] == 0).all()
+
+
 def test_what_is_not_finite_stays_in_its_row(dyn):
     tokens = torch.tensor([3, 1, 3, -1, 0, 9], dtype=torch.int32).cuda()
     dout = torch.ones(6, 64).cuda()
