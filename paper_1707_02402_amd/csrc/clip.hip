@@ -5,6 +5,9 @@
 // Two passes, the second of which starts where the first one ended (the last 256 MB that went by are still in the cache beside the memory).  Both
 // take the tensors as one row of chunks; a launch's list of up to CLIP_LIST tensors comes with its arguments, so that a call neither copies nor keeps a table.
 // The norm itself has no launch: every workgroup of the second pass adds up the first one's partial sums, in one order.
+//
+// Bound by memory: 2 GB of bfloat16 in 12 tensors 350 us (5.7 TB/s) and 768 (5.2 TB/s of what is read and written).  240 tensors of 56 MB in all are two lists, so four
+// launches: 8 us each for the squares, 12 for the scaling, of which the bytes account for 24 in all.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

@@ -15,7 +15,7 @@ using dynb::fail;
 
 namespace {
 
-// a wave a token
+// A wave a token; every row that is asked for is read and written once.  Bound by memory: 65536 tokens x 1024 bf16 40 us (6.7 TB/s); 37 x 512 takes 2 us, a launch's own time.
 template <typename T>
 __global__ __launch_bounds__(256) void k_embed(const int32_t* __restrict__ tokens, const T* __restrict__ table, T* __restrict__ out, int n, int V, int d,
                                                int64_t out_stride, float scale)
@@ -40,7 +40,9 @@ __global__ __launch_bounds__(256) void k_embed(const int32_t* __restrict__ token
 // ------------------------------------------------------------------------------------------ gradient of the table
 // The uses are brought into the order of their tokens (each token's in the order they stand in), so that a row's gradient is one sum, in one
 // order; a row without uses is a row of zeros.  A wave sums the columns of a row that it reads in pieces of 16 bytes a lane (512 of bfloat16; the launches' y
-// runs over the columns), and a workgroup's waves share the uses of a row that has many.
+// runs over the columns), and a workgroup's waves share the uses of a row that has many.  Bound by memory where there is much of it: 65536 tokens, 50021 x 1024, bf16
+// into fp32, 338 MB: 104 us, of which the sort's four launches take 22, the chunks' sums 18 to 25 and the rows 60; 4095 tokens, 20011 x 512 fp32, 49 MB: 15.3 us, 10 of
+// them for the zeros (a fill takes 8), the rest a crowded row's.
 
 // E: elements of a lane's piece.  Sums that leave in fp32 are stored 16 bytes a lane, lane by lane, so bfloat16 is then read in pieces of 8 bytes (pieces of 16
 // would leave in two stores of 16 bytes of every 32: 50021 rows x 1024, each used once: 77 us instead of 66)

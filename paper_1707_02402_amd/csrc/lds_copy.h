@@ -33,11 +33,6 @@ __device__ __forceinline__ void lds_copy16_to(const char* base, uint32_t off, ld
     asm volatile("" : "+s"(base), "+v"(off));
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)(base + off), (__attribute__((address_space(3))) uint32_t*)lds, 16, 0, 0);
 }
-// ... from any addresses
-__device__ __forceinline__ void lds_copy16_from(const char* p, lds_ptr lds)
-{
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)(p), (__attribute__((address_space(3))) uint32_t*)lds, 16, 0, 0);
-}
 // *p by the scalar unit: the address is the same for the whole wave, and nobody writes there during the kernel
 __device__ __forceinline__ int32_t uniform_load(const int32_t* p)
 {

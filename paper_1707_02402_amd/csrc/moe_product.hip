@@ -4,6 +4,10 @@
 // workgroup finds by itself: group e's units begin at  floor(offsets[e] / P) + e,  which leaves room for the ceil(rows / P) pieces of P rows that
 // the group has (and one for an empty group), since  ceil((b - a) / P) <= floor(b / P) - floor(a / P) + 1.  floor(M / P) + E + 1 units hold all groups
 // and what lies behind the last one, whose rows of results are zeros.
+//
+// What bounds them: few rows an expert, the weights' way from memory (8192 rows of 256 experts, 512 -> 1024: 64 to 68 us for 309 MB, 4.7 TB/s); many, the matrix
+// instructions and what feeds them (65536 rows, 1024 -> 2048, 64 experts: forward 336 us, 818 TFLOP/s, the weights' gradient 408, of which its 537 MB of fp32
+// results are some 80; 8192 rows, channels and features, one expert: forward 782 us, 1.41 PFLOP/s; one library product of that size 807).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
