@@ -443,7 +443,9 @@ __global__ __launch_bounds__(256) void k_embed_grad(const Range* __restrict__ ra
     using S = SumsTo<T, TG>;
     __shared__ float room[2][S::COLS];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int tile = int(blockIdx.x % unsigned(tiles)), v0 = int(blockIdx.x / unsigned(tiles)) * GRAD_ROWS, rows = min(GRAD_ROWS, V - v0);
+    // (very large tables: blockIdx.y goes on where x ends)
+    const int tile = int(blockIdx.x % unsigned(tiles)), v0 = int(blockIdx.y * (gridDim.x / unsigned(tiles)) + blockIdx.x / unsigned(tiles)) * GRAD_ROWS, rows = min(GRAD_ROWS, V - v0);
+    if (rows <= 0) return;
     const Range mine = ranges[v0 + min(lane, rows - 1)];
     const int k_mine = mine.end - mine.begin;
     // rows with few uses: neighbours a wave
@@ -595,8 +597,10 @@ extern "C" int dynb_embed_backward(const dynb_embed_shape* s, const int32_t* tok
         }
         float* const sums = reinterpret_cast<float*>(ws + L.sums);
         hipLaunchKernelGGL((k_embed_chunks<T>), dim3(unsigned((s->T + CHUNK - 1) / CHUNK), tiles), dim3(256), 0, st, keys, places, from, sums, ranges, s->T, s->V, s->d, dout_stride);
-        const unsigned groups = unsigned((s->V + GRAD_ROWS - 1) / GRAD_ROWS), grad_tiles = std::min(tiles, 0xffffffffu / 256u / groups);      // (threads of a launch)
-        hipLaunchKernelGGL((k_embed_grad<T, TG, PAST>), dim3(groups * grad_tiles), dim3(256), 0, st, ranges, places, from, sums, to, s->V, s->d, dout_stride, s->scale, int(grad_tiles));
+        // (an axis of a launch has room for fewer than 2^24 workgroups of 256 threads)
+        const unsigned groups = unsigned((s->V + GRAD_ROWS - 1) / GRAD_ROWS), wide = std::min(groups, (1u << 23) / tiles);
+        hipLaunchKernelGGL((k_embed_grad<T, TG, PAST>), dim3(wide * tiles, (groups + wide - 1) / wide), dim3(256), 0, st, ranges, places, from, sums, to, s->V, s->d, dout_stride, s->scale,
+                           int(tiles));
     };
     // Rows without uses are most of a large table.  Where the gradient is larger than the 256 MB behind the L2s, they are written past the caches, and what is read,
     // or will be, stays (8192 tokens, 128000 rows x 1024 in fp32, with the gradients' norm taken behind it: 427 us through them, 377 past them); a smaller one is

@@ -107,6 +107,25 @@ def test_gradient_beyond_the_caches(dyn, T, V, d):
     assert (got[unused] == 0).all()
 
 
+@pytest.mark.parametrize("T", [300, 9000])
+def test_gradient_of_the_most_rows(dyn, T):
+    """2^27 rows, more than a workgroup for every eight of them has room in a launch."""
+    V = 1 << 27
+    g = torch.Generator().manual_seed(T)
+    tokens = torch.randint(V, (T,), generator=g)
+    tokens[:3] = torch.tensor([0, V - 1, V // 2 + 77])
+    tokens[-100:] = tokens[5]
+    dout = torch.randn(T, 1, generator=g)
+    used, at = torch.unique(tokens, return_inverse=True)
+    ref = torch.zeros(len(used), 1, dtype=torch.float64).index_add_(0, at, dout.double())
+    mag = torch.zeros(len(used), 1, dtype=torch.float64).index_add_(0, at, dout.double().abs())
+    n = torch.bincount(at).double()[:, None]
+    got = dyn.dynb_embed_backward(tokens.int().cuda(), dout.cuda(), V, dtable=torch.full((V, 1), float("nan"), device="cuda"))
+    within(got[used.cuda()], ref, stored(ref, (n + 1) * 2.0 ** -23 * mag, torch.float32))
+    got[used.cuda()] = 0
+    assert not got.any()
+
+
 def test_what_is_not_finite_stays_in_its_row(dyn):
     tokens = torch.tensor([3, 1, 3, -1, 0, 9], dtype=torch.int32).cuda()
     dout = torch.ones(6, 64).cuda()
