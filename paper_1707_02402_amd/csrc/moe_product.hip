@@ -11,11 +11,9 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <initializer_list>
-#include <mutex>
-#include <set>
 #include <string>
-#include <utility>
 #include <type_traits>
 
 #include "device_utils.h"
@@ -1015,19 +1013,19 @@ using Kernel = void (*)(Args, int, int, int, Shares, float*);
 template <int DIR, class S>
 int launch_kernel(Kernel kernel, const Args& p, int64_t grid, int64_t units, int ct, int rt, const Shares& shares, float* partial, hipStream_t st, const char* who)
 {
-    // LDS beyond 64 KB has to be asked for; a kernel is asked for once on every device
-    static std::mutex lock;
-    static std::set<std::pair<int, Kernel>> asked;
-    {
-        int dev = 0;
-        hipError_t e = hipGetDevice(&dev);
-        std::lock_guard<std::mutex> guard(lock);
-        if (e == hipSuccess && !asked.count({dev, kernel})) {
-            e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, int(LDS_BYTES<DIR, S>));
-            if (e == hipSuccess) asked.insert({dev, kernel});
-        }
-        if (e != hipSuccess) return fail(DYNB_E_HIP, std::string(who) + ": " + hipGetErrorString(e));
+    // LDS beyond 64 KB has to be asked for; a kernel is asked for once on every device (beyond DEVICES and KERNELS, at every call)
+    constexpr int DEVICES = 64, KERNELS = 4;
+    static std::atomic<Kernel> asked[DEVICES][KERNELS];
+    int dev = 0, slot = 0;
+    hipError_t e = hipGetDevice(&dev);
+    std::atomic<Kernel>* const mine = asked[dev >= 0 && dev < DEVICES ? dev : 0];
+    while (slot < KERNELS && mine[slot].load() && mine[slot].load() != kernel) ++slot;
+    if (e == hipSuccess && (dev >= DEVICES || slot == KERNELS || !mine[slot].load())) {
+        e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, int(LDS_BYTES<DIR, S>));
+        Kernel none = nullptr;                                 // (two threads at once: one of them asks again at its next call)
+        if (e == hipSuccess && dev < DEVICES && slot < KERNELS) mine[slot].compare_exchange_strong(none, kernel);
     }
+    if (e != hipSuccess) return fail(DYNB_E_HIP, std::string(who) + ": " + hipGetErrorString(e));
     hipLaunchKernelGGL(kernel, dim3(unsigned(grid)), dim3(S::THREADS), (LDS_BYTES<DIR, S>), st, p, int(units), ct, rt, shares, partial);
     return launched(who);
 }
