@@ -562,6 +562,15 @@ def _new(stream, *shape, like, dtype=None):
     return t
 
 
+def _twin(stream, t):
+    """Another one (in half of _new's time)."""
+    import torch
+    t = torch.empty_like(t)
+    if stream is not None and stream != torch.cuda.current_stream():
+        t.record_stream(stream)
+    return t
+
+
 def _groups_struct(offsets, perm, k: int, M: int, rows: int) -> _Groups:
     import torch
     assert offsets.is_cuda and offsets.is_contiguous() and offsets.dtype == torch.int32
@@ -690,7 +699,8 @@ def dynb_layer_norm(x, gamma=None, beta=None, eps: float = 1e-5, out=None, want_
     if not want_stats:
         _check(lib.dynb_layer_norm(ct.byref(shape), x.data_ptr(), xs, _fp32(gamma, d), _fp32(beta, d), out.data_ptr(), ys, None, None, _stream(stream)))
         return out
-    mean, rstd = _new(stream, T, like=x, dtype=torch.float32), _new(stream, T, like=x, dtype=torch.float32)
+    mean = _new(stream, T, like=x, dtype=torch.float32)
+    rstd = _twin(stream, mean)
     _check(lib.dynb_layer_norm(ct.byref(shape), x.data_ptr(), xs, _fp32(gamma, d), _fp32(beta, d), out.data_ptr(), ys, mean.data_ptr(), rstd.data_ptr(),
                                _stream(stream)))
     return out, mean, rstd
@@ -709,12 +719,13 @@ def dynb_layer_norm_backward(dy, x, gamma, mean, rstd, dx=None, workspace=None, 
     if dx is None:
         dx = _new(stream, T, d, like=x)
     dxs = _rows(dx, T, d, x)
-    dgamma, dbeta = _new(stream, d, like=x, dtype=torch.float32), _new(stream, d, like=x, dtype=torch.float32)
+    dgamma = _new(stream, d, like=x, dtype=torch.float32)
+    dbeta = _twin(stream, dgamma)
     shape = _NormShape(T, d, _dtype_code(x), 0.0)
     if workspace is None:
         workspace = _scratch(lib.dynb_layer_norm_backward_workspace_bytes(ct.byref(shape)), x.device, stream)
     _check(lib.dynb_layer_norm_backward(ct.byref(shape), dy.data_ptr(), ds, x.data_ptr(), xs, _fp32(gamma, d), _fp32(mean, T), _fp32(rstd, T), dx.data_ptr(), dxs,
-                                        dgamma.data_ptr(), dbeta.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                                        dgamma.data_ptr(), dbeta.data_ptr(), workspace.data_ptr(), workspace.nbytes,
                                         _stream(stream)))
     return dx, dgamma, dbeta
 
