@@ -39,8 +39,8 @@ __global__ __launch_bounds__(256) void k_embed(const int32_t* __restrict__ token
 
 // ------------------------------------------------------------------------------------------ gradient of the table
 // The uses are brought into the order of their tokens (each token's in the order they stand in), so that a row's gradient is one sum, in one
-// order; a row without uses is a row of zeros.  A wave sums the columns of a row that it reads in pieces of 16 bytes a lane (512 of bfloat16; the launches' y
-// runs over the columns), and a workgroup's waves share the uses of a row that has many.  Bound by memory where there is much of it: 65536 tokens, 50021 x 1024, bf16
+// order; a row without uses is a row of zeros.  A wave sums the columns of a row that it reads in pieces of 16 bytes a lane (512 of bfloat16; others have
+// the further ones), and a workgroup's waves share the uses of a row that has many.  Bound by memory where there is much of it: 65536 tokens, 50021 x 1024, bf16
 // into fp32, 338 MB: 104 us, of which the sort's four launches take 22, the chunks' sums 18 to 25 and the rows 60; 4095 tokens, 20011 x 512 fp32, 49 MB: 15.3 us, 10 of
 // them for the zeros (a fill takes 8), the rest a crowded row's.
 
@@ -173,12 +173,13 @@ __device__ __forceinline__ int next_of(int from, int n, Is&& is)
 
 // Up to FEW tokens, one launch: every workgroup picks the uses of its rows (up to FEW_ROWS) from all tokens, whose 32 KB it reads in less than the launches of a
 // sort would take.
-// FEW_MANY: uses of a row from which all waves share them (4095 Zipf tokens, 20011 x 512: 1.9 us of 17 less than from 64).
+// Tiles of columns are neighbours in the launch, so that workgroups write one part of the table at a time (8192 Zipf tokens, 50021 x 1024 in fp32: 93 us with all
+// first tiles ahead of the second, 69 so).  FEW_MANY: uses of a row from which all waves share them (4095 Zipf tokens, 20011 x 512: 1.9 us of 17 less than from 64).
 constexpr int FEW = 8192, FEW_WAVES = 16, FEW_ROWS = 256, FEW_MANY = 24, FEW_STEPS = FEW / (FEW_WAVES * 64);
 
 template <typename T, typename TG, bool PAST>
 __global__ __launch_bounds__(FEW_WAVES * 64, 8) void k_embed_grad_few(const int32_t* __restrict__ tokens, const T* __restrict__ dout, TG* __restrict__ dtable, int n, int V, int d,
-                                                                      int64_t dout_stride, float scale, int rows_each)
+                                                                      int64_t dout_stride, float scale, int rows_each, int tiles)
 {
     __shared__ uint32_t uses[FEW];                             // place of the token * FEW_ROWS + row, in the tokens' order
     __shared__ int32_t found[FEW_WAVES], count[FEW_ROWS];
@@ -187,7 +188,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 8) void k_embed_grad_few(const int3
     constexpr int AHEAD = sizeof(T) == 2 ? 6 : 8;              // (what 64 registers hold; two rows more of bfloat16 spilled: 21.5 us for 18.4, 4095 tokens, 20011 x 512)
     __shared__ float room[FEW_WAVES / 2][S::COLS];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int v0 = int(blockIdx.x) * rows_each, rows = min(rows_each, V - v0);
+    const int tile = int(blockIdx.x % unsigned(tiles)), v0 = int(blockIdx.x / unsigned(tiles)) * rows_each, rows = min(rows_each, V - v0);
     constexpr uint32_t NONE = 0xffffffffu;
     if (threadIdx.x < FEW_ROWS) count[threadIdx.x] = 0;
     // wave w looks through its sixteenth of the tokens
@@ -225,7 +226,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 8) void k_embed_grad_few(const int3
         const int k = __builtin_amdgcn_readfirstlane(count[r]);
         if (k > FEW_MANY) continue;
         if (k == 0) {
-            for (int c = int(blockIdx.y) * S::COLS + lane * S::STEP / 64; c - lane * S::STEP / 64 < d; c += int(gridDim.y) * S::COLS)
+            for (int c = tile * S::COLS + lane * S::STEP / 64; c - lane * S::STEP / 64 < d; c += tiles * S::COLS)
                 S::template store_zeros<PAST>(dtable + size_t(v0 + r) * size_t(d), c, d);
             continue;
         }
@@ -237,7 +238,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 8) void k_embed_grad_few(const int3
             seen += __popcll(who);
         }
         wave_sync();
-        for (int c = int(blockIdx.y) * S::COLS + lane * S::STEP / 64; c - lane * S::STEP / 64 < d; c += int(gridDim.y) * S::COLS) {
+        for (int c = tile * S::COLS + lane * S::STEP / 64; c - lane * S::STEP / 64 < d; c += tiles * S::COLS) {
             S s;
             s.clear();
             s.template add<AHEAD>(dout, dout_stride, c, d, k, [&](int u) { return __builtin_amdgcn_readfirstlane(mine[wave][u]); });
@@ -250,7 +251,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 8) void k_embed_grad_few(const int3
     for (int r = -1;;) {
         r = next_of(r + 1, rows, [&](int i) { return count[i] > FEW_MANY; });
         if (r >= rows) break;
-        for (int c = int(blockIdx.y) * S::COLS + lane * S::STEP / 64; c - lane * S::STEP / 64 < d; c += int(gridDim.y) * S::COLS) {
+        for (int c = tile * S::COLS + lane * S::STEP / 64; c - lane * S::STEP / 64 < d; c += tiles * S::COLS) {
             S s;
             s.clear();
             for (int u = from; u < to; u += 64) {
@@ -431,8 +432,7 @@ __global__ __launch_bounds__(256) void k_embed_chunks(const uint32_t* __restrict
     }
 }
 
-// Tiles of columns are neighbours in the launch, so that the chip writes one part of the table at a time (50021 rows x 1024, 65536 tokens: 123 us with all rows'
-// first tiles ahead of the second, 106 so; workgroups of 8 rows: 105, of 4: 110).
+// Tiles of columns are neighbours here, too (65536 tokens: 123 us, 106 so; workgroups of 8 rows: 105, of 4: 110).
 constexpr int GRAD_ROWS = 8;                                   // rows of the table of a workgroup
 constexpr int MANY = 64;                                       // uses of a row that are one wave's (at least a chunk, so that more of them hold one's border)
 
@@ -591,8 +591,9 @@ extern "C" int dynb_embed_backward(const dynb_embed_shape* s, const int32_t* tok
             // two workgroups a CU, if the rows are not too many for that, nor too few (8192 tokens, 777 x 64: 42 us with 16 rows, 30 with 4; 512 tokens,
             // 2000 x 512: 6.9 with 8)
             const int rows = int(std::min<int64_t>(std::max<int64_t>((int64_t(s->V) * tiles + 511) / 512, 4), FEW_ROWS));
-            hipLaunchKernelGGL((k_embed_grad_few<T, TG, PAST>), dim3(unsigned((s->V + rows - 1) / rows), tiles), dim3(FEW_WAVES * 64), 0, st, tokens, from, to, s->T, s->V, s->d, dout_stride,
-                               s->scale, rows);
+            const unsigned groups = unsigned((s->V + rows - 1) / rows), few_tiles = std::min(tiles, std::max(1u, (1u << 22) / groups));      // (fewer than 2^32 threads)
+            hipLaunchKernelGGL((k_embed_grad_few<T, TG, PAST>), dim3(groups * few_tiles), dim3(FEW_WAVES * 64), 0, st, tokens, from, to, s->T, s->V, s->d, dout_stride, s->scale, rows,
+                               int(few_tiles));
             return;
         }
         float* const sums = reinterpret_cast<float*>(ws + L.sums);
