@@ -604,8 +604,8 @@ extern "C" int dynb_embed_backward(const dynb_embed_shape* s, const int32_t* tok
                            int(tiles));
     };
     // Rows without uses are most of a large table.  Where the gradient is larger than the 256 MB behind the L2s, they are written past the caches, and what is read,
-    // or will be, stays (8192 tokens, 128000 rows x 1024 in fp32, with the gradients' norm taken behind it: 427 us through them, 377 past them); a smaller one is
-    // left for the norm to find there (50021 rows: 126 us, 140 past them).
+    // or will be, stays (8192 tokens, 128000 rows x 1024 in fp32, with the gradients' norm taken behind it: 406 us through them, 355 past them); a smaller one is
+    // left for the norm to find there (50021 rows: 129 us, 138 past them).
     auto launch = [&](auto in, auto grad) {
         if (size_t(s->V) * size_t(s->d) * sizeof(grad) > size_t(256) << 20) launch_as(in, grad, std::true_type{});
         else launch_as(in, grad, std::false_type{});
