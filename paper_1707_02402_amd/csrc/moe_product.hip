@@ -657,16 +657,22 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
             // lanes of a store side by side: 16 bytes of every row a lane took the stores' address unit 64 clocks each, 8 us of a tile's 37 (forward, 1024 channels).
             if (nchunk > 0) meet();                            // (all waves are done with that chunk)
             const lds_ptr mine_at = lds + last + uint32_t(wave) * (BUF / S::WAVES / 16 * 16);
-            auto put = [&](auto* to, int64_t pitch) {          // to: row 0 of the tile, this wave's first column
+            // to: row 0 of the tile, this wave's first column.  A bfloat16 weights' gradient has `part` beside it: null, or where this tile's sums go in fp32 instead.
+            // Which of the two is asked anew for every piece that goes into LDS and comes out of it.  Asked once, with a way out each, it had 108 of the 256 x 256 kernel's
+            // registers spilled, and their loads waited for the next tile's requests (65536 rows, 1024 -> 2048: 64 experts 377 us, 345 so; 256 experts 721, 575).
+            auto put = [&](auto* to, float* part, int64_t pitch) {
                 using T = std::remove_pointer_t<decltype(to)>;
-                constexpr int P = 16 / int(sizeof(T)), LANES = FA * 32 / P, AT_ONCE = 64 / LANES, PITCH = FA * 32 * int(sizeof(T)) + 16;
-                static_assert(32 * PITCH <= int(BUF / S::WAVES), "room");
+                constexpr bool EITHER = DIR == GRAD_WEIGHT && sizeof(T) == 2;
+                constexpr int P = 16 / int(sizeof(T)), LANES = FA * 32 / P, AT_ONCE = 64 / LANES, PITCH = FA * 32 * int(sizeof(T)) + 16, PART_PITCH = FA * 32 * 4 + 16;
+                static_assert(32 * (EITHER ? PART_PITCH : PITCH) <= int(BUF / S::WAVES), "room");
+                const bool parts = EITHER && part;
+                const int size = parts ? 4 : int(sizeof(T)), in_pitch = parts ? PART_PITCH : PITCH;
                 const int col = lane % LANES * P, row = lane / LANES;
                 const bool on = now.c0 + cg * (FA * 32) + col < cols;
                 // (one address each, the steps are constants or scalars: an address a store was one too many to keep)
-                const lds_ptr in_at = mine_at + uint32_t(q * PITCH + 16 * hk * int(sizeof(T))), out_at = mine_at + uint32_t(row * PITCH + col * int(sizeof(T)));
-                char* lane_to = reinterpret_cast<char*>(to + int64_t(rg * 32 + row) * pitch + col);
-                const int64_t step = AT_ONCE * pitch * int(sizeof(T)), to_next = S::RG * 32 * pitch * int(sizeof(T));
+                const lds_ptr in_at = mine_at + uint32_t(q * in_pitch + 16 * hk * size), out_at = mine_at + uint32_t(row * in_pitch + col * size);
+                char* lane_to = (parts ? reinterpret_cast<char*>(part) : reinterpret_cast<char*>(to)) + (int64_t(rg * 32 + row) * pitch + col) * size;
+                const int64_t step = AT_ONCE * pitch * size, to_next = S::RG * 32 * pitch * size;
                 const char* act_at = nullptr;
                 int64_t act_step = 0, act_next = 0;
                 if constexpr (DIR == GRAD_INPUT && FUSED) {
@@ -687,13 +693,13 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
                             if (DIR == FORWARD && FUSED)
 #pragma unroll
                                 for (int i = 0; i < 8; ++i) v[i] = v[i] < 0.f ? 0.f : v[i];                  // (a NaN stays one)
-                            const lds_ptr at = in_at + (a * 32 + 8 * h) * int(sizeof(T));
                             using lds_u32x4 = __attribute__((address_space(3))) u32x4;
-                            if constexpr (sizeof(T) == 4) {
+                            if (sizeof(T) == 4 || parts) {
+                                const lds_ptr at = in_at + (a * 32 + 8 * h) * 4;
                                 *(lds_u32x4*)at = u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
                                 *(lds_u32x4*)(at + 16) = u32x4{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])};
                             } else
-                                *(lds_u32x4*)at = u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+                                *(lds_u32x4*)(in_at + (a * 32 + 8 * h) * 2) = u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
                         }
                         __builtin_amdgcn_sched_barrier(0);     // (all accumulators at once in other registers would have no room)
                     }
@@ -705,8 +711,35 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
 #pragma unroll
                         for (int i = 0; i < STORES; ++i) act[i] = act_ahead[b][i];
                     }
+                    auto take_out = [&](int at, int lds_pitch) {
 #pragma unroll
-                    for (int i = 0; i < STORES; ++i) v[i] = *(const __attribute__((address_space(3))) u32x4*)(out_at + i * AT_ONCE * PITCH);
+                        for (int i = 0; i < STORES; ++i) v[i] = *(const __attribute__((address_space(3))) u32x4*)(out_at + (i * AT_ONCE * lds_pitch + at));
+                    };
+                    const int left = now.rows - (b * S::RG + rg) * 32;
+                    if constexpr (EITHER) {
+                        if (parts) {                           // (which have rows, so chunks)
+#pragma unroll
+                            for (int h = 0; h < 32; h += 16) {                     // eight fp32 columns a lane, in two stores
+                                take_out(h, PART_PITCH);
+#pragma unroll
+                                for (int i = 0; i < STORES; ++i)
+                                    if (row + i * AT_ONCE < left && on) *reinterpret_cast<u32x4*>(lane_to + i * step + h) = v[i];
+                            }
+                        } else {
+                            take_out(0, PITCH);
+                            if (nchunk == 0)
+#pragma unroll
+                                for (int i = 0; i < STORES; ++i) v[i] = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+                            for (int i = 0; i < STORES; ++i)
+                                if (row + i * AT_ONCE < left && on) *reinterpret_cast<u32x4*>(lane_to + i * step) = v[i];
+                        }
+                        lane_to += to_next;
+                        wave_sync();
+                        __builtin_amdgcn_sched_barrier(0);
+                        continue;
+                    }
+                    take_out(0, PITCH);
                     if (nchunk == 0)
 #pragma unroll
                         for (int i = 0; i < STORES; ++i) v[i] = u32x4{0u, 0u, 0u, 0u};
@@ -717,7 +750,6 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
                                 v[i][j] = (__uint_as_float(act[i][j] << 16) > 0.f ? v[i][j] & 0xffffu : 0u) | (__uint_as_float(act[i][j] & 0xffff0000u) > 0.f ? v[i][j] & 0xffff0000u : 0u);
                         *reinterpret_cast<u32x4*>(lane_to + i * step) = v[i];
                     };
-                    const int left = now.rows - (b * S::RG + rg) * 32;
                     if (left >= 32 && now.c0 + cg * (FA * 32) + FA * 32 <= cols) {
                         if constexpr (DIR == GRAD_INPUT && FUSED && !ACT_AHEAD)
 #pragma unroll
@@ -740,10 +772,11 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
             const int first_col = now.c0 + cg * (FA * 32);
             if constexpr (DIR == GRAD_WEIGHT) {
                 const size_t row = size_t(now.r0) * size_t(p.K) + size_t(first_col), all = size_t(p.N) * size_t(p.K);
-                if constexpr (std::is_same_v<TO, float>) put((now.slot >= 0 ? partial + size_t(now.slot) * all : static_cast<float*>(p.out) + size_t(now.e) * all) + row, p.K);
-                else if (now.slot >= 0) put(partial + size_t(now.slot) * all + row, p.K);
-                else put(static_cast<TO*>(p.out) + size_t(now.e) * all + row, p.K);
-            } else put(static_cast<TO*>(p.out) + int64_t(now.begin) * p.out_stride + first_col, p.out_stride);
+                float* const part = now.slot >= 0 ? partial + size_t(now.slot) * all + row : nullptr;
+                TO* const to = static_cast<TO*>(p.out) + size_t(now.e) * all + row;
+                if constexpr (std::is_same_v<TO, float>) put(part ? part : to, nullptr, p.K);
+                else put(to, part, p.K);
+            } else put(static_cast<TO*>(p.out) + int64_t(now.begin) * p.out_stride + first_col, nullptr, p.out_stride);
             // (an end of its own for every size, so that the compiler keeps what is the same for all lanes in scalar registers)
             asm volatile("; %0" ::"n"(LIVE));
         };
