@@ -12,7 +12,8 @@ pytestmark = pytest.mark.skipif(not os.path.exists(OBJDUMP), reason="needs llvm-
 
 
 @pytest.mark.parametrize("name,variants", [("9k_productI", 16), ("13k_product_anyI", 4), ("6k_joinI", 2), ("7k_embedI", 2), ("16k_embed_grad_fewI", 8), ("12k_sort_count", 1),
-                                           ("12k_sort_place", 1), ("14k_embed_chunksI", 2), ("12k_embed_gradI", 8), ("14k_clip_squares", 1), ("12k_clip_scale", 1)])
+                                           ("12k_sort_place", 1), ("14k_embed_chunksI", 2), ("12k_embed_gradI", 8), ("14k_clip_squares", 1), ("12k_clip_scale", 1),
+                                           ("6k_normI", 15), ("11k_norm_gradI", 15), ("11k_norm_join", 1), ("11k_norm_longI", 2), ("14k_norm_dx_longI", 2), ("19k_norm_dparams_longI", 2)])
 def test_no_variant_has_scratch_memory(tmp_path, name, variants):
     found = {}
     for path in code_objects(tmp_path):
