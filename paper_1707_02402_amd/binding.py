@@ -185,10 +185,13 @@ def _check(rc: int):
 
 
 def _stream(stream=None):
-    if stream is None:                           # (current_stream() builds an object: 2.6 us, more than the smallest kernels take)
-        import torch
+    if stream is not None:
+        return ct.c_void_p(stream.cuda_stream)
+    import torch
+    try:                                         # current_stream() builds an object: 2.6 us, more than the smallest kernels take
         return ct.c_void_p(torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()))
-    return ct.c_void_p(stream.cuda_stream)
+    except AttributeError:                       # neither is torch's public interface: a torch without them is asked the slower way
+        return ct.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
 def _ptr(t):
