@@ -103,8 +103,8 @@ __global__ __launch_bounds__(256) void k_clip_squares(const List l, double* __re
     if (threadIdx.x == 0) partial[blockIdx.x] = add ? partial[blockIdx.x] + s : s;
 }
 
-template <typename T>
-__device__ __forceinline__ void scale(const T* p, T* to, int64_t left, float factor)
+template <typename T, typename F>
+__device__ __forceinline__ void scale(const T* p, T* to, int64_t left, F factor)
 {
     constexpr int P = PIECE<T>;
     u32x4 raw[CLIP_STEP];
@@ -114,7 +114,7 @@ __device__ __forceinline__ void scale(const T* p, T* to, int64_t left, float fac
         const int at = (i * 256 + int(threadIdx.x)) * P;
         float v[P];
 #pragma unroll
-        for (int j = 0; j < P; ++j) v[j] = element<T>(raw[i], j) * factor;
+        for (int j = 0; j < P; ++j) v[j] = float(F(element<T>(raw[i], j)) * factor);
         store_piece<P>(to + at, left >= CLIP_CHUNK / int64_t(sizeof(T)) ? P : int(left) - at, v);
     }
 }
@@ -128,14 +128,24 @@ __global__ __launch_bounds__(256) void k_clip_scale(const List l, const double* 
     if (blockIdx.x == 0 && threadIdx.x == 0) *norm = v;
     const bool down = v > max_norm && v < INFINITY;
     const float factor = down ? max_norm / v : 1.f;
+    // (a factor below fp32's normal range, of a norm above 10^37 or so, has lost digits, or all of them: fp64 then)
+    const bool tiny = factor < 0x1p-126f;
+    const double tiny_factor = double(max_norm) / double(v);
     for (uint32_t c = blockIdx.x; c < l.chunks; c += CLIP_GRID) {
         const uint32_t chunk = l.chunks - 1 - c;
         const int t = tensor_of(l, chunk);
         if (!l.out[t] || (!down && l.out[t] == l.grad[t])) continue;      // (nothing is wanted, or nothing changes)
         const bool bf = l.count[t] & 1;
         const int64_t at = int64_t(chunk - l.first[t]) * (CLIP_CHUNK / (bf ? 2 : 4)), left = (l.count[t] >> 1) - at;
-        if (bf) scale(static_cast<const bf16_t*>(l.grad[t]) + at, static_cast<bf16_t*>(l.out[t]) + at, left, factor);
-        else scale(static_cast<const float*>(l.grad[t]) + at, static_cast<float*>(l.out[t]) + at, left, factor);
+        auto scaled = [&](auto type) {
+            using T = decltype(type);
+            const T* const from = static_cast<const T*>(l.grad[t]) + at;
+            T* const to = static_cast<T*>(l.out[t]) + at;
+            if (tiny) scale(from, to, left, tiny_factor);
+            else scale(from, to, left, factor);
+        };
+        if (bf) scaled(bf16_t{});
+        else scaled(float{});
     }
 }
 
