@@ -242,9 +242,9 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
     // forward, input's gradient: unit = piece of rows * ct + column; a workgroup that stays takes every gridDim.x-th unit, by the list.
     // Up to SORTED groups and LIST units a workgroup, the units are the pieces that there are, those of more than half of a tile's rows first: rests of up to
     // 128 rows, which take half as long, even out what is left over (65536 rows, 64 experts by Zipf's law, 8 columns of tiles: 8.6 tiles' time a workgroup on average,
-    // 10 for the longest without, 9.1 so).  Beyond, find_piece's units.
+    // 10 for the longest without, 9.1 so).  Beyond, find_piece's units.  (All workgroups go by one numbering: it is the most units of any of them that decides.)
     int count = DIR == GRAD_WEIGHT ? 0 : STAYS ? (units - place + int(gridDim.x) - 1) / int(gridDim.x) : 1;
-    const bool sorted = DIR != GRAD_WEIGHT && STAYS && p.g.E < SORTED && count <= LIST;
+    const bool sorted = DIR != GRAD_WEIGHT && STAYS && p.g.E < SORTED && (units + int(gridDim.x) - 1) / int(gridDim.x) <= LIST;
     int at_unit = -1;
     // weights' gradient: a lane's groups
     const int w_lane = place / (ct * rt);

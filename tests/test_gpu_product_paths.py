@@ -3,6 +3,8 @@ import numpy as np
 import pytest
 import torch
 
+from tests.operator_util import stored
+
 pytestmark = pytest.mark.gpu
 BF = torch.bfloat16
 
@@ -35,3 +37,46 @@ def test_a_bfloat16_gradient_is_the_fp32_gradient_rounded_once(dyn, M, K, N, E, 
     narrow = dyn.moe_product_grad_weight(dout, x, off, dW=torch.full((E, N, K), float("nan"), dtype=BF, device="cuda"), **how)
     assert torch.isfinite(wide).all()
     assert torch.equal(narrow, wide.to(BF))
+
+
+def uneven(M, E, seed):
+    """Loads from nothing to some hundred rows, and rows behind the last group."""
+    r = np.random.Generator(np.random.Philox(key=[M + seed, E]))
+    share = np.where((r.random(E) < 0.1) & (np.arange(E) > 0), 0.0, r.random(E) + 0.2)
+    counts = np.bincount(r.choice(E, M - M // 50, p=share / share.sum()), minlength=E)
+    return np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+
+
+# 256 workgroups that stay look their tiles up 256 at a time: 8192 groups and more are never sorted, nor are more than 256 tiles a workgroup, which are looked up
+# anew after every 256 (840000 rows: 164 of the workgroups have 257 and the others 256, and all have to go by the same numbering)
+@pytest.mark.parametrize("M,K,N,E", [(840_000, 64, 5120, 3), (900_000, 64, 5120, 3), (838_000, 64, 5120, 3), (1_700_000, 64, 1280, 8192), (1_600_000, 128, 64, 8200)])
+def test_tiles_that_are_looked_up_as_they_come(dyn, M, K, N, E):
+    g = torch.Generator("cuda").manual_seed(E)
+    at = uneven(M, E, 1)
+    off = torch.from_numpy(at).cuda()
+    W = torch.randn(E, N, K, generator=g, device="cuda").mul_(K ** -0.5).to(BF)
+    x = torch.randn((M + 1) // 2, K, generator=g, device="cuda").to(BF)
+    perm = torch.randperm(M, generator=g, device="cuda").int()
+
+    def check(got, rows_of, relu):
+        """Every group's rows, 32768 at a time, against a product of its own."""
+        assert torch.isfinite(got).all() and not got[at[-1]:].any()
+        for e in range(E):
+            w = W[e].double().t().contiguous() if at[e + 1] > at[e] else None
+            for lo in range(at[e], at[e + 1], 32768):
+                rows, hi = rows_of(lo, min(at[e + 1], lo + 32768)), min(at[e + 1], lo + 32768)
+                ref = (rows @ w).clamp(min=0) if relu else rows @ w
+                wrong.append(((got[lo:hi].double() - ref).abs() > stored(ref, K * 2.0 ** -23 * (rows.abs() @ w.abs()), BF)).any())
+
+    wrong = []
+    out = torch.full((M, N), float("nan"), dtype=BF, device="cuda")
+    dyn.moe_product(x, W, off, perm=perm, k=2, relu=True, out=out)
+    check(out, lambda lo, hi: x[perm[lo:hi].long() // 2].double(), True)
+    del out
+    # the input's gradient of the turned layer: N channels into K features
+    V = W.transpose(1, 2).contiguous()                           # [E][K][N]
+    dout = torch.randn(M, K, generator=g, device="cuda").to(BF)
+    din = torch.full((M, N), float("nan"), dtype=BF, device="cuda")
+    dyn.moe_product_grad_input(dout, V, off, out=din)
+    check(din, lambda lo, hi: dout[lo:hi].double(), False)
+    assert int(torch.stack(wrong).sum()) == 0
