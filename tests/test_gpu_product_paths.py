@@ -80,3 +80,36 @@ def test_tiles_that_are_looked_up_as_they_come(dyn, M, K, N, E):
     dyn.moe_product_grad_input(dout, V, off, out=din)
     check(din, lambda lo, hi: dout[lo:hi].double(), False)
     assert int(torch.stack(wrong).sum()) == 0
+
+
+def agrees(got, ref, err):
+    """Results stored in bfloat16, on the device: within `err` of ref before they were rounded (operator_util.stored)."""
+    return bool(((got.double() - ref).abs() <= stored(ref, err, got.dtype)).all())
+
+
+@pytest.mark.parametrize("M,K,N,E", [(300, 64, 72, 2047), (300, 64, 72, 2048), (300, 64, 64, 5000), (9000, 40, 64, 5000), (300, 63, 65, 5000), (700, 32, 16, 70000), (700, 31, 17, 70000), (90000, 16, 24, 20000)])
+def test_groups_by_the_thousand(dyn, M, K, N, E):
+    """Rows find their groups in several steps of a search, and fewer rows than groups."""
+    g = torch.Generator("cuda").manual_seed(E + K)
+    at = uneven(M, E, 2)
+    off = torch.from_numpy(at).cuda()
+    live, used = int(at[-1]), torch.from_numpy(np.searchsorted(at, np.arange(M), side="right") - 1).cuda()
+    W = torch.randn(E, N, K, generator=g, device="cuda").mul_(K ** -0.5).to(BF)
+    x, dout = torch.randn(M, K, generator=g, device="cuda").to(BF), torch.randn(M, N, generator=g, device="cuda").to(BF)
+    out = dyn.moe_product(x, W, off, out=torch.full((M, N), float("nan"), dtype=BF, device="cuda"))
+    din = dyn.moe_product_grad_input(dout, W, off, out=torch.full((M, K), float("nan"), dtype=BF, device="cuda"))
+    assert not out[live:].any() and not din[live:].any()
+    for lo in range(0, live, 3000):
+        hi = min(live, lo + 3000)
+        w, xs, ds = W[used[lo:hi]].double(), x[lo:hi].double(), dout[lo:hi].double()
+        assert agrees(out[lo:hi], (w * xs[:, None, :]).sum(2), K * 2.0 ** -23 * (w * xs[:, None, :]).abs().sum(2)), (lo, hi)
+        assert agrees(din[lo:hi], (w * ds[:, :, None]).sum(1), N * 2.0 ** -23 * (w * ds[:, :, None]).abs().sum(1)), (lo, hi)
+    ref, mag = torch.zeros(E, N * K, dtype=torch.float64, device="cuda"), torch.zeros(E, N * K, dtype=torch.float64, device="cuda")
+    for lo in range(0, live, 3000):
+        hi = min(live, lo + 3000)
+        outer = (dout[lo:hi].double()[:, :, None] * x[lo:hi].double()[:, None, :]).flatten(1)
+        ref.index_add_(0, used[lo:hi], outer)
+        mag.index_add_(0, used[lo:hi], outer.abs())
+    longest = int(np.diff(at).max())
+    dW = dyn.moe_product_grad_weight(dout, x, off, dW=torch.full((E, N, K), float("nan"), device="cuda"))
+    assert agrees(dW.view(E, -1), ref, longest * 2.0 ** -23 * mag)
