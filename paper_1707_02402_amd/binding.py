@@ -198,14 +198,27 @@ def _ptr(t):
     return None if t is None else ct.c_void_p(t.data_ptr())
 
 
-def _scratch(nbytes: int, device, stream):
-    """Device buffer the binding allocates on the caller's behalf.  If the work runs on another stream than
-    the current one, the allocator is told so: it must not hand the block out again before that work is done."""
+def _made(stream, make):
+    """make() for work on `stream` (None: the current one).  Memory that torch hands out may still be in use by earlier work of the
+    stream it is handed out on, so it has to be the stream that the work runs on; the current one, where the caller goes on with a
+    result, is made known, so that the block is not handed out again ahead of the work there."""
+    if stream is None:
+        return make()
     import torch
-    t = torch.empty(max(int(nbytes), 1), dtype=torch.uint8, device=device)
-    if stream is not None and stream != torch.cuda.current_stream():
-        t.record_stream(stream)
-    return t
+    current = torch.cuda.current_stream()
+    if stream == current:
+        return make()
+    with torch.cuda.stream(stream):
+        made = make()
+    for t in made if isinstance(made, (tuple, list)) else (made,):
+        t.record_stream(current)
+    return made
+
+
+def _scratch(nbytes: int, device, stream):
+    """Device buffer the binding allocates on the caller's behalf."""
+    import torch
+    return _made(stream, lambda: torch.empty(max(int(nbytes), 1), dtype=torch.uint8, device=device))
 
 
 # ------------------------------------------------------------------------------------------ planner
@@ -330,8 +343,7 @@ def dynbatch_pack_weights(weights: dict, C: int, H: int, W: int, dtype: int, pac
     n_types = int(weights["w3a"].shape[0])
     shape = _Shape(C, H, W, dtype)
     if packed is None:
-        packed = torch.empty(max(int(lib.dynbatch_packed_weights_bytes(ct.byref(shape), n_types)), 256),
-                             dtype=torch.uint8, device=weights["w3a"].device)
+        packed = _scratch(max(int(lib.dynbatch_packed_weights_bytes(ct.byref(shape), n_types)), 256), weights["w3a"].device, stream)
     w = _weights_struct({**weights, "packed": None})
     _check(lib.dynbatch_pack_weights(ct.byref(shape), n_types, ct.byref(w), _ptr(packed),
                                      packed.numel() * packed.element_size(), _stream(stream)))
@@ -352,9 +364,7 @@ def dynbatch_execute(plan: Plan, weights: dict, feats, out=None, workspace=None,
         t = weights.get(key)
         assert t is None or (t.is_cuda and t.is_contiguous() and t.dtype == torch.float32), key
     if out is None:
-        out = torch.empty_like(feats)
-        if stream is not None and stream != torch.cuda.current_stream():
-            out.record_stream(stream)
+        out = _made(stream, lambda: torch.empty_like(feats))
     assert out.is_cuda and out.is_contiguous() and out.shape == feats.shape and out.dtype == feats.dtype
     if workspace is None:
         workspace = _scratch(lib.dynbatch_workspace_bytes(plan.handle, ct.byref(shape)), feats.device, stream)
@@ -386,15 +396,12 @@ def dynbatch_backward(plan: Plan, weights: dict, feats, out, forward_workspace, 
     import torch
     shape = _shape_of(feats)
     assert dout.is_cuda and dout.is_contiguous() and dout.dtype == torch.float32 and dout.shape == feats.shape
-    f32 = lambda t: torch.empty(t.shape, dtype=torch.float32, device=feats.device)
+    f32 = lambda *shape: _made(stream, lambda: torch.empty(shape, dtype=torch.float32, device=feats.device))
     C = shape.C
     n_types = weights["w3a"].shape[0]
     g = grads if grads is not None else dict(
-        dfeats=f32(feats), dw3a=f32(weights["w3a"]), dw3b=f32(weights["w3b"]),
-        db3a=torch.empty((n_types, C), dtype=torch.float32, device=feats.device),
-        db3b=torch.empty((n_types, C), dtype=torch.float32, device=feats.device),
-        dw1=torch.empty((n_types, C, 2 * C), dtype=torch.float32, device=feats.device),
-        db1=torch.empty((n_types, C), dtype=torch.float32, device=feats.device))
+        dfeats=f32(*feats.shape), dw3a=f32(*weights["w3a"].shape), dw3b=f32(*weights["w3b"].shape), db3a=f32(n_types, C),
+        db3b=f32(n_types, C), dw1=f32(n_types, C, 2 * C), db1=f32(n_types, C))
     for k in ("dfeats", "dw1", "db1", "dw3a", "db3a", "dw3b", "db3b"):
         assert g[k].is_cuda and g[k].is_contiguous() and g[k].dtype == torch.float32
     if workspace is None:
@@ -437,9 +444,10 @@ def dynbatch_classify(roots, head: dict, probs=None, want_logits: bool = False, 
         assert t is None or (t.is_cuda and t.is_contiguous() and t.dtype == torch.float32), key
     shape = _head_shape(roots, head)
     B, A = roots.shape[0], shape.n_answers
+    rows = lambda: _made(stream, lambda: torch.empty((B, A), dtype=torch.float32, device=roots.device))
     if probs is None:
-        probs = torch.empty((B, A), dtype=torch.float32, device=roots.device)
-    logits = torch.empty((B, A), dtype=torch.float32, device=roots.device) if want_logits else None
+        probs = rows()
+    logits = rows() if want_logits else None
     if workspace is None:
         workspace = _scratch(lib.dynbatch_classify_workspace_bytes(ct.byref(shape), B), roots.device, stream)
     w = _HeadWeights(*[(head.get(k).data_ptr() if head.get(k) is not None else None) for k in ("wc", "bc", "wf1", "bf1", "wf2", "bf2")])
@@ -488,11 +496,8 @@ def moe_forward(x, Wg, Wn, noise, W1, W2, k: int, out=None, want_aux: bool = Fal
     assert noise is None or (noise.is_cuda and noise.is_contiguous() and noise.dtype == torch.float32
                              and noise.shape == (T, E))
     shape = _MoeShape(T, d, h, E, k, DYNB_BF16, flags)
-    side = stream is not None and stream != torch.cuda.current_stream()
     if out is None:
-        out = torch.empty_like(x)
-        if side:
-            out.record_stream(stream)
+        out = _made(stream, lambda: torch.empty_like(x))
     if workspace is None:
         n = int(lib.moe_workspace_bytes(ct.byref(shape)))
         if n == 0:
@@ -500,20 +505,12 @@ def moe_forward(x, Wg, Wn, noise, W1, W2, k: int, out=None, want_aux: bool = Fal
         workspace = _scratch(n, x.device, stream)
     aux_t, aux_c = None, None
     if want_aux:
-        dev = x.device
-        aux_t = SimpleNamespace(
-            logits=torch.empty((T, E), dtype=torch.float32, device=dev),
-            topk_idx=torch.empty((T, k), dtype=torch.int32, device=dev),
-            topk_w=torch.empty((T, k), dtype=torch.float32, device=dev),
-            counts=torch.empty(E, dtype=torch.int32, device=dev),
-            offsets=torch.empty(E + 1, dtype=torch.int32, device=dev),
-            perm=torch.empty(T * k, dtype=torch.int32, device=dev),
-            inv=torch.empty(T * k, dtype=torch.int32, device=dev))
-        if side:
-            for t_ in vars(aux_t).values():
-                t_.record_stream(stream)
-        aux_c = _MoeAux(*[getattr(aux_t, n).data_ptr() for n in
-                          ("logits", "topk_idx", "topk_w", "counts", "offsets", "perm", "inv")])
+        names = ("logits", "topk_idx", "topk_w", "counts", "offsets", "perm", "inv")
+        sizes = ((T, E), (T, k), (T, k), (E,), (E + 1,), (T * k,), (T * k,))
+        aux_t = SimpleNamespace(**dict(zip(names, _made(stream, lambda: [
+            torch.empty(size, dtype=torch.float32 if name in ("logits", "topk_w") else torch.int32, device=x.device)
+            for name, size in zip(names, sizes)]))))
+        aux_c = _MoeAux(*[getattr(aux_t, n).data_ptr() for n in names])
     args = (ct.byref(shape), _ptr(x), _ptr(Wg), _ptr(Wn), _ptr(noise), _ptr(W1), _ptr(W2), _ptr(out),
             ct.byref(aux_c) if aux_c is not None else None, _ptr(workspace),
             workspace.numel() * workspace.element_size(), _stream(stream))
@@ -557,21 +554,17 @@ def _rows(t, n: int, width: int, like=None) -> int:
 
 
 def _new(stream, *shape, like, dtype=None):
-    """An uninitialised result; where the work runs on another stream than the current one, the allocator is told."""
+    """An uninitialised result."""
     import torch
-    t = torch.empty(shape, dtype=dtype if dtype is not None else like.dtype, device=like.device)
-    if stream is not None and stream != torch.cuda.current_stream():
-        t.record_stream(stream)
-    return t
+    if stream is None:                           # (the usual case, without the detour)
+        return torch.empty(shape, dtype=dtype if dtype is not None else like.dtype, device=like.device)
+    return _made(stream, lambda: torch.empty(shape, dtype=dtype if dtype is not None else like.dtype, device=like.device))
 
 
 def _twin(stream, t):
     """Another one (in half of _new's time)."""
     import torch
-    t = torch.empty_like(t)
-    if stream is not None and stream != torch.cuda.current_stream():
-        t.record_stream(stream)
-    return t
+    return torch.empty_like(t) if stream is None else _made(stream, lambda: torch.empty_like(t))
 
 
 def _groups_struct(offsets, perm, k: int, M: int, rows: int) -> _Groups:
@@ -758,9 +751,7 @@ def dynb_clip_gradients(grads, max_norm: float, norm=None, workspace=None, strea
     t = grads if isinstance(grads, GradTensors) else GradTensors(grads)
     device = t.grads[0].device if t.grads else torch.device("cuda", torch.cuda.current_device())
     if norm is None:
-        norm = torch.empty((), dtype=torch.float32, device=device)
-        if stream is not None and stream != torch.cuda.current_stream():
-            norm.record_stream(stream)
+        norm = _made(stream, lambda: torch.empty((), dtype=torch.float32, device=device))
     assert norm.is_cuda and norm.dtype == torch.float32 and norm.numel() == 1
     if workspace is None:
         workspace = _scratch(lib.dynb_clip_workspace_bytes(), device, stream)
