@@ -558,7 +558,8 @@ int dynb_layer_norm_backward(const dynb_norm_shape* shape, const void* dy, int64
  * caller to see, who will want to leave the step out.)  The squares are added up in fp64.        */
 typedef struct {
     const void* grad;         /* device [count] dtype, dense                                     */
-    void* out;                /* device [count] dtype: grad itself or a tensor that overlaps with none; NULL: the tensor counts for the
+    void* out;                /* device [count] dtype: grad itself or a tensor that overlaps with none, nor with another's out (a
+                                 gradient that is to be scaled in place stands in the list once); NULL: the tensor counts for the
                                  norm only                                                       */
     int64_t count;            /* elements; 0: nothing                                            */
     int32_t dtype;            /* DYNB_F32 or DYNB_BF16                                           */

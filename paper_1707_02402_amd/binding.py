@@ -729,7 +729,8 @@ def dynb_layer_norm_backward(dy, x, gamma, mean, rstd, dx=None, workspace=None, 
 # ------------------------------------------------------------------------------------------ clipping
 class GradTensors:
     """A network's gradient tensors (device, contiguous, float32 or bfloat16) and where the clipped ones go (None: into the gradients
-    themselves), marshalled once for the steps in which they stay where they are.  Keeps the tensors alive."""
+    themselves), marshalled once for the steps in which they stay where they are.  Keeps the tensors alive.  No two results may share
+    memory: a gradient that several names stand for is listed once."""
 
     def __init__(self, grads, out=None):
         self.grads = list(grads)
@@ -737,7 +738,10 @@ class GradTensors:
         assert len(self.grads) == len(self.out)
         for g, o in zip(self.grads, self.out):
             assert g.is_cuda and g.is_contiguous() and o.is_cuda and o.is_contiguous() and o.dtype == g.dtype and o.numel() == g.numel()
-        self.array = (_GradTensor * max(len(self.grads), 1))(*[(g.data_ptr(), o.data_ptr(), g.numel(), _dtype_code(g)) for g, o in zip(self.grads, self.out)])
+        listed = [(g.data_ptr(), o.data_ptr(), g.numel(), _dtype_code(g)) for g, o in zip(self.grads, self.out)]
+        places = [t[1] for t in listed if t[2]]
+        assert len(set(places)) == len(places), "two results at one place"
+        self.array = (_GradTensor * max(len(self.grads), 1))(*listed)
 
 
 def dynb_clip_workspace_bytes() -> int:
