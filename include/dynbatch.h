@@ -491,8 +491,8 @@ typedef struct {
  *   in    [M or groups->rows][K] bf16     W [E][N][K] bf16, dense     out, dout [M][N] bf16
  *   act, din [M][K] bf16                  dW [E][N][K] grad_dtype (DYNB_F32 or DYNB_BF16), dense
  * Results may not overlap with what is read.  Any sizes and addresses are accepted; K and N that are multiples of 8 with
- * rows on 16-byte borders, at most 2^22 elements apart and (gathered ones) within 4 GB, are copied straight into LDS, others by way of registers.  Nothing is read back and nothing waits on the host.  Sums are in a fixed order: equal calls
- * give equal bits.
+ * rows on 16-byte borders, at most 2^22 elements apart and (gathered ones) within 4 GB, are copied straight into LDS, others by way of registers, which
+ * takes two to four times as long.  Nothing is read back and nothing waits on the host.  Sums are in a fixed order: equal calls give equal bits.
  * Errors: DYNB_E_INVAL (NULL, sizes <= 0, strides below a row's length, misaligned), DYNB_E_UNSUPPORTED (dtype, flag, more
  * than 2^30 rows, 2^22 channels, 2^20 experts or 2^24 tiles of results), DYNB_E_WORKSPACE, DYNB_E_HIP.  */
 int moe_product(const moe_product_shape* shape, const moe_groups* groups, const void* in, int64_t in_stride,
@@ -523,7 +523,7 @@ int dynb_embed(const dynb_embed_shape* shape, const int32_t* tokens, const void*
                void* stream);
 /*   dout device [T][d] dtype, rows dout_stride elements apart; dtable device [V][d] grad_dtype (DYNB_F32 or DYNB_BF16), dense: every
  *   row is written; workspace device, >= dynb_embed_backward_workspace_bytes, 256-byte aligned, scratch.
- * A row's sum runs over its tokens in their order, in pieces whose borders depend on the tokens only: equal calls give equal bits.
+ * A row's sum runs over its tokens in their order, in pieces whose borders depend on the tokens and the shape only: equal calls give equal bits.
  * Errors as dynb_embed, and DYNB_E_WORKSPACE.                                                    */
 size_t dynb_embed_backward_workspace_bytes(const dynb_embed_shape* shape);
 int dynb_embed_backward(const dynb_embed_shape* shape, const int32_t* tokens, const void* dout, int64_t dout_stride,

@@ -16,6 +16,7 @@ using dynb::fail;
 namespace {
 
 // A wave a token; every row that is asked for is read and written once.  Bound by memory: 65536 tokens x 1024 bf16 40 us (6.7 TB/s); 37 x 512 takes 2 us, a launch's own time.
+// Narrow rows leave lanes idle and are bound by the waves: 65536 x 128 bf16 12 us (2.9 TB/s), 65536 x 64 10 (1.8).
 template <typename T>
 __global__ __launch_bounds__(256) void k_embed(const int32_t* __restrict__ tokens, const T* __restrict__ table, T* __restrict__ out, int n, int V, int d,
                                                int64_t out_stride, float scale)
@@ -175,6 +176,8 @@ __device__ __forceinline__ int next_of(int from, int n, Is&& is)
 // sort would take.
 // Tiles of columns are neighbours in the launch, so that workgroups write one part of the table at a time (8192 Zipf tokens, 50021 x 1024 in fp32: 93 us with all
 // first tiles ahead of the second, 69 so).  FEW_MANY: uses of a row from which all waves share them (4095 Zipf tokens, 20011 x 512: 1.9 us of 17 less than from 64).
+// A row's uses are one workgroup's for a tile of columns, however many there are: 8192 tokens, bf16 into fp32, 1024 wide, take 147 us over 2 rows, and 109 over 50021
+// rows with 60 % of them on one token, which the sort of one token more does in 25 and 52.  (Zipf's law over 50021 rows: 41 us, and 54 by the sort.)
 constexpr int FEW = 8192, FEW_WAVES = 16, FEW_ROWS = 256, FEW_MANY = 24, FEW_STEPS = FEW / (FEW_WAVES * 64);
 
 template <typename T, typename TG, bool PAST>

@@ -6,8 +6,10 @@
 // and what lies behind the last one, whose rows of results are zeros.
 //
 // What bounds them: few rows an expert, the weights' way from memory (8192 rows of 256 experts, 512 -> 1024: 64 to 68 us for 309 MB, 4.7 TB/s); many, the matrix
-// instructions and what feeds them (65536 rows, 1024 -> 2048, 64 experts: forward 336 us, 818 TFLOP/s, the weights' gradient 408, of which its 537 MB of fp32
-// results are some 80; 8192 rows, channels and features, one expert: forward 782 us, 1.41 PFLOP/s; one library product of that size 807).
+// instructions and what feeds them (65536 rows, 1024 -> 2048, 64 experts: forward 336 us, 818 TFLOP/s, the weights' gradient 408, 361 into bfloat16;
+// 8192 rows, channels and features, one expert: forward 782 us, 1.41 PFLOP/s; one library product of that size 807).  Sums as short as 1024 pay for their tiles'
+// ends: with even loads the time is 1.73 us for each chunk of 64 places of a workgroup's tile, 1.24 PFLOP/s, and 9 us for every tile, in which its results leave
+// and nothing is multiplied (the weights' gradient into fp32: 13 us); uneven loads by Zipf's law with exponent 0.6 add 14 % (the weights' gradient: 20 %).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -795,7 +797,9 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
 
 // ------------------------------------------------------------------------------------------ any size, stride and address
 // Mid's tiles and its places in LDS, by way of registers: pieces of 16 bytes are loaded from wherever they lie (rows of odd length lie between the borders that a copy
-// straight into LDS keeps to), the last of a row element by element, a chunk ahead.
+// straight into LDS keeps to), the last of a row element by element, a chunk ahead.  65536 rows, 1001 -> 1501, one expert: 465 us forward, 485 the input's
+// gradient, 855 the weights', where 1000 -> 1504 takes 231, 207 and 241 through k_product, whose tiles
+// of 256 x 256 read either operand half as often and have their next chunk on its way without registers (what share each has was not taken apart).
 template <int DIR, typename TO>
 __global__ __launch_bounds__(256, 2) void k_product_any(Args p, int units, int ct, int rt, Shares shares, float* __restrict__ partial)
 {
@@ -1019,8 +1023,9 @@ bool on_16(std::initializer_list<const void*> pointers)
 // Few: rows that leave most of a larger tile empty, or too few tiles of 128 x 128 for the chip.  Big: where its tiles are many and long enough.  us, forward / the
 // input's gradient, by rows, K, N, experts, Zipf exponent:
 //                                   Big          Mid          Few
-//   74 x 512 x 1024, 256, 1.1       18 / 24      18 / 16      13 / 13
-//   1000 x 1024 x 1024, 8, 0.5      27 / 27      14 / 14      11 / 10
+//   16 x 2048 x 512, 1              30 / 13      15 / 7       13 / 8
+//   74 x 512 x 1024, 256, 1.1       18 / 24      10 / 14      10 / 10
+//   1000 x 1024 x 1024, 8, 0.5      27 / 26      14 / 13      10 / 10
 //   3000 x 2048 x 2048, 1           47 / 45      29 / 29      34 / 36
 //   4096 x 2048 x 1024, 16, 0.6     49 / 35      28 / 31      35 / 34
 //   8192 x 512 x 1024, 256, 1.1     81 / 88      56 / 57      52 / 53
@@ -1034,6 +1039,7 @@ bool on_16(std::initializer_list<const void*> pointers)
 //   65536 x 1024 x 2048, 256, 0.6  421 / 390    434 / 411    506 / 484
 //   65536 x 1024 x 2048, 512, 0.6  606 / 579    562 / 554    614 / 627
 //   8192 x 8192 x 8192, 1          782 / 768   1319 / 1402  2367 / 2516
+// (16 rows of one group: four workgroups, 32 chunks one after the other, so the latency of memory; the sum is not shared out)
 enum KindOf { BIG, MID, FEW };
 KindOf kind_of(const moe_product_shape* s, int cols, int depth)
 {
@@ -1099,8 +1105,9 @@ struct WeightPlan {
 WeightPlan weight_plan(const moe_product_shape* s, bool fast)
 {
     WeightPlan w = {};
-    // us, Big / Mid, by rows, K, N, experts: 65536 x 1024 x 2048, 64 421 / 480, 256 756 / 890; 65536 x 512 x 1024, 64 134 / 139; 65536 x 512 x 512, 64 92 / 60;
-    // 8192 x 4096 x 4096, 1 240 / 267; 3000 x 2048 x 2048, 1 52 / 44; 16384 x 512 x 1024, 256 160 / 157; 74 x 512 x 1024, 256 109 / 100
+    // us, Big / Mid, into fp32 and into bfloat16, by rows, K, N, experts: 65536 x 1024 x 2048, 64 398 / 479 and 357 / 413, 256 764 / 893 and 582 / 673;
+    // 65536 x 512 x 1024, 64 139 / 145 and 129 / 130; 65536 x 512 x 512, 64 94 / 63 and 74 / 63; 8192 x 4096 x 4096, 1 222 / 257 and 218 / 253;
+    // 3000 x 2048 x 2048, 1 54 / 45 and 55 / 46; 16384 x 512 x 1024, 256 165 / 160 and 133 / 134; 74 x 512 x 1024, 256 108 / 102 and 61 / 52
     w.big = fast && int64_t(s->M) / 64 * ((s->K + 255) / 256) * ((s->N + 255) / 256) >= 8192;
     const int side = w.big ? 256 : 128, slots = w.big ? CUS : 2 * CUS;
     w.ct = (s->K + side - 1) / side;

@@ -17,7 +17,9 @@ namespace {
 
 // A lane keeps up to 16 elements of a row, so that it is read once: the mean, then the squares of what differs from it, from registers.  Rows of up to
 // 1024 elements are a wave's each, up to 16384 a workgroup's of 4 or 16 waves.  Longer ones are read three times (k_norm_long and its like).
-// Bound by memory: a row in, a row out, no more.  65536 x 1024 bf16 51 us (5.3 TB/s; a large copy here 4.8), fp32 96 (5.6); 37 x 512 takes 2.7 us, a launch's own time.
+// Bound by memory where rows fill their lanes: a row in, a row out, no more.  65536 x 1024 bf16 51 us (5.3 TB/s; a large copy here 4.8), fp32 96 (5.6); 37 x 512
+// takes 3.4 us, a launch's own time.  Narrower rows have a wave each all the same, most of whose lanes have nothing to do, and are bound by the waves:
+// 65536 x 256 bf16 27 us (2.5 TB/s), fp32 25 (5.3); 65536 x 64 bf16 25 us (0.7 TB/s), fp32 20 (1.7).
 // The variance from registers, and not the mean of squares less the squared mean, which would lose all digits where the mean is large.
 constexpr int LANE = 16;
 
@@ -98,8 +100,9 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void k_norm(const T*
 // The backward pass reads dy and x once: a lane has the same columns of every row that its wave (workgroup) goes through and adds up their share of the
 // parameters' gradients in registers.  A workgroup's shares are added in LDS and leave as one line of `partial` ([workgroup][2][d]), which k_norm_join adds up,
 // so that every sum has one order.  The next row is on its way while one is worked on.  65536 x 1024 bf16: 74 us (403 MB, 5.5 TB/s) and 4.6 for k_norm_join; with a
-// pass of its own for the parameters' gradients dy and x would be read twice.  Small ones (4097 x 777 fp32: 11.6 us and 3.9) wait for their rows' few loads, and
-// for the second launch.
+// pass of its own for the parameters' gradients dy and x would be read twice.  Narrow rows as above (65536 x 256: bf16 44 us, 2.3 TB/s, fp32 35, 5.7; 65536 x 64:
+// 42 and 33 us, 0.6 and 1.5 TB/s); sixteen waves, 8192 x 12288: bf16 130 us, 4.6 TB/s, fp32 231, 5.2.  Small ones (4097 x 777
+// fp32: 11.6 us and 3.9) wait for their rows' few loads, and for the second launch.
 template <typename T, int NV, int WAVES>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void k_norm_grad(const T* dy, int64_t dy_stride, const T* x, int64_t x_stride, const float* __restrict__ gamma,
                                                                              const float* __restrict__ mean, const float* __restrict__ rstd, T* dx, int64_t dx_stride,
