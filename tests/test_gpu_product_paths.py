@@ -48,8 +48,10 @@ def uneven(M, E, seed):
 
 
 # 256 workgroups that stay look their tiles up 256 at a time: 8192 groups and more are never sorted, nor are more than 256 tiles a workgroup, which are looked up
-# anew after every 256 (840000 rows: 164 of the workgroups have 257 and the others 256, and all have to go by the same numbering)
-@pytest.mark.parametrize("M,K,N,E", [(840_000, 64, 5120, 3), (900_000, 64, 5120, 3), (838_000, 64, 5120, 3), (1_700_000, 64, 1280, 8192), (1_600_000, 128, 64, 8200)])
+# anew after every 256 (840000 rows: 164 of the workgroups have 257 and the others 256, and all have to go by the same numbering).  837600 rows and 8191 groups are
+# the last that are sorted
+@pytest.mark.parametrize("M,K,N,E", [(840_000, 64, 5120, 3), (900_000, 64, 5120, 3), (838_000, 64, 5120, 3), (837_600, 64, 5120, 3), (1_700_000, 64, 1280, 8192), (1_600_000, 128, 64, 8200),
+                                     (1_600_000, 128, 64, 8191)])
 def test_tiles_that_are_looked_up_as_they_come(dyn, M, K, N, E):
     g = torch.Generator("cuda").manual_seed(E)
     at = uneven(M, E, 1)
