@@ -16,6 +16,7 @@
  *                                 expert, one grouped FFN per expert, weighted combine
  *      moe_product*()     GPU   — the expert layers' matrix products by themselves, and their gradients; with
  *      dynb_embed*(), dynb_layer_norm*(), dynb_clip_gradients(): what training around such layers takes
+ *      moe_gated*(), dynb_store8(), dynb_load8(): gated layers, and activations kept in 8 bits
  *
  * Conventions
  *   - Every function returns DYNB_OK (0) or a negative DYNB_E_* code; dynb_last_error() gives a
@@ -48,7 +49,7 @@ enum {
     DYNB_E_HIP = -6           /* a HIP runtime call failed                                      */
 };
 
-enum { DYNB_F32 = 0, DYNB_BF16 = 1 };
+enum { DYNB_F32 = 0, DYNB_BF16 = 1, DYNB_I8 = 2 };                /* DYNB_I8: rows in 8 bits, see dynb_rows8 */
 
 /* Scheduling modes for dynbatch_plan (flags & DYNB_SCHED_MASK). */
 enum {
@@ -552,6 +553,72 @@ size_t dynb_layer_norm_backward_workspace_bytes(const dynb_norm_shape* shape);
 int dynb_layer_norm_backward(const dynb_norm_shape* shape, const void* dy, int64_t dy_stride, const void* x, int64_t x_stride,
                              const float* gamma, const float* mean, const float* rstd, void* dx, int64_t dx_stride,
                              float* dgamma, float* dbeta, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Rows of activations in 8 bits, for what a backward pass has to keep.  Every 32 neighbours of a row (the last ones may be fewer)
+ * share a scale: with a = max |x|, s = a / 127 rounded up to a bfloat16, at least 2^-126, and q = the whole number nearest to
+ * x * (1 / s), ties to even; both in fp32, step by step.  The row stands for q s: an element is off by at most s / 2, a / 252.
+ * A block with an infinity or a NaN is NaN altogether; numbers next to the largest of fp32 may come back as infinities. */
+typedef struct {
+    void* q;                  /* device [T][d] int8, rows q_stride elements apart                */
+    int64_t q_stride;         /* at least d                                                      */
+    void* scale;              /* device [T][(d + 31) / 32] bfloat16, rows scale_stride apart     */
+    int64_t scale_stride;
+} dynb_rows8;
+typedef struct {
+    int32_t T;                /* rows (0: no work)                                               */
+    int32_t d;                /* width                                                           */
+    int32_t dtype;            /* DYNB_F32 or DYNB_BF16: x                                        */
+} dynb_rows8_shape;
+
+/* x, device [T][d] dtype, rows x_stride elements apart, into 8 bits; and what they stand for, rounded to dtype, back into x.
+ * Errors: DYNB_E_INVAL (NULL, sizes <= 0, strides below a row's length, misaligned), DYNB_E_UNSUPPORTED (dtype, more than 2^28
+ * columns), DYNB_E_HIP.                                                                          */
+int dynb_store8(const dynb_rows8_shape* shape, const void* x, int64_t x_stride, const dynb_rows8* rows, void* stream);
+int dynb_load8(const dynb_rows8_shape* shape, const dynb_rows8* rows, void* x, int64_t x_stride, void* stream);
+
+/* dynb_layer_norm_backward with x (the layer's input) in 8 bits; mean and rstd as dynb_layer_norm gave them.  Other arguments, workspace and errors as there. */
+int dynb_layer_norm_backward8(const dynb_norm_shape* shape, const void* dy, int64_t dy_stride, const dynb_rows8* x, const float* gamma,
+                              const float* mean, const float* rstd, void* dx, int64_t dx_stride, float* dgamma, float* dbeta,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
+/* A gated feed-forward layer of experts, its first half and what the backward pass has of its own; the second layer is
+ * moe_product, the other gradients moe_product_grad_input and moe_product_grad_weight with N = 2 h.
+ *   gate[r] = in[row(r)] Wg_e^T, up[r] = in[row(r)] Wu_e^T           out[r] = f(gate[r]) up[r]
+ *   with dact[r] = dout[r] W_e (the second layer's):  dgate = dact up f'(gate), dup = dact f(gate), hidden = f(gate) up
+ * f(g) = g sigma(g) (SiLU), or GELU in its tanh form, g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2.                      */
+typedef struct {
+    int32_t M;                /* rows of all groups together (0: no work)                        */
+    int32_t K;                /* moe_gated: channels of a row of in; moe_gated_grad: of dout     */
+    int32_t h;                /* hidden features: of gate, of up, of out                         */
+    int32_t E;                /* experts                                                         */
+    int32_t dtype;            /* DYNB_BF16 only                                                  */
+    uint32_t flags;           /* MOE_GATE_SILU or MOE_GATE_GELU                                  */
+} moe_gated_shape;
+enum { MOE_GATE_SILU = 0, MOE_GATE_GELU = 1 };
+
+/* gate and up of every row, kept between the passes: row r's gate at rows + r * stride, its up h elements further on.
+ * DYNB_BF16: scale is not used.  DYNB_I8: either part is a row of h elements as in dynb_rows8; gate's scales are at
+ * scale + r * scale_stride, up's (h + 31) / 32 elements further on.                              */
+typedef struct {
+    void* rows;               /* device [M][2][h]                                                */
+    int64_t stride;           /* at least 2 h                                                    */
+    void* scale;              /* device [M][2][(h + 31) / 32] bfloat16, or NULL                  */
+    int64_t scale_stride;     /* at least 2 ((h + 31) / 32)                                      */
+    int32_t dtype;            /* DYNB_BF16 or DYNB_I8                                            */
+} moe_gated_pre;
+
+/* All tensors on the device, rows `..._stride` elements apart; groups as in moe_product.
+ *   moe_gated:       in [M or groups->rows][K] bf16   W [E][2][h][K] bf16, dense (Wg, Wu)   out [M][h] bf16
+ *                    pre   what to keep for the backward pass (rounded from fp32; out is not made from the rounded ones), or NULL
+ *   moe_gated_grad:  dout [M][K] bf16   W [E][K][h] bf16, dense   pre  as kept   dpre [M][2][h] bf16
+ *                    hidden [M][h] bf16 or NULL: f(gate) up of what was kept, for the second layer's weights' gradient
+ * Rows behind the last group: out, pre, dpre and hidden are 0.  Results may not overlap with what is read.  Any sizes and addresses;
+ * K and h that are multiples of 8 with rows on 16-byte borders (8-bit rows: on 8-byte borders) run faster.  Equal calls give equal bits.
+ * Errors as moe_product, with h and the dtype of pre.                                           */
+int moe_gated(const moe_gated_shape* shape, const moe_groups* groups, const void* in, int64_t in_stride, const void* W, void* out,
+              int64_t out_stride, const moe_gated_pre* pre, void* stream);
+int moe_gated_grad(const moe_gated_shape* shape, const moe_groups* groups, const void* dout, int64_t dout_stride, const void* W,
+                   const moe_gated_pre* pre, void* dpre, int64_t dpre_stride, void* hidden, int64_t hidden_stride, void* stream);
 
 /* The norm of many gradient tensors together, sqrt(sum of g^2), and the gradients scaled down to a largest one:
  * out = g * max_norm / norm if norm is finite and above max_norm, else out = g.  (A norm that is not finite is for the

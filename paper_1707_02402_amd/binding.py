@@ -9,13 +9,14 @@ from __future__ import annotations
 import ctypes as ct
 import os
 from types import SimpleNamespace
+from typing import NamedTuple
 
 import numpy as np
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libdynbatch.so")
 
-DYNB_F32, DYNB_BF16 = 0, 1
+DYNB_F32, DYNB_BF16, DYNB_I8 = 0, 1, 2
 DYNB_SCHED_IMPROVED, DYNB_SCHED_STANDARD, DYNB_SCHED_NAIVE, DYNB_SCHED_DEPTH = 0, 1, 2, 3
 DYNB_PLAN_THROUGHPUT = 8
 DYNB_PLAN_BALANCE = 4
@@ -33,6 +34,7 @@ EXPORTS = ["dynb_last_error", "dynbatch_plan", "dynbatch_plan_dag", "dynbatch_pl
            "dynb_embed", "dynb_embed_backward_workspace_bytes", "dynb_embed_backward",
            "dynb_layer_norm", "dynb_layer_norm_backward_workspace_bytes", "dynb_layer_norm_backward",
            "dynb_clip_workspace_bytes", "dynb_clip_gradients",
+           "moe_gated", "moe_gated_grad", "dynb_store8", "dynb_load8", "dynb_layer_norm_backward8",
            "dynb_timing_enable", "dynb_probe_mfma_bf16", "dynb_probe_copy", "dynb_probe_read",
            "dynb_timing_read"]
 
@@ -106,6 +108,22 @@ class _NormShape(ct.Structure):
     _fields_ = [(n, ct.c_int32) for n in ("T", "d", "dtype")] + [("eps", ct.c_float)]
 
 
+class _Rows8(ct.Structure):
+    _fields_ = [("q", ct.c_void_p), ("q_stride", ct.c_int64), ("scale", ct.c_void_p), ("scale_stride", ct.c_int64)]
+
+
+class _Rows8Shape(ct.Structure):
+    _fields_ = [(n, ct.c_int32) for n in ("T", "d", "dtype")]
+
+
+class _GatedShape(ct.Structure):
+    _fields_ = [(n, ct.c_int32) for n in ("M", "K", "h", "E", "dtype")] + [("flags", ct.c_uint32)]
+
+
+class _GatedPre(ct.Structure):
+    _fields_ = [("rows", ct.c_void_p), ("stride", ct.c_int64), ("scale", ct.c_void_p), ("scale_stride", ct.c_int64), ("dtype", ct.c_int32)]
+
+
 class _GradTensor(ct.Structure):
     _fields_ = [("grad", ct.c_void_p), ("out", ct.c_void_p), ("count", ct.c_int64), ("dtype", ct.c_int32)]
 
@@ -165,6 +183,12 @@ def _load():
     L.dynb_layer_norm_backward_workspace_bytes.argtypes = [NS]
     L.dynb_layer_norm_backward_workspace_bytes.restype = SZ
     L.dynb_layer_norm_backward.argtypes = [NS, VP, I64, VP, I64, VP, VP, VP, VP, I64, VP, VP, VP, SZ, VP]
+    R8, R8S, GS, GP = (ct.POINTER(t) for t in (_Rows8, _Rows8Shape, _GatedShape, _GatedPre))
+    L.dynb_layer_norm_backward8.argtypes = [NS, VP, I64, R8, VP, VP, VP, VP, I64, VP, VP, VP, SZ, VP]
+    L.dynb_store8.argtypes = [R8S, VP, I64, R8, VP]
+    L.dynb_load8.argtypes = [R8S, R8, VP, I64, VP]
+    L.moe_gated.argtypes = [GS, GR, VP, I64, VP, VP, I64, GP, VP]
+    L.moe_gated_grad.argtypes = [GS, GR, VP, I64, VP, GP, VP, I64, VP, I64, VP]
     L.dynb_clip_workspace_bytes.argtypes = []
     L.dynb_clip_workspace_bytes.restype = SZ
     L.dynb_clip_gradients.argtypes = [ct.POINTER(_GradTensor), ct.c_int32, ct.c_float, VP, VP, SZ, VP]
@@ -635,6 +659,106 @@ def moe_product_grad_weight(dout, x, offsets, perm=None, k: int = 1, dW=None, gr
     return dW
 
 
+# ------------------------------------------------------------------------------------------ gated layers
+MOE_GATE_SILU, MOE_GATE_GELU = 0, 1
+
+
+def _pre_struct(pre, M: int, h: int) -> _GatedPre:
+    import torch
+    rows = pre.q if isinstance(pre, Rows8) else pre
+    stride = rows.stride()
+    assert rows.is_cuda and rows.shape == (M, 2, h) and stride[1] == h and (h == 1 or stride[2] == 1), (rows.shape, stride)
+    row = stride[0] if M > 1 else max(stride[0], 2 * h)
+    if rows is pre:
+        assert rows.dtype is torch.bfloat16
+        return _GatedPre(rows.data_ptr(), row, None, 0, DYNB_BF16)
+    scale, n = pre.scale, (h + 31) // 32
+    s = scale.stride()
+    assert rows.dtype is torch.int8 and scale.is_cuda and scale.dtype is torch.bfloat16 and scale.shape == (M, 2, n) and s[1] == n and (n == 1 or s[2] == 1), (scale.shape, s)
+    return _GatedPre(rows.data_ptr(), row, scale.data_ptr(), s[0] if M > 1 else max(s[0], 2 * n), DYNB_I8)
+
+
+def moe_gated(x, W, offsets, perm=None, k: int = 1, gate: int = MOE_GATE_SILU, out=None, pre=None, stream=None):
+    """out[r] = f(x[row(r)] Wg_e^T) (x[row(r)] Wu_e^T) for the rows r of every group e, f SiLU or GELU (tanh form).  x [rows,K], W [E,2,h,K] (Wg, Wu)
+    bf16; offsets, perm and k as in moe_product.  pre: what to keep of gate and up for the backward pass, a bf16 tensor [M,2,h] or Rows8(q [M,2,h],
+    scale [M,2,(h + 31) // 32]) to be written, or None.  Returns out [M,h] bf16."""
+    import torch
+    E, two, h, K = W.shape
+    M = x.shape[0] if perm is None else perm.shape[0]
+    xs = _rows(x, x.shape[0], K)
+    assert two == 2 and W.is_cuda and W.is_contiguous() and W.dtype == x.dtype == torch.bfloat16 and offsets.shape == (E + 1,)
+    if out is None:
+        out = _new(stream, M, h, like=x)
+    os_ = _rows(out, M, h, x)
+    g = _groups_struct(offsets, perm, k, M, x.shape[0])
+    shape = _GatedShape(M, K, h, E, DYNB_BF16, gate)
+    _check(lib.moe_gated(ct.byref(shape), ct.byref(g), x.data_ptr(), xs, W.data_ptr(), out.data_ptr(), os_, None if pre is None else ct.byref(_pre_struct(pre, M, h)),
+                         _stream(stream)))
+    return out
+
+
+def moe_gated_grad(dout, W, offsets, pre, gate: int = MOE_GATE_SILU, dpre=None, hidden=None, want_hidden: bool = True, stream=None):
+    """Backward through the second layer's product and the gate: with dact[r] = dout[r] W_e, the gradients dact up f'(gate) and dact f(gate) of what was kept,
+    and f(gate) up again, which the second layer's weights' gradient wants.  dout [M,N], W [E,N,h] bf16 (moe_product's second layer), pre as moe_gated kept
+    it.  Returns (dpre [M,2,h], hidden [M,h]) bf16, or dpre alone without want_hidden.  dpre.view(M, 2 * h) and W.view(E, 2 * h, K) of moe_gated are what
+    moe_product_grad_input and moe_product_grad_weight take."""
+    import torch
+    E, N, h = W.shape
+    M = dout.shape[0]
+    ds = _rows(dout, M, N)
+    assert W.is_cuda and W.is_contiguous() and W.dtype == dout.dtype == torch.bfloat16 and offsets.shape == (E + 1,)
+    if dpre is None:
+        dpre = _new(stream, M, 2, h, like=dout)
+    assert not isinstance(dpre, Rows8)
+    d = _pre_struct(dpre, M, h)
+    if hidden is None and want_hidden:
+        hidden = _new(stream, M, h, like=dout)
+    hs = 0 if hidden is None else _rows(hidden, M, h, dout)
+    g = _groups_struct(offsets, None, 1, M, M)
+    shape = _GatedShape(M, N, h, E, DYNB_BF16, gate)
+    _check(lib.moe_gated_grad(ct.byref(shape), ct.byref(g), dout.data_ptr(), ds, W.data_ptr(), ct.byref(_pre_struct(pre, M, h)), d.rows, d.stride,
+                              None if hidden is None else hidden.data_ptr(), hs, _stream(stream)))
+    return dpre if hidden is None else (dpre, hidden)
+
+
+# ------------------------------------------------------------------------------------------ rows in 8 bits
+class Rows8(NamedTuple):
+    """Rows of activations in 8 bits: q [...,d] int8, scale [...,(d + 31) // 32] bfloat16, a scale for every 32 neighbours of a row."""
+    q: object
+    scale: object
+
+
+def _rows8_struct(r: Rows8, T: int, d: int) -> _Rows8:
+    import torch
+    assert r.q.dtype is torch.int8 and r.scale.dtype is torch.bfloat16
+    return _Rows8(r.q.data_ptr(), _rows(r.q, T, d), r.scale.data_ptr(), _rows(r.scale, T, (d + 31) // 32))
+
+
+def dynb_store8(x, out=None, stream=None) -> Rows8:
+    """Rows x [T,d] float32 or bfloat16 in 8 bits, (q [T,d] int8, scale [T,(d + 31) // 32] bfloat16): s = max|x| / 127 of 32 neighbours, rounded up to a
+    bfloat16, q = x / s rounded (both in fp32).  A block with an infinity or a NaN comes back as NaN."""
+    import torch
+    T, d = x.shape
+    xs = _rows(x, T, d)
+    if out is None:
+        out = Rows8(_new(stream, T, d, like=x, dtype=torch.int8), _new(stream, T, (d + 31) // 32, like=x, dtype=torch.bfloat16))
+    shape = _Rows8Shape(T, d, _dtype_code(x))
+    _check(lib.dynb_store8(ct.byref(shape), x.data_ptr(), xs, ct.byref(_rows8_struct(out, T, d)), _stream(stream)))
+    return out
+
+
+def dynb_load8(rows: Rows8, out=None, dtype: int = DYNB_BF16, stream=None):
+    """What rows in 8 bits stand for, q s.  Returns a tensor [T,d] of `dtype`, bfloat16 or float32 (`out`: such a tensor, to be overwritten)."""
+    import torch
+    T, d = rows.q.shape
+    if out is None:
+        out = _new(stream, T, d, like=rows.q, dtype=torch.float32 if dtype == DYNB_F32 else torch.bfloat16)
+    os_ = _rows(out, T, d)
+    shape = _Rows8Shape(T, d, _dtype_code(out))
+    _check(lib.dynb_load8(ct.byref(shape), ct.byref(_rows8_struct(rows, T, d)), out.data_ptr(), os_, _stream(stream)))
+    return out
+
+
 # ------------------------------------------------------------------------------------------ embeddings
 def dynb_embed(tokens, table, scale: float = 1.0, out=None, stream=None):
     """out[t] = scale * table[tokens[t]], a row of zeros for a token outside [0, V).  tokens [T] int32, table [V,d] float32 or bfloat16
@@ -707,22 +831,25 @@ def dynb_layer_norm_backward_workspace_bytes(T: int, d: int, dtype: int) -> int:
 
 
 def dynb_layer_norm_backward(dy, x, gamma, mean, rstd, dx=None, workspace=None, stream=None):
-    """Gradients of dynb_layer_norm: dy, x [T,d], mean and rstd what it returned.  Returns (dx [T,d] in the dtype of x, dgamma [d], dbeta [d]
-    float32)."""
+    """Gradients of dynb_layer_norm: dy, x [T,d], mean and rstd what it returned; x may be Rows8, the layer's input in 8 bits.  Returns (dx [T,d] in the dtype of
+    dy, dgamma [d], dbeta [d] float32)."""
     import torch
-    T, d = x.shape
-    xs, ds = _rows(x, T, d), _rows(dy, T, d, x)
+    T, d = dy.shape
+    eight = isinstance(x, Rows8)
+    ds, xs = _rows(dy, T, d), 0 if eight else _rows(x, T, d, dy)
     if dx is None:
-        dx = _new(stream, T, d, like=x)
-    dxs = _rows(dx, T, d, x)
-    dgamma = _new(stream, d, like=x, dtype=torch.float32)
+        dx = _new(stream, T, d, like=dy)
+    dxs = _rows(dx, T, d, dy)
+    dgamma = _new(stream, d, like=dy, dtype=torch.float32)
     dbeta = _twin(stream, dgamma)
-    shape = _NormShape(T, d, _dtype_code(x), 0.0)
+    shape = _NormShape(T, d, _dtype_code(dy), 0.0)
     if workspace is None:
-        workspace = _scratch(lib.dynb_layer_norm_backward_workspace_bytes(ct.byref(shape)), x.device, stream)
-    _check(lib.dynb_layer_norm_backward(ct.byref(shape), dy.data_ptr(), ds, x.data_ptr(), xs, _fp32(gamma, d), _fp32(mean, T), _fp32(rstd, T), dx.data_ptr(), dxs,
-                                        dgamma.data_ptr(), dbeta.data_ptr(), workspace.data_ptr(), workspace.nbytes,
-                                        _stream(stream)))
+        workspace = _scratch(lib.dynb_layer_norm_backward_workspace_bytes(ct.byref(shape)), dy.device, stream)
+    rest = (_fp32(gamma, d), _fp32(mean, T), _fp32(rstd, T), dx.data_ptr(), dxs, dgamma.data_ptr(), dbeta.data_ptr(), workspace.data_ptr(), workspace.nbytes, _stream(stream))
+    if eight:
+        _check(lib.dynb_layer_norm_backward8(ct.byref(shape), dy.data_ptr(), ds, ct.byref(_rows8_struct(x, T, d)), *rest))
+    else:
+        _check(lib.dynb_layer_norm_backward(ct.byref(shape), dy.data_ptr(), ds, x.data_ptr(), xs, *rest))
     return dx, dgamma, dbeta
 
 

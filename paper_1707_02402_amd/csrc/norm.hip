@@ -10,6 +10,7 @@
 #include "device_utils.h"
 #include "plan_internal.h"
 #include "rows.h"
+#include "rows8.h"
 
 using dynb::fail;
 
@@ -97,16 +98,45 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void k_norm(const T*
     }
 }
 
+// The backward pass's x as it lies (RowsOf), or in 8 bits (Rows8)
+template <typename T>
+struct RowsOf {
+    const T* x;
+    int64_t stride;
+    using Raw = u32x4;
+    __device__ __forceinline__ Raw load(int64_t row, int c, int d) const { return load_piece(x + row * stride + c, d - c); }
+    static __device__ __forceinline__ float value(const Raw& v, int j) { return element<T>(v, j); }
+    __device__ __forceinline__ float at(int64_t row, int c) const { return load_f32(x + row * stride + c); }
+};
+template <typename T>
+struct Rows8 {
+    const int8_t* q;
+    int64_t stride;
+    const bf16_t* scale;
+    int64_t scale_stride;
+    struct Raw { u32x2 q; float s; };
+    __device__ __forceinline__ Raw load(int64_t row, int c, int d) const
+    {
+        if (c >= d) return Raw{{0u, 0u}, 0.f};
+        if constexpr (PIECE<T> == 8) return Raw{load_eight(q + row * stride + c, d - c), bf16_to_f32(scale[row * scale_stride + c / BLOCK8])};
+        else return Raw{{load_four(q + row * stride + c, d - c), 0u}, bf16_to_f32(scale[row * scale_stride + c / BLOCK8])};
+    }
+    static __device__ __forceinline__ float value(const Raw& v, int j) { return unpack8(v.q[j >> 2], j & 3) * v.s; }
+    __device__ __forceinline__ float at(int64_t row, int c) const { return float(q[row * stride + c]) * bf16_to_f32(scale[row * scale_stride + c / BLOCK8]); }
+};
+// said to be other numbers, so that what follows from them is made anew
+__device__ __forceinline__ void anew(u32x4& v) { asm volatile("" : "+v"(v)); }
+template <typename R> __device__ __forceinline__ void anew(R& v) { asm volatile("" : "+v"(v.q), "+v"(v.s)); }
+
 // The backward pass reads dy and x once: a lane has the same columns of every row that its wave (workgroup) goes through and adds up their share of the
 // parameters' gradients in registers.  A workgroup's shares are added in LDS and leave as one line of `partial` ([workgroup][2][d]), which k_norm_join adds up,
 // so that every sum has one order.  The next row is on its way while one is worked on.  65536 x 1024 bf16: 74 us (403 MB, 5.5 TB/s) and 4.6 for k_norm_join; with a
 // pass of its own for the parameters' gradients dy and x would be read twice.  Narrow rows as above (65536 x 256: bf16 44 us, 2.3 TB/s, fp32 35, 5.7; 65536 x 64:
 // 42 and 33 us, 0.6 and 1.5 TB/s); sixteen waves, 8192 x 12288: bf16 130 us, 4.6 TB/s, fp32 231, 5.2.  Small ones (4097 x 777
 // fp32: 11.6 us and 3.9) wait for their rows' few loads, and for the second launch.
-template <typename T, int NV, int WAVES>
-__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void k_norm_grad(const T* dy, int64_t dy_stride, const T* x, int64_t x_stride, const float* __restrict__ gamma,
-                                                                             const float* __restrict__ mean, const float* __restrict__ rstd, T* dx, int64_t dx_stride,
-                                                                             float* __restrict__ partial, int n, int d)
+template <typename T, class X, int NV, int WAVES>
+__device__ __forceinline__ void norm_grad_rows(const T* dy, int64_t dy_stride, X x, const float* __restrict__ gamma, const float* __restrict__ mean, const float* __restrict__ rstd, T* dx,
+                                               int64_t dx_stride, float* __restrict__ partial, int n, int d)
 {
     constexpr int P = PIECE<T>, NL = WAVES * 64, AT_ONCE = WAVES == 1 ? 4 : 1;
     // Sixteen waves have 128 registers each, which hold gamma, both sums and dy and x as they were loaded, of 16 columns.  y, h and y gamma, which the compiler would
@@ -129,14 +159,15 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void k_norm_grad(con
             }
         }
     const int step = int(gridDim.x) * AT_ONCE;
-    u32x4 a[NV], b[NV];
+    u32x4 a[NV];
+    typename X::Raw b[NV];
     float m = 0.f, r = 0.f;
     auto load = [&](int64_t row) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = (i * NL + lane) * P;
             a[i] = load_piece(dy + row * dy_stride + c, d - c);
-            b[i] = load_piece(x + row * x_stride + c, d - c);
+            b[i] = x.load(row, c, d);
         }
         m = mean[row];
         r = rstd[row];
@@ -151,7 +182,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void k_norm_grad(con
 #pragma unroll
             for (int j = 0; j < P; ++j) {
                 const bool on = (i * NL + lane) * P + j < d;   // (what lies behind the row must not count, whatever mean and rstd are)
-                h[i][j] = on ? (element<T>(b[i], j) - m) * r : 0.f;
+                h[i][j] = on ? (X::value(b[i], j) - m) * r : 0.f;
                 const float y = element<T>(a[i], j);
                 dg[i][j] += y * h[i][j];
                 db[i][j] += y;
@@ -183,11 +214,12 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void k_norm_grad(con
             for (int i = 0; i < NV; ++i) {
                 const int c = (i * NL + lane) * P;
                 if constexpr (TIGHT) {
-                    asm volatile("" : "+v"(a[i]), "+v"(b[i]));         // (said to be other numbers)
+                    anew(a[i]);
+                    anew(b[i]);
 #pragma unroll
                     for (int j = 0; j < P; ++j) {
                         v[i][j] = element<T>(a[i], j) * g_[i][j];
-                        h[i][j] = (element<T>(b[i], j) - m0) * r0;
+                        h[i][j] = (X::value(b[i], j) - m0) * r0;
                     }
                 }
 #pragma unroll
@@ -218,6 +250,20 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void k_norm_grad(con
             store_piece<P>(mine + size_t(which) * size_t(d) + c, d - c, sum[i]);
         }
     }
+}
+
+template <typename T, int NV, int WAVES>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void k_norm_grad(const T* dy, int64_t dy_stride, const T* x, int64_t x_stride, const float* __restrict__ gamma,
+                                                                             const float* __restrict__ mean, const float* __restrict__ rstd, T* dx, int64_t dx_stride,
+                                                                             float* __restrict__ partial, int n, int d)
+{
+    norm_grad_rows<T, RowsOf<T>, NV, WAVES>(dy, dy_stride, RowsOf<T>{x, x_stride}, gamma, mean, rstd, dx, dx_stride, partial, n, d);
+}
+template <typename T, int NV, int WAVES>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void k_norm8_grad(const T* dy, int64_t dy_stride, Rows8<T> x, const float* __restrict__ gamma, const float* __restrict__ mean,
+                                                                              const float* __restrict__ rstd, T* dx, int64_t dx_stride, float* __restrict__ partial, int n, int d)
+{
+    norm_grad_rows<T, Rows8<T>, NV, WAVES>(dy, dy_stride, x, gamma, mean, rstd, dx, dx_stride, partial, n, d);
 }
 
 // dgamma and dbeta, as they lie one behind the other in a line of `partial`
@@ -276,30 +322,42 @@ __global__ __launch_bounds__(256) void k_norm_long(const T* x, int64_t x_stride,
     }
 }
 
-template <typename T>
-__global__ __launch_bounds__(256) void k_norm_dx_long(const T* dy, int64_t dy_stride, const T* x, int64_t x_stride, const float* __restrict__ gamma,
-                                                 const float* __restrict__ mean, const float* __restrict__ rstd, T* dx, int64_t dx_stride, int d)
+template <typename T, class X>
+__device__ __forceinline__ void norm_dx_long(const T* dy, int64_t dy_stride, X x, const float* __restrict__ gamma, const float* __restrict__ mean, const float* __restrict__ rstd, T* dx,
+                                             int64_t dx_stride, int d)
 {
     __shared__ float room[4];
     const int64_t t = blockIdx.x;
     const float m = mean[t], r = rstd[t];
     float s1 = 0.f, s2 = 0.f;
     for (int c = threadIdx.x; c < d; c += 256) {
-        const float g = load_f32(dy + t * dy_stride + c) * (gamma ? gamma[c] : 1.f), h = (load_f32(x + t * x_stride + c) - m) * r;
+        const float g = load_f32(dy + t * dy_stride + c) * (gamma ? gamma[c] : 1.f), h = (x.at(t, c) - m) * r;
         s1 += g;
         s2 += g * h;
     }
     s1 = group_sum(s1, room) / float(d);
     s2 = group_sum(s2, room) / float(d);
     for (int c = threadIdx.x; c < d; c += 256) {
-        const float g = load_f32(dy + t * dy_stride + c) * (gamma ? gamma[c] : 1.f), h = (load_f32(x + t * x_stride + c) - m) * r;
+        const float g = load_f32(dy + t * dy_stride + c) * (gamma ? gamma[c] : 1.f), h = (x.at(t, c) - m) * r;
         store_f32(dx + t * dx_stride + c, r * (g - s1 - h * s2));
     }
 }
-
 template <typename T>
-__global__ __launch_bounds__(256) void k_norm_dparams_long(const T* dy, int64_t dy_stride, const T* x, int64_t x_stride, const float* __restrict__ mean,
-                                                      const float* __restrict__ rstd, float* __restrict__ dgamma, float* __restrict__ dbeta, int n, int d)
+__global__ __launch_bounds__(256) void k_norm_dx_long(const T* dy, int64_t dy_stride, const T* x, int64_t x_stride, const float* __restrict__ gamma,
+                                                 const float* __restrict__ mean, const float* __restrict__ rstd, T* dx, int64_t dx_stride, int d)
+{
+    norm_dx_long<T>(dy, dy_stride, RowsOf<T>{x, x_stride}, gamma, mean, rstd, dx, dx_stride, d);
+}
+template <typename T>
+__global__ __launch_bounds__(256) void k_norm8_dx_long(const T* dy, int64_t dy_stride, Rows8<T> x, const float* __restrict__ gamma, const float* __restrict__ mean,
+                                                       const float* __restrict__ rstd, T* dx, int64_t dx_stride, int d)
+{
+    norm_dx_long<T>(dy, dy_stride, x, gamma, mean, rstd, dx, dx_stride, d);
+}
+
+template <typename T, class X>
+__device__ __forceinline__ void norm_dparams_long(const T* dy, int64_t dy_stride, X x, const float* __restrict__ mean, const float* __restrict__ rstd, float* __restrict__ dgamma,
+                                                  float* __restrict__ dbeta, int n, int d)
 {
     __shared__ float room[2][4][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
@@ -307,7 +365,7 @@ __global__ __launch_bounds__(256) void k_norm_dparams_long(const T* dy, int64_t 
     if (c < d)
         for (int64_t t = wave; t < n; t += 4) {
             const float v = load_f32(dy + t * dy_stride + c);
-            sg += v * (load_f32(x + t * x_stride + c) - mean[t]) * rstd[t];
+            sg += v * (x.at(t, c) - mean[t]) * rstd[t];
             sb += v;
         }
     room[0][wave][lane] = sg;
@@ -316,6 +374,18 @@ __global__ __launch_bounds__(256) void k_norm_dparams_long(const T* dy, int64_t 
     if (wave != 0 || c >= d) return;
     if (dgamma) dgamma[c] = (room[0][0][lane] + room[0][1][lane]) + (room[0][2][lane] + room[0][3][lane]);
     if (dbeta) dbeta[c] = (room[1][0][lane] + room[1][1][lane]) + (room[1][2][lane] + room[1][3][lane]);
+}
+template <typename T>
+__global__ __launch_bounds__(256) void k_norm_dparams_long(const T* dy, int64_t dy_stride, const T* x, int64_t x_stride, const float* __restrict__ mean,
+                                                      const float* __restrict__ rstd, float* __restrict__ dgamma, float* __restrict__ dbeta, int n, int d)
+{
+    norm_dparams_long<T>(dy, dy_stride, RowsOf<T>{x, x_stride}, mean, rstd, dgamma, dbeta, n, d);
+}
+template <typename T>
+__global__ __launch_bounds__(256) void k_norm8_dparams_long(const T* dy, int64_t dy_stride, Rows8<T> x, const float* __restrict__ mean, const float* __restrict__ rstd,
+                                                            float* __restrict__ dgamma, float* __restrict__ dbeta, int n, int d)
+{
+    norm_dparams_long<T>(dy, dy_stride, x, mean, rstd, dgamma, dbeta, n, d);
 }
 
 int check(const dynb_norm_shape* s, const std::string& who)
@@ -398,18 +468,23 @@ extern "C" size_t dynb_layer_norm_backward_workspace_bytes(const dynb_norm_shape
     return std::max<size_t>(lines * 2 * size_t(s->d) * 4, 256);
 }
 
-extern "C" int dynb_layer_norm_backward(const dynb_norm_shape* s, const void* dy, int64_t dy_stride, const void* x, int64_t x_stride, const float* gamma, const float* mean,
-                                        const float* rstd, void* dx, int64_t dx_stride, float* dgamma, float* dbeta, void* workspace, size_t workspace_bytes, void* stream)
+namespace {
+
+// x: as it lies, or null and `rows` in 8 bits
+int norm_backward(const dynb_norm_shape* s, const void* dy, int64_t dy_stride, const void* x, int64_t x_stride, const dynb_rows8* rows, const float* gamma, const float* mean,
+                  const float* rstd, void* dx, int64_t dx_stride, float* dgamma, float* dbeta, void* workspace, size_t workspace_bytes, void* stream, const std::string& who)
 {
-    const int rc = check(s, "dynb_layer_norm_backward");
+    const int rc = check(s, who);
     if (rc != DYNB_OK) return rc;
-    if (!workspace || (s->T > 0 && (!dy || !x || !mean || !rstd))) return fail(DYNB_E_INVAL, "dynb_layer_norm_backward: NULL argument");
-    if (dy_stride < s->d || x_stride < s->d || (dx && dx_stride < s->d)) return fail(DYNB_E_INVAL, "dynb_layer_norm_backward: rows overlap (stride below d)");
-    if (workspace_bytes < dynb_layer_norm_backward_workspace_bytes(s)) return fail(DYNB_E_WORKSPACE, "dynb_layer_norm_backward: workspace too small");
-    if (reinterpret_cast<uintptr_t>(workspace) & 255) return fail(DYNB_E_INVAL, "dynb_layer_norm_backward: workspace not 256-byte aligned");
+    const bool there = x || (rows && rows->q && rows->scale);
+    if (!workspace || (s->T > 0 && (!dy || !there || !mean || !rstd))) return fail(DYNB_E_INVAL, who + ": NULL argument");
+    if (dy_stride < s->d || (dx && dx_stride < s->d) || (rows ? rows->q_stride < s->d || rows->scale_stride < (int64_t(s->d) + BLOCK8 - 1) / BLOCK8 : x_stride < s->d))
+        return fail(DYNB_E_INVAL, who + ": rows overlap (stride below d)");
+    if (workspace_bytes < dynb_layer_norm_backward_workspace_bytes(s)) return fail(DYNB_E_WORKSPACE, who + ": workspace too small");
+    if (reinterpret_cast<uintptr_t>(workspace) & 255) return fail(DYNB_E_INVAL, who + ": workspace not 256-byte aligned");
     if (misaligned(dy, s->dtype) || misaligned(x, s->dtype) || misaligned(dx, s->dtype) || misaligned(gamma, DYNB_F32) || misaligned(mean, DYNB_F32) ||
-        misaligned(rstd, DYNB_F32) || misaligned(dgamma, DYNB_F32) || misaligned(dbeta, DYNB_F32))
-        return fail(DYNB_E_INVAL, "dynb_layer_norm_backward: misaligned pointer");
+        misaligned(rstd, DYNB_F32) || misaligned(dgamma, DYNB_F32) || misaligned(dbeta, DYNB_F32) || (rows && misaligned(rows->scale, DYNB_BF16)))
+        return fail(DYNB_E_INVAL, who + ": misaligned pointer");
     hipStream_t st = static_cast<hipStream_t>(stream);
     float* const partial = dgamma || dbeta ? static_cast<float*>(workspace) : nullptr;
     const int lines = grad_lines(s);
@@ -417,24 +492,49 @@ extern "C" int dynb_layer_norm_backward(const dynb_norm_shape* s, const void* dy
         using T = decltype(in);
         constexpr int NV = decltype(nv)::value, WAVES = decltype(waves)::value;
         const T *a = static_cast<const T*>(dy), *b = static_cast<const T*>(x);
+        const Rows8<T> r = rows ? Rows8<T>{static_cast<const int8_t*>(rows->q), rows->q_stride, static_cast<const bf16_t*>(rows->scale), rows->scale_stride} : Rows8<T>{};
         T* const to = static_cast<T*>(dx);
         if constexpr (WAVES > 0) {
-            if (lines > 0)
-                hipLaunchKernelGGL((k_norm_grad<T, NV, WAVES>), dim3(unsigned(lines)), dim3(WAVES == 1 ? 256 : WAVES * 64), 0, st, a, dy_stride, b, x_stride, gamma, mean, rstd, to,
-                                   dx_stride, partial, s->T, s->d);
+            const dim3 threads(WAVES == 1 ? 256 : WAVES * 64);
+            if (lines > 0 && rows)
+                hipLaunchKernelGGL((k_norm8_grad<T, NV, WAVES>), dim3(unsigned(lines)), threads, 0, st, a, dy_stride, r, gamma, mean, rstd, to, dx_stride, partial, s->T, s->d);
+            else if (lines > 0)
+                hipLaunchKernelGGL((k_norm_grad<T, NV, WAVES>), dim3(unsigned(lines)), threads, 0, st, a, dy_stride, b, x_stride, gamma, mean, rstd, to, dx_stride, partial, s->T, s->d);
             if (partial) hipLaunchKernelGGL(k_norm_join, dim3(unsigned((2 * int64_t(s->d) + 63) / 64)), dim3(1024), 0, st, partial, dgamma, dbeta, lines, s->d);
             return;
         }
         // (the parameters' first: dx may be dy or x)
-        if (dgamma || dbeta)
-            hipLaunchKernelGGL((k_norm_dparams_long<T>), dim3(unsigned((s->d + 63) / 64)), dim3(256), 0, st, a, dy_stride, b, x_stride, mean, rstd, dgamma, dbeta, s->T, s->d);
-        for (int64_t t = 0; t < s->T && dx; t += MOST_ROWS)
-            hipLaunchKernelGGL((k_norm_dx_long<T>), dim3(unsigned(std::min<int64_t>(s->T - t, MOST_ROWS))), dim3(256), 0, st, a + t * dy_stride, dy_stride, b + t * x_stride, x_stride, gamma,
-                               mean + t, rstd + t, to + t * dx_stride, dx_stride, s->d);
+        const dim3 columns(unsigned((s->d + 63) / 64));
+        if ((dgamma || dbeta) && rows) hipLaunchKernelGGL((k_norm8_dparams_long<T>), columns, dim3(256), 0, st, a, dy_stride, r, mean, rstd, dgamma, dbeta, s->T, s->d);
+        else if (dgamma || dbeta) hipLaunchKernelGGL((k_norm_dparams_long<T>), columns, dim3(256), 0, st, a, dy_stride, b, x_stride, mean, rstd, dgamma, dbeta, s->T, s->d);
+        for (int64_t t = 0; t < s->T && dx; t += MOST_ROWS) {
+            const dim3 n(unsigned(std::min<int64_t>(s->T - t, MOST_ROWS)));
+            if (rows)
+                hipLaunchKernelGGL((k_norm8_dx_long<T>), n, dim3(256), 0, st, a + t * dy_stride, dy_stride, Rows8<T>{r.q + t * r.stride, r.stride, r.scale + t * r.scale_stride, r.scale_stride},
+                                   gamma, mean + t, rstd + t, to + t * dx_stride, dx_stride, s->d);
+            else
+                hipLaunchKernelGGL((k_norm_dx_long<T>), n, dim3(256), 0, st, a + t * dy_stride, dy_stride, b + t * x_stride, x_stride, gamma, mean + t, rstd + t, to + t * dx_stride, dx_stride,
+                                   s->d);
+        }
     };
     if (s->dtype == DYNB_BF16) by_width(bf16_t{}, s->d, launch);
     else by_width(float{}, s->d, launch);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return fail(DYNB_E_HIP, std::string("dynb_layer_norm_backward: ") + hipGetErrorString(e));
+    if (e != hipSuccess) return fail(DYNB_E_HIP, who + ": " + hipGetErrorString(e));
     return DYNB_OK;
+}
+
+}  // namespace
+
+extern "C" int dynb_layer_norm_backward(const dynb_norm_shape* s, const void* dy, int64_t dy_stride, const void* x, int64_t x_stride, const float* gamma, const float* mean,
+                                        const float* rstd, void* dx, int64_t dx_stride, float* dgamma, float* dbeta, void* workspace, size_t workspace_bytes, void* stream)
+{
+    return norm_backward(s, dy, dy_stride, x, x_stride, nullptr, gamma, mean, rstd, dx, dx_stride, dgamma, dbeta, workspace, workspace_bytes, stream, "dynb_layer_norm_backward");
+}
+
+extern "C" int dynb_layer_norm_backward8(const dynb_norm_shape* s, const void* dy, int64_t dy_stride, const dynb_rows8* x, const float* gamma, const float* mean, const float* rstd, void* dx,
+                                         int64_t dx_stride, float* dgamma, float* dbeta, void* workspace, size_t workspace_bytes, void* stream)
+{
+    const dynb_rows8 none = {};
+    return norm_backward(s, dy, dy_stride, nullptr, 0, x ? x : &none, gamma, mean, rstd, dx, dx_stride, dgamma, dbeta, workspace, workspace_bytes, stream, "dynb_layer_norm_backward8");
 }
