@@ -46,5 +46,6 @@ struct Gate {
     int64_t hidden_stride;
     __device__ __forceinline__ int blocks() const { return (h + 31) / 32; }
 };
+template <int KEEP_> struct GateKeeping : Gate { static constexpr int KEEP = KEEP_; };         // ... in a kernel that is made for one way of keeping
 
 }  // namespace

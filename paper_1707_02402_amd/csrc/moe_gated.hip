@@ -10,6 +10,12 @@ __global__ __launch_bounds__(256, 2) void k_gated_any(Args p, Gate gate, int uni
     product_tiles_any<DIR, bf16_t>(p, gate, units, ct, 1, Shares{}, nullptr);
 }
 
+template <int DIR, class S, int KEEP>
+__global__ __launch_bounds__(S::THREADS, S::SIMD) void k_gated(Args p, GateKeeping<KEEP> gate, int units, int ct)
+{
+    product_tiles<DIR, bf16_t, S, false>(p, gate, units, ct, 1, Shares{}, nullptr);
+}
+
 int check(const moe_gated_shape* s, const std::string& who)
 {
     if (!s) return fail(DYNB_E_INVAL, who + ": NULL shape");
@@ -47,16 +53,65 @@ Gate gate_of(const moe_gated_shape* s, const moe_gated_pre* p, void* hidden, int
     return g;
 }
 
-template <int DIR>
-int launch_gated(const moe_product_shape* s, const Args& p, const Gate& gate, hipStream_t st, const char* who)
+// LDS beyond 64 KB has to be asked for: a kernel is asked for once on every device (beyond DEVICES, at every call)
+template <class K, class... A>
+int launch_with(K kernel, std::atomic<bool>* asked, uint32_t lds, int64_t grid, int threads, hipStream_t st, const char* who, A... args)
 {
+    constexpr int DEVICES = 64;
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e == hipSuccess && (dev < 0 || dev >= DEVICES || !asked[dev].load())) {
+        e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
+        if (e == hipSuccess && dev >= 0 && dev < DEVICES) asked[dev].store(true);
+    }
+    if (e != hipSuccess) return fail(DYNB_E_HIP, std::string(who) + ": " + hipGetErrorString(e));
+    hipLaunchKernelGGL(kernel, dim3(unsigned(grid)), dim3(unsigned(threads)), lds, st, args...);
+    return launched(who);
+}
+
+template <int DIR>
+int launch_gated(const moe_product_shape* s, const Args& p, const Gate& gate, bool fast, hipStream_t st, const char* who)
+{
+    auto launch = [&](auto kind, auto keep) {
+        using S = decltype(kind);
+        constexpr int KEEP = decltype(keep)::value;
+        static std::atomic<bool> asked[64];
+        const int wide = DIR == FORWARD ? S::COLS / 2 : S::COLS, ct = (gate.h + wide - 1) / wide;
+        const int64_t units = (S::BIG ? int64_t(s->M) / S::ROWS + s->E + 1 : most_pieces(s->M, s->E, S::ROWS)) * ct;
+        if (units > MOST_GROUPS) return fail(DYNB_E_UNSUPPORTED, std::string(who) + ": too many results");
+        GateKeeping<KEEP> g = {};
+        static_cast<Gate&>(g) = gate;
+        return launch_with(k_gated<DIR, S, KEEP>, asked, LDS_BYTES<DIR, S>, S::BIG ? std::min<int64_t>(units, CUS) : units, S::THREADS, st, who, p, g, int(units), ct);
+    };
+    auto keeping = [&](auto kind) {
+        if (gate.keep == KEEP_8) return launch(kind, std::integral_constant<int, KEEP_8>{});
+        if constexpr (DIR == FORWARD)
+            if (gate.keep == KEEP_NOTHING) return launch(kind, std::integral_constant<int, KEEP_NOTHING>{});
+        return launch(kind, std::integral_constant<int, KEEP_BF16>{});
+    };
+    if (fast) switch (kind_of(s, DIR == FORWARD ? s->N : s->K, DIR == FORWARD ? s->K : s->N)) {
+        case BIG: return keeping(Big{});
+        case MID: return keeping(Mid{});
+        default:
+            if constexpr (DIR == FORWARD) {                    // (8 bits: 32 features have to be a wave's)
+                if (gate.keep == KEEP_8) return launch(Mid{}, std::integral_constant<int, KEEP_8>{});
+                if (gate.keep == KEEP_NOTHING) return launch(Few{}, std::integral_constant<int, KEEP_NOTHING>{});
+                return launch(Few{}, std::integral_constant<int, KEEP_BF16>{});
+            } else return keeping(Few{});
+        }
+    static std::atomic<bool> asked[64];
     const int wide = DIR == FORWARD ? Mid::COLS / 2 : Mid::COLS, ct = (gate.h + wide - 1) / wide;
     const int64_t units = most_pieces(s->M, s->E, Mid::ROWS) * ct;
     if (units > MOST_GROUPS) return fail(DYNB_E_UNSUPPORTED, std::string(who) + ": too many results");
-    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k_gated_any<DIR>), hipFuncAttributeMaxDynamicSharedMemorySize, int(LDS_BYTES<DIR, Mid>));
-    if (e != hipSuccess) return fail(DYNB_E_HIP, std::string(who) + ": " + hipGetErrorString(e));
-    hipLaunchKernelGGL((k_gated_any<DIR>), dim3(unsigned(units)), dim3(256), (LDS_BYTES<DIR, Mid>), st, p, gate, int(units), ct);
-    return launched(who);
+    return launch_with(k_gated_any<DIR>, asked, LDS_BYTES<DIR, Mid>, units, 256, st, who, p, gate, int(units), ct);
+}
+
+// whether what is kept lies on borders of 8 elements
+bool kept_on_8(const moe_gated_pre* p)
+{
+    if (!p) return true;
+    if (p->dtype == DYNB_BF16) return p->stride % 8 == 0 && on_16({p->rows});
+    return p->stride % 8 == 0 && (reinterpret_cast<uintptr_t>(p->rows) & 7) == 0;
 }
 
 }  // namespace
@@ -73,7 +128,10 @@ extern "C" int moe_gated(const moe_gated_shape* s, const moe_groups* g, const vo
     if (in_stride < s->K || out_stride < s->h) return fail(DYNB_E_INVAL, "moe_gated: rows overlap (stride below their length)");
     if (odd(in) || odd(W) || odd(out)) return fail(DYNB_E_INVAL, "moe_gated: misaligned pointer");
     const Args p = {groups_of(&as, g), static_cast<const bf16_t*>(W), static_cast<const bf16_t*>(in), 0, in_stride, nullptr, 0, out, out_stride, as.K, as.N, 0};
-    return launch_gated<FORWARD>(&as, p, gate_of(s, pre, nullptr, 0), static_cast<hipStream_t>(stream), "moe_gated");
+    // (32-bit offsets within an expert's two matrices: up's rows lie h rows behind gate's)
+    const bool fast = s->K % 8 == 0 && s->h % 8 == 0 && in_stride % 8 == 0 && out_stride % 8 == 0 && on_16({in, W, out}) && kept_on_8(pre) && reached(g, in_stride, 0) &&
+                      (int64_t(s->h) + 256) * s->K * 2 < int64_t(1) << 32;
+    return launch_gated<FORWARD>(&as, p, gate_of(s, pre, nullptr, 0), fast, static_cast<hipStream_t>(stream), "moe_gated");
 }
 
 extern "C" int moe_gated_grad(const moe_gated_shape* s, const moe_groups* g, const void* dout, int64_t dout_stride, const void* W, const moe_gated_pre* pre, void* dpre, int64_t dpre_stride,
@@ -90,5 +148,7 @@ extern "C" int moe_gated_grad(const moe_gated_shape* s, const moe_groups* g, con
     if (dout_stride < s->K || dpre_stride < 2 * int64_t(s->h) || (hidden && hidden_stride < s->h)) return fail(DYNB_E_INVAL, "moe_gated_grad: rows overlap (stride below their length)");
     if (odd(dout) || odd(W) || odd(dpre) || odd(hidden)) return fail(DYNB_E_INVAL, "moe_gated_grad: misaligned pointer");
     const Args p = {groups_of(&as, g), static_cast<const bf16_t*>(W), static_cast<const bf16_t*>(dout), 0, dout_stride, nullptr, 0, dpre, dpre_stride, as.K, as.N, 0};
-    return launch_gated<GRAD_INPUT>(&as, p, gate_of(s, pre, hidden, hidden_stride), static_cast<hipStream_t>(stream), "moe_gated_grad");
+    const bool fast = s->K % 8 == 0 && s->h % 8 == 0 && dout_stride % 8 == 0 && dpre_stride % 8 == 0 && hidden_stride % 8 == 0 && on_16({dout, W, dpre, hidden}) && kept_on_8(pre) &&
+                      reached(g, 0, dout_stride);
+    return launch_gated<GRAD_INPUT>(&as, p, gate_of(s, pre, hidden, hidden_stride), fast, static_cast<hipStream_t>(stream), "moe_gated_grad");
 }

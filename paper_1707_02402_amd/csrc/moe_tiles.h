@@ -214,6 +214,197 @@ __device__ __forceinline__ Place walk(int u, int rows, int ct)
     return Place{group * TALL + in % tall, in / tall};
 }
 
+// A kept pair's gate and up, features c .. c + 7 of a row (`left` of them are there), as they lie and as numbers
+template <int KEEP>
+struct KeptEight {
+    u32x4 g, u;
+    __device__ __forceinline__ void load(const Gate& gate, int64_t row, int c, int left)
+    {
+        const bf16_t* const from = static_cast<const bf16_t*>(gate.pre) + row * gate.pre_stride + c;
+        g = load_piece(from, left);
+        u = load_piece(from + gate.h, left);
+    }
+    __device__ __forceinline__ float gate_at(int i) const { return element<bf16_t>(g, i); }
+    __device__ __forceinline__ float up_at(int i) const { return element<bf16_t>(u, i); }
+};
+template <>
+struct KeptEight<KEEP_8> {
+    u32x2 g, u;
+    bf16_t sg, su;
+    __device__ __forceinline__ void load(const Gate& gate, int64_t row, int c, int left)
+    {
+        const int8_t* const from = static_cast<const int8_t*>(gate.pre) + row * gate.pre_stride + c;
+        const bf16_t* const scale = gate.scale + row * gate.scale_stride + c / BLOCK8;
+        g = load_eight(from, left);
+        u = load_eight(from + gate.h, left);
+        sg = scale[0];
+        su = scale[gate.blocks()];
+    }
+    __device__ __forceinline__ float gate_at(int i) const { return unpack8(g[i >> 2], i & 3) * bf16_to_f32(sg); }
+    __device__ __forceinline__ float up_at(int i) const { return unpack8(u[i >> 2], i & 3) * bf16_to_f32(su); }
+};
+// The gradients of gate and up of eight features, and f(gate) up, for dact(i), the gradient of feature i.  alive: 0 for a row of no group, whose results are 0 whatever was
+// kept there
+template <int KEEP, class F>
+__device__ __forceinline__ void grad_of_eight(const Gate& gate, const KeptEight<KEEP>& kept, bool grouped, F dact, float* dg, float* du, float* f)
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float u = kept.up_at(i), d = dact(i);
+        const GateValue v = gate_both(gate.form, kept.gate_at(i));
+        dg[i] = grouped ? d * u * v.slope : 0.f;
+        du[i] = grouped ? d * v.f : 0.f;
+        f[i] = grouped ? v.f * u : 0.f;
+    }
+}
+__device__ __forceinline__ u32x4 pack_eight(const float* v) { return u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])}; }
+
+// How a gated layer's tile leaves (h and all rows on borders of 8 elements).  Like a product's, by way of LDS, each wave its own share `room` of the last chunk's place,
+// block of 32 rows after block.
+//
+// Forward: a lane's sums are gate and up of the same eight features.  What is kept in 8 bits shares scales among the 32 features of two blocks of columns, which the
+// two halves of the wave have.  nchunk 0: rows of no group, zeros, and the LDS is the next tile's.
+template <class S, int LIVE, int KEEP>
+__device__ __forceinline__ void leave_pairs(const f32x16 (&acc)[S::FA][LIVE > 0 ? LIVE : 1], const Gate& gate, const Args& p, const Tile& now, lds_ptr room, int nchunk, int lane, int cg, int rg)
+{
+    using lds_u32x4 = __attribute__((address_space(3))) u32x4;
+    using lds_u32x2 = __attribute__((address_space(3))) u32x2;
+    constexpr int FA = S::FA, PARTS = KEEP == KEEP_BF16 ? 3 : 1, PITCH = FA * 32 + 16, PART = 32 * PITCH, PITCH8 = FA * 16 + 16, PART8 = 32 * PITCH8;
+    constexpr int LANES = FA * 2, AT_ONCE = 64 / LANES, STORES = 32 / AT_ONCE;
+    static_assert(KEEP != KEEP_8 || FA % 2 == 0, "a block of 32 features");
+    static_assert(PARTS * PART + (KEEP == KEEP_8 ? 2 * PART8 : 0) <= int(BUF_BYTES<FORWARD, S> / S::WAVES), "room");
+    const int q = lane & 31, hk = lane >> 5, h = gate.h, first = now.c0 + cg * (FA * 16), col = lane % LANES * 8, row = lane / LANES;
+    const bool on = first + col < h;
+    const int64_t from = now.begin + rg * 32;
+    const lds_ptr in = room + uint32_t(q * PITCH + hk * 16), in8 = room + uint32_t(PARTS * PART + q * PITCH8 + hk * 8);
+    const lds_ptr out = room + uint32_t(row * PITCH + col * 2), out8 = room + uint32_t(PARTS * PART + row * PITCH8 + col);
+#pragma unroll
+    for (int b = 0; b < LIVE; ++b) {
+        const int block = (b * S::RG) * 32, left = now.rows - block - rg * 32;
+        if (nchunk > 0) {
+#pragma unroll
+            for (int a = 0; a < FA; ++a) {
+                float y[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) y[i] = gate_f(gate.form, acc[a][b][i]) * acc[a][b][8 + i];
+                *(lds_u32x4*)(in + uint32_t(a * 32)) = pack_eight(y);
+                if constexpr (KEEP == KEEP_BF16)
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) y[i] = acc[a][b][8 * s + i];
+                        *(lds_u32x4*)(in + uint32_t((1 + s) * PART + a * 32)) = pack_eight(y);
+                    }
+                __builtin_amdgcn_sched_barrier(0);             // (all accumulators at once in other registers would have no room)
+            }
+            if constexpr (KEEP == KEEP_8)
+#pragma unroll
+                for (int a = 0; a < FA; a += 2)
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        uint32_t largest = 0u;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) largest = max(largest, magnitude(acc[a + (i >> 3)][b][8 * s + (i & 7)]));
+                        const Scale8 c = scale8(max(largest, uint32_t(__shfl_xor(int(largest), 32))));
+#pragma unroll
+                        for (int n = 0; n < 2; ++n) {
+                            float x[8];
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) x[i] = acc[a + n][b][8 * s + i];
+                            *(lds_u32x2*)(in8 + uint32_t(s * PART8 + (a + n) * 16)) = u32x2{pack8(x[0], x[1], x[2], x[3], c.inv), pack8(x[4], x[5], x[6], x[7], c.inv)};
+                        }
+                        const int f = first + a * 16;
+                        if (hk == 0 && q < left && f < h) gate.scale[(from + block + q) * gate.scale_stride + s * gate.blocks() + f / BLOCK8] = scale8_bits(c);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+            wave_sync();
+        } else if (KEEP == KEEP_8 && hk == 0 && q < left)
+#pragma unroll
+            for (int a = 0; a < FA; a += 2)
+                if (first + a * 16 < h)
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) gate.scale[(from + block + q) * gate.scale_stride + s * gate.blocks() + (first + a * 16) / BLOCK8] = scale8_bits(scale8(0u));
+        const u32x4 none = {0u, 0u, 0u, 0u};
+        bf16_t* const to = static_cast<bf16_t*>(p.out) + (from + block + row) * p.out_stride + first + col;
+#pragma unroll
+        for (int i = 0; i < STORES; ++i) {
+            const u32x4 v = nchunk > 0 ? *(const lds_u32x4*)(out + uint32_t(i * AT_ONCE * PITCH)) : none;
+            if (row + i * AT_ONCE < left && on) *reinterpret_cast<u32x4*>(to + i * AT_ONCE * p.out_stride) = v;
+        }
+        if constexpr (KEEP == KEEP_BF16) {
+            bf16_t* const pre = static_cast<bf16_t*>(gate.pre) + (from + block + row) * gate.pre_stride + first + col;
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int i = 0; i < STORES; ++i) {
+                    const u32x4 v = nchunk > 0 ? *(const lds_u32x4*)(out + uint32_t((1 + s) * PART + i * AT_ONCE * PITCH)) : none;
+                    if (row + i * AT_ONCE < left && on) *reinterpret_cast<u32x4*>(pre + i * AT_ONCE * gate.pre_stride + s * h) = v;
+                }
+        }
+        if constexpr (KEEP == KEEP_8) {
+            int8_t* const pre = static_cast<int8_t*>(gate.pre) + (from + block + row) * gate.pre_stride + first + col;
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int i = 0; i < STORES; ++i) {
+                    const u32x2 v = nchunk > 0 ? *(const lds_u32x2*)(out8 + uint32_t(s * PART8 + i * AT_ONCE * PITCH8)) : u32x2{0u, 0u};
+                    if (row + i * AT_ONCE < left && on) *reinterpret_cast<u32x2*>(pre + i * AT_ONCE * gate.pre_stride + s * h) = v;
+                }
+        }
+        wave_sync();
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
+// Backward: dact goes through LDS in fp32, unrounded, and meets the kept pair where a lane has eight neighbouring features of a row.  A row has FA * 8 pieces of 16 bytes there,
+// piece j of row q at place j ^ q (of the places that there are), so that neither side's accesses meet in a bank.
+template <class S, int LIVE, int KEEP>
+__device__ __forceinline__ void leave_grads(const f32x16 (&acc)[S::FA][LIVE > 0 ? LIVE : 1], const Gate& gate, const Args& p, const Tile& now, lds_ptr room, int nchunk, int lane, int cg, int rg)
+{
+    using lds_f32x4 = __attribute__((address_space(3))) f32x4;
+    constexpr int FA = S::FA, PIECES = FA * 8, LANES = FA * 4, AT_ONCE = 64 / LANES, STORES = 32 / AT_ONCE;
+    static_assert(32 * PIECES * 16 <= int(BUF_BYTES<GRAD_INPUT, S> / S::WAVES), "room");
+    const int q = lane & 31, hk = lane >> 5, h = gate.h, col = lane % LANES * 8, row = lane / LANES, c = now.c0 + cg * (FA * 32) + col;
+    const bool on = c < h;
+    bf16_t* const out = static_cast<bf16_t*>(p.out);
+#pragma unroll
+    for (int b = 0; b < LIVE; ++b) {
+        const int64_t from = now.begin + (b * S::RG + rg) * 32 + row;
+        const int left = now.rows - (b * S::RG + rg) * 32 - row;
+        KeptEight<KEEP> kept[STORES];
+#pragma unroll
+        for (int i = 0; i < STORES; ++i) kept[i].load(gate, from + (left > i * AT_ONCE ? i * AT_ONCE : -row - (b * S::RG + rg) * 32), on ? c : h - 8, 8);
+        if (nchunk > 0)
+#pragma unroll
+            for (int a = 0; a < FA; ++a) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    *(lds_f32x4*)(room + uint32_t((q * PIECES + ((a * 8 + hk * 4 + j) ^ (q & (PIECES - 1)))) * 16)) =
+                        f32x4{acc[a][b][4 * j], acc[a][b][4 * j + 1], acc[a][b][4 * j + 2], acc[a][b][4 * j + 3]};
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        wave_sync();
+#pragma unroll
+        for (int i = 0; i < STORES; ++i) {
+            const int r = row + i * AT_ONCE;
+            f32x4 d[2] = {};
+            if (nchunk > 0)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) d[j] = *(const lds_f32x4*)(room + uint32_t((r * PIECES + ((col / 4 + j) ^ (r & (PIECES - 1)))) * 16));
+            float dg[8], du[8], f[8];
+            grad_of_eight<KEEP>(gate, kept[i], nchunk > 0, [&](int e) { return d[e >> 2][e & 3]; }, dg, du, f);
+            if (i * AT_ONCE < left && on) {
+                const int64_t at = from + i * AT_ONCE;
+                *reinterpret_cast<u32x4*>(out + at * p.out_stride + c) = pack_eight(dg);
+                *reinterpret_cast<u32x4*>(out + at * p.out_stride + h + c) = pack_eight(du);
+                if (gate.hidden) *reinterpret_cast<u32x4*>(gate.hidden + at * gate.hidden_stride + c) = pack_eight(f);
+            }
+        }
+        wave_sync();
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
 // A gated layer's forward tiles: a block of 32 columns is gate and up of 16 features, in the order that gives a lane (row q of the accumulators' columns, half hk) gate of
 // features 8 hk .. 8 hk + 7 in its first eight sums and up of the same ones in the others.  Which of the 16 features row s_q of the block's operand is (of gate up to
 // row 15, of up from there):
@@ -775,7 +966,9 @@ __device__ __forceinline__ void product_tiles(Args p, G gate, int units, int ct,
                 }
             };
             const int first_col = now.c0 + cg * (FA * 32);
-            if constexpr (DIR == GRAD_WEIGHT) {
+            if constexpr (PAIRS) leave_pairs<S, LIVE, G::KEEP>(acc, gate, p, now, mine_at, nchunk, lane, cg, rg);
+            else if constexpr (G::ON) leave_grads<S, LIVE, G::KEEP>(acc, gate, p, now, mine_at, nchunk, lane, cg, rg);
+            else if constexpr (DIR == GRAD_WEIGHT) {
                 const size_t row = size_t(now.r0) * size_t(p.K) + size_t(first_col), all = size_t(p.N) * size_t(p.K);
                 float* const part = now.slot >= 0 ? partial + size_t(now.slot) * all + row : nullptr;
                 TO* const to = static_cast<TO*>(p.out) + size_t(now.e) * all + row;
@@ -792,7 +985,10 @@ __device__ __forceinline__ void product_tiles(Args p, G gate, int units, int ct,
         if (nchunk == 0) then = next_tile();
         primed = nchunk > 0 && then.depth > 0;
         // (the fewest that there can have been: of the blocks that are whole)
-        stores = now.c0 + cg * (FA * 32) + FA * 32 <= cols ? max(0, (now.rows / 32 - rg + S::RG - 1) / S::RG) * FA * (DIR == GRAD_WEIGHT ? int(sizeof(TO)) : 2) : 0;
+        if constexpr (G::ON)
+            // (gated: out, and of the kept pair two in bfloat16 or two in 8 bits and scales; backwards three, or two without the hidden rows)
+            stores = now.c0 + (cg + 1) * WAVE_WIDE <= cols ? max(0, (now.rows / 32 - rg + S::RG - 1) / S::RG) * FA * (PAIRS ? (G::KEEP == KEEP_NOTHING ? 1 : 3) : 4) : 0;
+        else stores = now.c0 + cg * (FA * 32) + FA * 32 <= cols ? max(0, (now.rows / 32 - rg + S::RG - 1) / S::RG) * FA * (DIR == GRAD_WEIGHT ? int(sizeof(TO)) : 2) : 0;
         now = then;
     }
     answered_but<0>();                                         // (nothing is on its way to LDS that another workgroup may have next)
@@ -803,41 +999,6 @@ __device__ __forceinline__ void product_tiles(Args p, G gate, int units, int ct,
 // straight into LDS keeps to), the last of a row element by element, a chunk ahead.  65536 rows, 1001 -> 1501, one expert: 465 us forward, 485 the input's
 // gradient, 855 the weights', where 1000 -> 1504 takes 231, 207 and 241 through k_product, whose tiles
 // of 256 x 256 read either operand half as often and have their next chunk on its way without registers (what share each has was not taken apart).
-// The gradients of gate and up of row `row`, features c .. c + 7 (`left` of them are there), and f(gate) up, for dact(i), the gradient of feature c + i; zeros for a row
-// of no group, whatever the kept pair holds there
-template <class F>
-__device__ __forceinline__ void grad_of_eight(const Gate& gate, int64_t row, int c, int left, bool grouped, F dact, float* dg, float* du, float* f)
-{
-    float g[8], u[8];
-    if (gate.keep == KEEP_8) {
-        const int8_t* const from = static_cast<const int8_t*>(gate.pre) + row * gate.pre_stride + c;
-        const bf16_t* const scale = gate.scale + row * gate.scale_stride + c / BLOCK8;
-        const u32x2 a = load_eight(from, left), b = load_eight(from + gate.h, left);
-        const float sa = bf16_to_f32(scale[0]), sb = bf16_to_f32(scale[gate.blocks()]);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            g[i] = unpack8(a[i >> 2], i & 3) * sa;
-            u[i] = unpack8(b[i >> 2], i & 3) * sb;
-        }
-    } else {
-        const bf16_t* const from = static_cast<const bf16_t*>(gate.pre) + row * gate.pre_stride + c;
-        const u32x4 a = load_piece(from, left), b = load_piece(from + gate.h, left);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            g[i] = element<bf16_t>(a, i);
-            u[i] = element<bf16_t>(b, i);
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const GateValue v = gate_both(gate.form, g[i]);
-        const float d = dact(i);
-        dg[i] = grouped ? d * u[i] * v.slope : 0.f;
-        du[i] = grouped ? d * v.f : 0.f;
-        f[i] = grouped ? v.f * u[i] : 0.f;
-    }
-}
-
 // A gated layer's results, each lane's where they belong: of every block b of 32 rows row q, of every block a of 32 columns gate and up of 8 features (forward) or
 // the gradients of 16 hidden features.
 template <int DIR>
@@ -891,7 +1052,13 @@ __device__ __forceinline__ void leave_any(const f32x16 (&acc)[2][2], const Gate&
                 const int c = t.c0 + (cg * 2 + (n >> 1)) * 32 + 16 * hk + 8 * (n & 1), left = h - c;
                 if (!there || left <= 0) continue;
                 float dg[8], du[8], f[8];
-                grad_of_eight(gate, row, c, left, t.depth > 0, [&](int i) { return acc[n >> 1][b][8 * (n & 1) + i]; }, dg, du, f);
+                auto both = [&](auto keep) {
+                    KeptEight<decltype(keep)::value> kept;
+                    kept.load(gate, row, c, left);
+                    grad_of_eight(gate, kept, t.depth > 0, [&](int i) { return acc[n >> 1][b][8 * (n & 1) + i]; }, dg, du, f);
+                };
+                if (gate.keep == KEEP_8) both(std::integral_constant<int, KEEP_8>{});
+                else both(std::integral_constant<int, KEEP_BF16>{});
                 store_piece<8>(out + row * p.out_stride + c, left, dg);
                 store_piece<8>(out + row * p.out_stride + h + c, left, du);
                 if (gate.hidden) store_piece<8>(gate.hidden + row * gate.hidden_stride + c, left, f);
