@@ -26,8 +26,8 @@ __device__ __forceinline__ float gate_f(const GateForm& k, float g)
 }
 __device__ __forceinline__ GateValue gate_both(const GateForm& k, float g)
 {
-    const float c = within_1e4(g), c2 = c * c, s = gate_sigma(k, g, c2);
-    return GateValue{g * s, s + s * (1.f - s) * (c * (k.a + k.b3 * c2))};
+    const float c = within_1e4(g), c2 = c * c, s = gate_sigma(k, g, c2), w = k.a + k.b3 * c2;
+    return GateValue{g * s, s + s * (c * (w - s * w))};
 }
 
 // What a gated layer keeps of its forward pass: gate and up of row r at pre + r * stride and h further on, in bfloat16 or in 8 bits with their scales
@@ -44,6 +44,7 @@ struct Gate {
     int64_t scale_stride;
     bf16_t* hidden;           // backward: f(gate) up, or null
     int64_t hidden_stride;
+    bool past;                // results go past the caches
     __device__ __forceinline__ int blocks() const { return (h + 31) / 32; }
 };
 template <int KEEP_> struct GateKeeping : Gate { static constexpr int KEEP = KEEP_; };         // ... in a kernel that is made for one way of keeping

@@ -4,12 +4,133 @@
 
 namespace {
 
-template <int DIR>
-__global__ __launch_bounds__(256, 2) void k_gated_any(Args p, Gate gate, int units, int ct)
+// ------------------------------------------------------------------------------------------ any size, stride and address
+// 128 columns (64 features' gate and up) by 128 or 64 rows, by way of registers: pieces of 16 bytes are loaded from wherever they lie and wait there, DEPTH chunks of 64 places of the sum
+// ahead, then go where a copy would have put them.  Places of rows and features are found once a tile; behind a tile's last row or feature the last one is loaded again, and the
+// results that it gives go nowhere.  Only the last chunk looks where its rows end.
+template <int DIR, class S, int KEEP, int DEPTH>
+__device__ __forceinline__ void gated_any(const Args& p, const Gate& gate, const Tile& t, lds_ptr lds)
 {
-    product_tiles_any<DIR, bf16_t>(p, gate, units, ct, 1, Shares{}, nullptr);
+    constexpr bool A_ACROSS = DIR != FORWARD;
+    constexpr int AU = S::COLS / 64, BU = S::ROWS / 64, EACH = 8 / S::WAVES, UA = A_ACROSS ? YUNIT : XUNIT, UB = XUNIT, FA = S::FA, NB = S::NB;
+    constexpr uint32_t BUF = BUF_BYTES<DIR, S>;
+    using lds_u32x4 = __attribute__((address_space(3))) u32x4;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, q = lane & 31, hk = lane >> 5, cg = wave % S::CG, rg = wave / S::CG;
+    const int h = gate.h, nchunk = (t.depth + 63) / 64, along = (lane & 7) * 8;
+    const bf16_t *a_at[AU][EACH], *b_at[BU][EACH];
+    int a_left[AU];                                            // backward: columns from the piece's first
+    const bf16_t* const w = p.a + size_t(t.e) * size_t(p.N) * size_t(p.K);
+    if (nchunk > 0) {
+#pragma unroll
+        for (int j = 0; j < EACH; ++j) {
+            const int block = wave + j * S::WAVES, s_q = copied_row(block, lane);
+#pragma unroll
+            for (int i = 0; i < AU; ++i) {
+                if constexpr (DIR == FORWARD) {
+                    const int feature = min(t.c0 + (i * 2 + (lane >> 5)) * 16 + pair_feature(s_q), h - 1);
+                    a_at[i][j] = w + (size_t(s_q >> 4) * size_t(h) + size_t(feature)) * size_t(p.K) + along;
+                } else {
+                    const int col = t.c0 + i * 64 + along;
+                    a_left[i] = h - col;
+                    a_at[i][j] = w + size_t(min(copied_place(block, lane), t.depth - 1)) * size_t(p.K) + min(col, h - 1);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < BU; ++i) b_at[i][j] = p.b + p.g.row(t.begin + min(i * 64 + (lane >> 5) * 32 + s_q, t.rows - 1)) * p.b_stride + along;
+        }
+    }
+    struct Chunk { u32x4 a[AU][EACH], b[BU][EACH]; } chunks[DEPTH];
+    const u32x4 none = {0u, 0u, 0u, 0u};
+    auto load = [&](Chunk& to, int c) {
+        if (c >= nchunk) return;
+        const size_t z = size_t(c) * 64;
+        if (c < nchunk - 1 && (!A_ACROSS || h >= 8)) {
+#pragma unroll
+            for (int j = 0; j < EACH; ++j) {
+                // (a piece of the weights that reaches over its row's end has the next row's beginning there, in columns that go nowhere; there is a next row, of eight columns or more)
+#pragma unroll
+                for (int i = 0; i < AU; ++i) to.a[i][j] = load_piece(a_at[i][j] + (A_ACROSS ? z * size_t(p.K) : z), 8);
+#pragma unroll
+                for (int i = 0; i < BU; ++i) to.b[i][j] = load_piece(b_at[i][j] + z, 8);
+            }
+            return;
+        }
+        const int rest = t.depth - int(z) - along;
+#pragma unroll
+        for (int j = 0; j < EACH; ++j) {
+            const int place = int(z) + copied_place(wave + j * S::WAVES, lane);
+#pragma unroll
+            for (int i = 0; i < AU; ++i) {
+                if constexpr (!A_ACROSS) to.a[i][j] = rest > 0 ? load_piece(a_at[i][j] + z, rest) : none;
+                else to.a[i][j] = place < t.depth && a_left[i] > 0 ? load_piece(w + size_t(place) * size_t(p.K) + (h - a_left[i]), a_left[i]) : none;
+            }
+#pragma unroll
+            for (int i = 0; i < BU; ++i) to.b[i][j] = rest > 0 ? load_piece(b_at[i][j] + z, rest) : none;
+        }
+    };
+    auto write = [&](const Chunk& from, lds_ptr to) {
+#pragma unroll
+        for (int j = 0; j < EACH; ++j) {
+            const int block = wave + j * S::WAVES;
+#pragma unroll
+            for (int i = 0; i < AU; ++i) *(lds_u32x4*)(to + uint32_t(i * UA + block * (A_ACROSS ? YBLOCK : XBLOCK) + lane * 16)) = from.a[i][j];
+#pragma unroll
+            for (int i = 0; i < BU; ++i) *(lds_u32x4*)(to + uint32_t(AU * UA + i * UB + block * XBLOCK + lane * 16)) = from.b[i][j];
+        }
+    };
+    const uint32_t a_slot = uint32_t(cg * FA / 2 * UA) + (A_ACROSS ? places_at(lane, false) : fragment_at(q, hk)), b_slot = uint32_t(AU * UA) + fragment_at(q, hk);
+    f32x16 acc[FA][NB];
+#pragma unroll
+    for (int a = 0; a < FA; ++a)
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.f;
+#pragma unroll
+    for (int n = 0; n < DEPTH; ++n) load(chunks[n], n);
+    uint32_t at = 0;
+    auto one = [&](Chunk& chunk, int c) {
+        if (c >= nchunk) return;
+        write(chunk, lds + at);
+        meet();                                                // (who is still at the other place's chunk has not written this one's successor)
+        load(chunk, c + DEPTH);
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+            bf16x8 af[FA], bf[NB];
+#pragma unroll
+            for (int a = 0; a < FA; ++a) {
+                if constexpr (A_ACROSS) af[a] = read_across(lds + (at + a_slot + uint32_t(a / 2 * UA + a % 2 * 64 + ks * 2 * YBLOCK)));
+                else af[a] = read_along(lds + (at + a_slot + uint32_t(a / 2 * UA + a % 2 * 512 + ks * 32)));
+            }
+#pragma unroll
+            for (int b = 0; b < NB; ++b) bf[b] = read_along(lds + (at + b_slot + uint32_t((b * S::RG + rg) / 2 * UB + (b * S::RG + rg) % 2 * 512 + ks * 32)));
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int a = 0; a < FA; ++a) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(af[a], bf[b], acc[a][b], 0, 0, 0);
+        }
+        at = BUF - at;
+    };
+#pragma unroll 1
+    for (int c = 0; c < nchunk; c += DEPTH)
+#pragma unroll
+        for (int n = 0; n < DEPTH; ++n) one(chunks[n], c + n);
+    meet();
+    constexpr int ROOM = int(2 * BUF / S::WAVES / 16 * 16);
+    if constexpr (DIR == FORWARD) leave_pairs<S, NB, KEEP, false, ROOM>(acc, gate, p, t, lds + uint32_t(wave * ROOM), nchunk > 0, lane, cg, rg);
+    else leave_grads<S, NB, KEEP, false, ROOM>(acc, gate, p, t, lds + uint32_t(wave * ROOM), nchunk > 0, lane, cg, rg);
+}
+template <int DIR, class S, int KEEP>
+__global__ __launch_bounds__(S::THREADS, S::SIMD) void k_gated_any(Args p, GateKeeping<KEEP> gate, int units, int ct)
+{
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
+    const Place w = walk<1>(int(blockIdx.x), units / ct, ct);
+    const Piece at = counted(p.g.M, p.g.E) ? count_pieces(p.g, S::ROWS, w.row, reinterpret_cast<int*>(lds_raw)) : find_piece(p.g, S::ROWS, w.row);
+    if (at.rows > 0)
+        gated_any<DIR, S, KEEP, 3>(p, gate, Tile{at.e, at.begin, at.rows, w.col * (DIR == FORWARD ? S::COLS / 2 : S::COLS), 0, at.e < p.g.E ? (DIR == FORWARD ? p.K : p.N) : 0, -1}, (lds_ptr)lds_raw);
 }
 
+// ------------------------------------------------------------------------------------------ K and h multiples of 8, rows on 16-byte borders
 template <int DIR, class S, int KEEP>
 __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_gated(Args p, GateKeeping<KEEP> gate, int units, int ct)
 {
@@ -34,7 +155,9 @@ int check_pre(const moe_gated_shape* s, const moe_gated_pre* p, const std::strin
     if ((p->dtype == DYNB_BF16 && odd(p->rows)) || (p->dtype == DYNB_I8 && odd(p->scale))) return fail(DYNB_E_INVAL, who + ": misaligned pre");
     return DYNB_OK;
 }
-Gate gate_of(const moe_gated_shape* s, const moe_gated_pre* p, void* hidden, int64_t hidden_stride)
+constexpr int64_t PAST = 64 << 20;                             // bytes of results from which they go past the caches (put_eight)
+// written: bytes of results for a row's feature
+Gate gate_of(const moe_gated_shape* s, const moe_gated_pre* p, void* hidden, int64_t hidden_stride, int written)
 {
     constexpr double LOG2E = 1.4426950408889634, C = 1.5957691216057308;                   // 2 sqrt(2 / pi)
     const double a = s->flags == MOE_GATE_GELU ? C : 1.0, b = s->flags == MOE_GATE_GELU ? C * 0.044715 : 0.0;
@@ -50,6 +173,7 @@ Gate gate_of(const moe_gated_shape* s, const moe_gated_pre* p, void* hidden, int
     }
     g.hidden = static_cast<bf16_t*>(hidden);
     g.hidden_stride = hidden_stride;
+    g.past = int64_t(s->M) * s->h * written >= PAST;
     return g;
 }
 
@@ -69,41 +193,45 @@ int launch_with(K kernel, std::atomic<bool>* asked, uint32_t lds, int64_t grid, 
     return launched(who);
 }
 
+template <int DIR, class S, int KEEP, bool ANY>
+int launch_kind(const moe_product_shape* s, const Args& p, const Gate& gate, hipStream_t st, const char* who)
+{
+    static std::atomic<bool> asked[64];
+    const int wide = DIR == FORWARD ? S::COLS / 2 : S::COLS, ct = (gate.h + wide - 1) / wide;
+    const int64_t units = (S::BIG ? int64_t(s->M) / S::ROWS + s->E + 1 : most_pieces(s->M, s->E, S::ROWS)) * ct;
+    if (units > MOST_GROUPS) return fail(DYNB_E_UNSUPPORTED, std::string(who) + ": too many results");
+    GateKeeping<KEEP> g = {};
+    static_cast<Gate&>(g) = gate;
+    const int64_t grid = S::BIG ? std::min<int64_t>(units, CUS) : units;
+    if constexpr (ANY) return launch_with(k_gated_any<DIR, S, KEEP>, asked, 2 * BUF_BYTES<DIR, S>, grid, S::THREADS, st, who, p, g, int(units), ct);
+    else return launch_with(k_gated<DIR, S, KEEP>, asked, LDS_BYTES<DIR, S>, grid, S::THREADS, st, who, p, g, int(units), ct);
+}
+
+using AnyMid = Kind<2, 2, 2, 2, 2, 2>;   // 128 x 128
+using AnyFew = Kind<2, 1, 2, 2, 2, 2>;   // 128 columns x 64 rows
+
 template <int DIR>
 int launch_gated(const moe_product_shape* s, const Args& p, const Gate& gate, bool fast, hipStream_t st, const char* who)
 {
-    auto launch = [&](auto kind, auto keep) {
+    auto keeping = [&](auto kind, auto any) {
         using S = decltype(kind);
-        constexpr int KEEP = decltype(keep)::value;
-        static std::atomic<bool> asked[64];
-        const int wide = DIR == FORWARD ? S::COLS / 2 : S::COLS, ct = (gate.h + wide - 1) / wide;
-        const int64_t units = (S::BIG ? int64_t(s->M) / S::ROWS + s->E + 1 : most_pieces(s->M, s->E, S::ROWS)) * ct;
-        if (units > MOST_GROUPS) return fail(DYNB_E_UNSUPPORTED, std::string(who) + ": too many results");
-        GateKeeping<KEEP> g = {};
-        static_cast<Gate&>(g) = gate;
-        return launch_with(k_gated<DIR, S, KEEP>, asked, LDS_BYTES<DIR, S>, S::BIG ? std::min<int64_t>(units, CUS) : units, S::THREADS, st, who, p, g, int(units), ct);
-    };
-    auto keeping = [&](auto kind) {
-        if (gate.keep == KEEP_8) return launch(kind, std::integral_constant<int, KEEP_8>{});
-        if constexpr (DIR == FORWARD)
-            if (gate.keep == KEEP_NOTHING) return launch(kind, std::integral_constant<int, KEEP_NOTHING>{});
-        return launch(kind, std::integral_constant<int, KEEP_BF16>{});
-    };
-    if (fast) switch (kind_of(s, DIR == FORWARD ? s->N : s->K, DIR == FORWARD ? s->K : s->N)) {
-        case BIG: return keeping(Big{});
-        case MID: return keeping(Mid{});
-        default:
-            if constexpr (DIR == FORWARD) {                    // (8 bits: 32 features have to be a wave's)
-                if (gate.keep == KEEP_8) return launch(Mid{}, std::integral_constant<int, KEEP_8>{});
-                if (gate.keep == KEEP_NOTHING) return launch(Few{}, std::integral_constant<int, KEEP_NOTHING>{});
-                return launch(Few{}, std::integral_constant<int, KEEP_BF16>{});
-            } else return keeping(Few{});
+        constexpr bool ANY = decltype(any)::value;
+        if (gate.keep == KEEP_8) {
+            // (8 bits: 32 features have to be a wave's)
+            if constexpr (DIR == FORWARD && S::FA < 2) return launch_kind<DIR, Mid, KEEP_8, ANY>(s, p, gate, st, who);
+            else return launch_kind<DIR, S, KEEP_8, ANY>(s, p, gate, st, who);
         }
-    static std::atomic<bool> asked[64];
-    const int wide = DIR == FORWARD ? Mid::COLS / 2 : Mid::COLS, ct = (gate.h + wide - 1) / wide;
-    const int64_t units = most_pieces(s->M, s->E, Mid::ROWS) * ct;
-    if (units > MOST_GROUPS) return fail(DYNB_E_UNSUPPORTED, std::string(who) + ": too many results");
-    return launch_with(k_gated_any<DIR>, asked, LDS_BYTES<DIR, Mid>, units, 256, st, who, p, gate, int(units), ct);
+        if constexpr (DIR == FORWARD)
+            if (gate.keep == KEEP_NOTHING) return launch_kind<DIR, S, KEEP_NOTHING, ANY>(s, p, gate, st, who);
+        return launch_kind<DIR, S, KEEP_BF16, ANY>(s, p, gate, st, who);
+    };
+    const KindOf kind = kind_of(s, DIR == FORWARD ? s->N : s->K, DIR == FORWARD ? s->K : s->N);
+    if (!fast) return kind == FEW ? keeping(AnyFew{}, std::true_type{}) : keeping(AnyMid{}, std::true_type{});
+    switch (kind) {
+    case BIG: return keeping(Big{}, std::false_type{});
+    case MID: return keeping(Mid{}, std::false_type{});
+    default: return keeping(Few{}, std::false_type{});
+    }
 }
 
 // whether what is kept lies on borders of 8 elements
@@ -131,7 +259,7 @@ extern "C" int moe_gated(const moe_gated_shape* s, const moe_groups* g, const vo
     // (32-bit offsets within an expert's two matrices: up's rows lie h rows behind gate's)
     const bool fast = s->K % 8 == 0 && s->h % 8 == 0 && in_stride % 8 == 0 && out_stride % 8 == 0 && on_16({in, W, out}) && kept_on_8(pre) && reached(g, in_stride, 0) &&
                       (int64_t(s->h) + 256) * s->K * 2 < int64_t(1) << 32;
-    return launch_gated<FORWARD>(&as, p, gate_of(s, pre, nullptr, 0), fast, static_cast<hipStream_t>(stream), "moe_gated");
+    return launch_gated<FORWARD>(&as, p, gate_of(s, pre, nullptr, 0, !pre ? 2 : pre->dtype == DYNB_BF16 ? 6 : 4), fast, static_cast<hipStream_t>(stream), "moe_gated");
 }
 
 extern "C" int moe_gated_grad(const moe_gated_shape* s, const moe_groups* g, const void* dout, int64_t dout_stride, const void* W, const moe_gated_pre* pre, void* dpre, int64_t dpre_stride,
@@ -150,5 +278,5 @@ extern "C" int moe_gated_grad(const moe_gated_shape* s, const moe_groups* g, con
     const Args p = {groups_of(&as, g), static_cast<const bf16_t*>(W), static_cast<const bf16_t*>(dout), 0, dout_stride, nullptr, 0, dpre, dpre_stride, as.K, as.N, 0};
     const bool fast = s->K % 8 == 0 && s->h % 8 == 0 && dout_stride % 8 == 0 && dpre_stride % 8 == 0 && hidden_stride % 8 == 0 && on_16({dout, W, dpre, hidden}) && kept_on_8(pre) &&
                       reached(g, 0, dout_stride);
-    return launch_gated<GRAD_INPUT>(&as, p, gate_of(s, pre, hidden, hidden_stride), fast, static_cast<hipStream_t>(stream), "moe_gated_grad");
+    return launch_gated<GRAD_INPUT>(&as, p, gate_of(s, pre, hidden, hidden_stride, hidden ? 6 : 4), fast, static_cast<hipStream_t>(stream), "moe_gated_grad");
 }

@@ -27,10 +27,148 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_product(Args p, int uni
 {
     product_tiles<DIR, TO, S, FUSED>(p, NoGate{}, units, ct, rt, shares, partial);
 }
+
+// ------------------------------------------------------------------------------------------ any size, stride and address
+// Mid's tiles and its places in LDS, by way of registers: pieces of 16 bytes are loaded from wherever they lie (rows of odd length lie between the borders that a copy
+// straight into LDS keeps to), the last of a row element by element, a chunk ahead.  65536 rows, 1001 -> 1501, one expert: 465 us forward, 485 the input's
+// gradient, 855 the weights', where 1000 -> 1504 takes 231, 207 and 241 through k_product, whose tiles
+// of 256 x 256 read either operand half as often and have their next chunk on its way without registers (what share each has was not taken apart).
 template <int DIR, typename TO>
 __global__ __launch_bounds__(256, 2) void k_product_any(Args p, int units, int ct, int rt, Shares shares, float* __restrict__ partial)
 {
-    product_tiles_any<DIR, TO>(p, NoGate{}, units, ct, rt, shares, partial);
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
+    using S = Mid;
+    constexpr bool A_ACROSS = DIR != FORWARD, B_ACROSS = DIR == GRAD_WEIGHT;
+    constexpr int U = 2, EACH = 2, UA = A_ACROSS ? YUNIT : XUNIT, UB = B_ACROSS ? YUNIT : XUNIT;
+    constexpr uint32_t BUF = BUF_BYTES<DIR, S>;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, q = lane & 31, hk = lane >> 5, cg = wave % 2, rg = wave / 2;
+    const int cols = DIR == FORWARD ? p.N : p.K;
+    const lds_ptr lds = (lds_ptr)lds_raw;
+    using lds_u32x4 = __attribute__((address_space(3))) u32x4;
+
+    u32x4 a_piece[U][EACH], b_piece[U][EACH];
+    auto load = [&](const Tile& t, int z0) {
+        const u32x4 none = {0u, 0u, 0u, 0u};
+        const size_t w = size_t(t.e) * size_t(p.N) * size_t(p.K);
+#pragma unroll
+        for (int j = 0; j < EACH; ++j) {
+            const int block = wave + j * S::WAVES, s_q = copied_row(block, lane), z = z0 + copied_place(block, lane), along = z0 + (lane & 7) * 8, rest = t.depth - along;
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const int a_col = t.c0 + i * 64 + (lane & 7) * 8, row = i * 64 + (lane >> 5) * 32 + s_q;
+                if constexpr (DIR == FORWARD) {                // (the features in the order that gives a lane 16 neighbours)
+                    const int feature = t.c0 + i * 64 + (lane >> 5) * 32 + (s_q >> 2 & 1) * 16 + (s_q >> 3) * 4 + (s_q & 3);
+                    a_piece[i][j] = feature < cols && rest > 0 ? load_piece(p.a + w + size_t(feature) * size_t(p.K) + along, rest) : none;
+                    b_piece[i][j] = row < t.rows && rest > 0 ? load_piece(p.b + p.g.row(t.begin + row) * p.b_stride + along, rest) : none;
+                } else if constexpr (DIR == GRAD_INPUT) {
+                    a_piece[i][j] = z < t.depth && a_col < cols ? load_piece(p.a + w + size_t(z) * size_t(p.K) + a_col, cols - a_col) : none;
+                    b_piece[i][j] = row < t.rows && rest > 0 ? load_piece(p.b + int64_t(t.begin + row) * p.b_stride + along, rest) : none;
+                } else {
+                    const int b_col = t.r0 + i * 64 + (lane & 7) * 8;
+                    a_piece[i][j] = z < t.depth && a_col < cols ? load_piece(p.a + p.g.row(t.begin + z) * p.a_stride + a_col, cols - a_col) : none;
+                    b_piece[i][j] = z < t.depth && b_col < p.N ? load_piece(p.b + int64_t(t.begin + z) * p.b_stride + b_col, p.N - b_col) : none;
+                }
+            }
+        }
+    };
+    auto write = [&](lds_ptr to) {
+#pragma unroll
+        for (int j = 0; j < EACH; ++j)
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const int block = wave + j * S::WAVES;
+                *(lds_u32x4*)(to + uint32_t(i * UA + block * (A_ACROSS ? YBLOCK : XBLOCK) + lane * 16)) = a_piece[i][j];
+                *(lds_u32x4*)(to + uint32_t(U * UA + i * UB + block * (B_ACROSS ? YBLOCK : XBLOCK) + lane * 16)) = b_piece[i][j];
+            }
+    };
+    const uint32_t a_slot = uint32_t(cg * UA) + (A_ACROSS ? places_at(lane, false) : fragment_at(q, hk));
+    const uint32_t b_slot = uint32_t(U * UA) + uint32_t(rg * (B_ACROSS ? 64 : 512)) + (B_ACROSS ? places_at(lane, true) : fragment_at(q, hk));
+
+    auto work = [&](const Tile& t) {
+        f32x16 acc[2][2];
+#pragma unroll
+        for (int i = 0; i < 64; ++i) acc[i >> 5][i >> 4 & 1][i & 15] = 0.f;
+        if (t.depth > 0) load(t, 0);
+        uint32_t at = 0;
+        for (int z0 = 0; z0 < t.depth; z0 += 64) {
+            write(lds + at);
+            __syncthreads();                                   // (who is still at the other place's chunk has not written this one's successor)
+            if (z0 + 64 < t.depth) load(t, z0 + 64);
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) {
+                bf16x8 af[2], bf[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    // (rows: block i of this wave is the i-th unit's fragment rg)
+                    if constexpr (A_ACROSS) af[i] = read_across(lds + at + a_slot + uint32_t(i * 64 + ks * 2 * YBLOCK));
+                    else af[i] = read_along(lds + at + a_slot + uint32_t(i * 512 + ks * 32));
+                    if constexpr (B_ACROSS) bf[i] = read_across(lds + at + b_slot + uint32_t(i * UB + ks * 2 * YBLOCK));
+                    else bf[i] = read_along(lds + at + b_slot + uint32_t(i * UB + ks * 32));
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[i & 1][i >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(af[i & 1], bf[i >> 1], acc[i & 1][i >> 1], 0, 0, 0);
+            }
+            at = BUF - at;
+        }
+        __syncthreads();
+        const lds_ptr mine_at = lds + uint32_t(wave) * (2 * BUF / S::WAVES / 16 * 16);
+        auto put = [&](auto* to, int64_t pitch) {
+            using T = std::remove_pointer_t<decltype(to)>;
+            constexpr int P = PIECE<T>, LANES = 64 / P, AT_ONCE = 64 / LANES, PITCH = 64 * int(sizeof(T)) + 16;
+            static_assert(32 * PITCH <= int(2 * BUF / S::WAVES), "room");
+            const int col = lane % LANES * P, row = lane / LANES, first = t.c0 + cg * 64, left = cols - first - col;
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                    float v = acc[i >> 4][b][i & 15];
+                    if (DIR == FORWARD && p.relu) v = v < 0.f ? 0.f : v;                                     // (a NaN stays one)
+                    const lds_ptr here = mine_at + uint32_t(q * PITCH + ((i >> 4) * 32 + 16 * hk + (i & 15)) * int(sizeof(T)));
+                    if constexpr (sizeof(T) == 4) *(__attribute__((address_space(3))) float*)here = v;
+                    else *(__attribute__((address_space(3))) bf16_t*)here = f32_to_bf16(v);
+                }
+                wave_sync();
+                for (int i = 0; i < 32; i += AT_ONCE) {
+                    const int r = (b * 2 + rg) * 32 + row + i;
+                    if (r >= t.rows || left <= 0) continue;
+                    const u32x4 v = *(const lds_u32x4*)(mine_at + uint32_t((row + i) * PITCH + col * int(sizeof(T))));
+                    u32x4 act;
+                    const bool masked = DIR == GRAD_INPUT && p.act;
+                    if (masked) act = load_piece(p.act + int64_t(t.begin + r) * p.act_stride + first + col, left);
+                    float w[P];
+#pragma unroll
+                    for (int j = 0; j < P; ++j) {
+                        w[j] = element<T>(v, j);
+                        if (masked && !(element<bf16_t>(act, j) > 0.f)) w[j] = 0.f;
+                    }
+                    store_piece<P>(to + int64_t(r) * pitch + first + col, left, w);
+                }
+                wave_sync();
+            }
+        };
+        if constexpr (DIR == GRAD_WEIGHT) {
+            const size_t all = size_t(p.N) * size_t(p.K), row = size_t(t.r0) * size_t(p.K);
+            if (t.slot >= 0) put(partial + size_t(t.slot) * all + row, p.K);
+            else put(static_cast<TO*>(p.out) + size_t(t.e) * all + row, p.K);
+        } else put(static_cast<TO*>(p.out) + int64_t(t.begin) * p.out_stride, p.out_stride);
+        __syncthreads();
+    };
+    if constexpr (DIR == GRAD_WEIGHT) {
+        const int w_lane = int(blockIdx.x) / (ct * rt);
+        const Place at = walk<4>(int(blockIdx.x) % (ct * rt), rt, ct);
+        const int64_t from = shares.each * w_lane, to = from + shares.each;
+        for (int e = group_at(p.g, shares, from); e < p.g.E && start_of(p.g, shares, e) < to; ++e) {
+            const int a = p.g.begin(e), n = max(p.g.begin(e + 1) - a, 0);
+            const int64_t s = start_of(p.g, shares, e), first = s + shares.extra;
+            const int lo = int(min(max(from - first, int64_t(0)), int64_t(n))), hi = int(min(max(to - first, int64_t(0)), int64_t(n)));
+            if (n == 0 ? s < from : hi <= lo) continue;
+            work(Tile{e, a + lo, min(p.N - at.row * S::ROWS, S::ROWS), at.col * S::COLS, at.row * S::ROWS, hi - lo, hi - lo == n ? -1 : 2 * w_lane + (lo > 0 ? 0 : 1)});
+        }
+    } else {
+        const Place w = walk<1>(int(blockIdx.x), units / ct, ct);
+        const Piece at = counted(p.g.M, p.g.E) ? count_pieces(p.g, S::ROWS, w.row, reinterpret_cast<int*>(lds_raw)) : find_piece(p.g, S::ROWS, w.row);
+        if (at.rows > 0) work(Tile{at.e, at.begin, at.rows, w.col * S::COLS, 0, at.e < p.g.E ? (DIR == FORWARD ? p.K : p.N) : 0, -1});
+    }
 }
 
 // Gradients whose sum a border between two lanes cuts: their parts, in order.  A workgroup looks after a share of the elements for one border, and only for the

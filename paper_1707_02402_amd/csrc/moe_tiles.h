@@ -214,74 +214,90 @@ __device__ __forceinline__ Place walk(int u, int rows, int ct)
     return Place{group * TALL + in % tall, in / tall};
 }
 
-// A kept pair's gate and up, features c .. c + 7 of a row (`left` of them are there), as they lie and as numbers
-template <int KEEP>
+// Eight features of a row to or from anywhere: `left` of them are there (at least one).  WHOLE: all eight, and on a border of eight.
+// past: results that no cache will hold for who reads them next go past the caches, and leave them to the operands (65536 rows, 1024 -> 2 x 2048, 64 experts: forward
+// 614 -> 598 us, with the pair kept in bfloat16 696 -> 654, backward 496 -> 478; what fits the caches is read from them by the next call, and leaves as usual).
+template <bool WHOLE, bool PAST>
+__device__ __forceinline__ void put_eight(bf16_t* p, int left, const u32x4& v)
+{
+    if constexpr (WHOLE && PAST) __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(p));
+    else if constexpr (WHOLE) *reinterpret_cast<u32x4*>(p) = v;
+    else if (left >= 8) *reinterpret_cast<u32x4_at2*>(p) = v;
+    else
+#pragma unroll
+        for (int i = 0; i < 7; ++i)
+            if (i < left) p[i] = bf16_t(v[i >> 1] >> (16 * (i & 1)));
+}
+template <bool WHOLE, bool PAST>
+__device__ __forceinline__ void put_eight(int8_t* p, int left, const u32x2& v)
+{
+    if constexpr (WHOLE && PAST) __builtin_nontemporal_store(v, reinterpret_cast<u32x2*>(p));
+    else if constexpr (WHOLE) *reinterpret_cast<u32x2*>(p) = v;
+    else store_eight(p, left, v);
+}
+// (the compiler would make one store of the two, and an ordinary one)
+template <class F>
+__device__ __forceinline__ void put_past(bool past, F put)
+{
+    if (past) {
+        asm volatile("; past the caches" ::: "memory");
+        put(std::true_type{});
+        asm volatile("" ::: "memory");
+    } else put(std::false_type{});
+}
+// ... of a kept pair's gate and up, as they lie and as numbers
+template <int KEEP, bool WHOLE>
 struct KeptEight {
     u32x4 g, u;
     __device__ __forceinline__ void load(const Gate& gate, int64_t row, int c, int left)
     {
         const bf16_t* const from = static_cast<const bf16_t*>(gate.pre) + row * gate.pre_stride + c;
-        g = load_piece(from, left);
-        u = load_piece(from + gate.h, left);
+        g = load_piece(from, WHOLE ? 8 : left);
+        u = load_piece(from + gate.h, WHOLE ? 8 : left);
     }
     __device__ __forceinline__ float gate_at(int i) const { return element<bf16_t>(g, i); }
     __device__ __forceinline__ float up_at(int i) const { return element<bf16_t>(u, i); }
 };
-template <>
-struct KeptEight<KEEP_8> {
+template <bool WHOLE>
+struct KeptEight<KEEP_8, WHOLE> {
     u32x2 g, u;
     bf16_t sg, su;
     __device__ __forceinline__ void load(const Gate& gate, int64_t row, int c, int left)
     {
         const int8_t* const from = static_cast<const int8_t*>(gate.pre) + row * gate.pre_stride + c;
         const bf16_t* const scale = gate.scale + row * gate.scale_stride + c / BLOCK8;
-        g = load_eight(from, left);
-        u = load_eight(from + gate.h, left);
+        g = load_eight(from, WHOLE ? 8 : left);
+        u = load_eight(from + gate.h, WHOLE ? 8 : left);
         sg = scale[0];
         su = scale[gate.blocks()];
     }
     __device__ __forceinline__ float gate_at(int i) const { return unpack8(g[i >> 2], i & 3) * bf16_to_f32(sg); }
     __device__ __forceinline__ float up_at(int i) const { return unpack8(u[i >> 2], i & 3) * bf16_to_f32(su); }
 };
-// The gradients of gate and up of eight features, and f(gate) up, for dact(i), the gradient of feature i.  alive: 0 for a row of no group, whose results are 0 whatever was
-// kept there
-template <int KEEP, class F>
-__device__ __forceinline__ void grad_of_eight(const Gate& gate, const KeptEight<KEEP>& kept, bool grouped, F dact, float* dg, float* du, float* f)
-{
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float u = kept.up_at(i), d = dact(i);
-        const GateValue v = gate_both(gate.form, kept.gate_at(i));
-        dg[i] = grouped ? d * u * v.slope : 0.f;
-        du[i] = grouped ? d * v.f : 0.f;
-        f[i] = grouped ? v.f * u : 0.f;
-    }
-}
 __device__ __forceinline__ u32x4 pack_eight(const float* v) { return u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])}; }
 
-// How a gated layer's tile leaves (h and all rows on borders of 8 elements).  Like a product's, by way of LDS, each wave its own share `room` of the last chunk's place,
-// block of 32 rows after block.
+// How a gated layer's tile leaves: like a product's, by way of LDS, each wave its own `room` (the fast tiles': its share of the last chunk's place), block of 32 rows after block.
+// WHOLE: h and all rows are on borders of eight elements.
 //
 // Forward: a lane's sums are gate and up of the same eight features.  What is kept in 8 bits shares scales among the 32 features of two blocks of columns, which the
-// two halves of the wave have.  nchunk 0: rows of no group, zeros, and the LDS is the next tile's.
-template <class S, int LIVE, int KEEP>
-__device__ __forceinline__ void leave_pairs(const f32x16 (&acc)[S::FA][LIVE > 0 ? LIVE : 1], const Gate& gate, const Args& p, const Tile& now, lds_ptr room, int nchunk, int lane, int cg, int rg)
+// two halves of the wave have.  summed false: rows of no group, zeros, and the LDS is not this wave's.
+template <class S, int LIVE, int KEEP, bool WHOLE, int ROOM>
+__device__ __forceinline__ void leave_pairs(const f32x16 (&acc)[S::FA][LIVE > 0 ? LIVE : 1], const Gate& gate, const Args& p, const Tile& now, lds_ptr room, bool summed, int lane, int cg, int rg)
 {
     using lds_u32x4 = __attribute__((address_space(3))) u32x4;
     using lds_u32x2 = __attribute__((address_space(3))) u32x2;
     constexpr int FA = S::FA, PARTS = KEEP == KEEP_BF16 ? 3 : 1, PITCH = FA * 32 + 16, PART = 32 * PITCH, PITCH8 = FA * 16 + 16, PART8 = 32 * PITCH8;
     constexpr int LANES = FA * 2, AT_ONCE = 64 / LANES, STORES = 32 / AT_ONCE;
     static_assert(KEEP != KEEP_8 || FA % 2 == 0, "a block of 32 features");
-    static_assert(PARTS * PART + (KEEP == KEEP_8 ? 2 * PART8 : 0) <= int(BUF_BYTES<FORWARD, S> / S::WAVES), "room");
-    const int q = lane & 31, hk = lane >> 5, h = gate.h, first = now.c0 + cg * (FA * 16), col = lane % LANES * 8, row = lane / LANES;
-    const bool on = first + col < h;
+    static_assert(PARTS * PART + (KEEP == KEEP_8 ? 2 * PART8 : 0) <= ROOM, "room");
+    const int q = lane & 31, hk = lane >> 5, h = gate.h, first = now.c0 + cg * (FA * 16), col = lane % LANES * 8, row = lane / LANES, cols = h - first - col;
     const int64_t from = now.begin + rg * 32;
     const lds_ptr in = room + uint32_t(q * PITCH + hk * 16), in8 = room + uint32_t(PARTS * PART + q * PITCH8 + hk * 8);
     const lds_ptr out = room + uint32_t(row * PITCH + col * 2), out8 = room + uint32_t(PARTS * PART + row * PITCH8 + col);
 #pragma unroll
     for (int b = 0; b < LIVE; ++b) {
         const int block = (b * S::RG) * 32, left = now.rows - block - rg * 32;
-        if (nchunk > 0) {
+        if (summed) {
 #pragma unroll
             for (int a = 0; a < FA; ++a) {
                 float y[8];
@@ -324,33 +340,36 @@ __device__ __forceinline__ void leave_pairs(const f32x16 (&acc)[S::FA][LIVE > 0 
                 if (first + a * 16 < h)
 #pragma unroll
                     for (int s = 0; s < 2; ++s) gate.scale[(from + block + q) * gate.scale_stride + s * gate.blocks() + (first + a * 16) / BLOCK8] = scale8_bits(scale8(0u));
-        const u32x4 none = {0u, 0u, 0u, 0u};
-        bf16_t* const to = static_cast<bf16_t*>(p.out) + (from + block + row) * p.out_stride + first + col;
+        put_past(WHOLE && gate.past, [&](auto past) {
+            constexpr bool PAST = decltype(past)::value;
+            const u32x4 none = {0u, 0u, 0u, 0u};
+            bf16_t* const to = static_cast<bf16_t*>(p.out) + (from + block + row) * p.out_stride + first + col;
 #pragma unroll
-        for (int i = 0; i < STORES; ++i) {
-            const u32x4 v = nchunk > 0 ? *(const lds_u32x4*)(out + uint32_t(i * AT_ONCE * PITCH)) : none;
-            if (row + i * AT_ONCE < left && on) *reinterpret_cast<u32x4*>(to + i * AT_ONCE * p.out_stride) = v;
-        }
-        if constexpr (KEEP == KEEP_BF16) {
-            bf16_t* const pre = static_cast<bf16_t*>(gate.pre) + (from + block + row) * gate.pre_stride + first + col;
+            for (int i = 0; i < STORES; ++i) {
+                const u32x4 v = summed ? *(const lds_u32x4*)(out + uint32_t(i * AT_ONCE * PITCH)) : none;
+                if (row + i * AT_ONCE < left && cols > 0) put_eight<WHOLE, PAST>(to + i * AT_ONCE * p.out_stride, cols, v);
+            }
+            if constexpr (KEEP == KEEP_BF16) {
+                bf16_t* const pre = static_cast<bf16_t*>(gate.pre) + (from + block + row) * gate.pre_stride + first + col;
 #pragma unroll
-            for (int s = 0; s < 2; ++s)
+                for (int s = 0; s < 2; ++s)
 #pragma unroll
-                for (int i = 0; i < STORES; ++i) {
-                    const u32x4 v = nchunk > 0 ? *(const lds_u32x4*)(out + uint32_t((1 + s) * PART + i * AT_ONCE * PITCH)) : none;
-                    if (row + i * AT_ONCE < left && on) *reinterpret_cast<u32x4*>(pre + i * AT_ONCE * gate.pre_stride + s * h) = v;
-                }
-        }
-        if constexpr (KEEP == KEEP_8) {
-            int8_t* const pre = static_cast<int8_t*>(gate.pre) + (from + block + row) * gate.pre_stride + first + col;
+                    for (int i = 0; i < STORES; ++i) {
+                        const u32x4 v = summed ? *(const lds_u32x4*)(out + uint32_t((1 + s) * PART + i * AT_ONCE * PITCH)) : none;
+                        if (row + i * AT_ONCE < left && cols > 0) put_eight<WHOLE, PAST>(pre + i * AT_ONCE * gate.pre_stride + s * h, cols, v);
+                    }
+            }
+            if constexpr (KEEP == KEEP_8) {
+                int8_t* const pre = static_cast<int8_t*>(gate.pre) + (from + block + row) * gate.pre_stride + first + col;
 #pragma unroll
-            for (int s = 0; s < 2; ++s)
+                for (int s = 0; s < 2; ++s)
 #pragma unroll
-                for (int i = 0; i < STORES; ++i) {
-                    const u32x2 v = nchunk > 0 ? *(const lds_u32x2*)(out8 + uint32_t(s * PART8 + i * AT_ONCE * PITCH8)) : u32x2{0u, 0u};
-                    if (row + i * AT_ONCE < left && on) *reinterpret_cast<u32x2*>(pre + i * AT_ONCE * gate.pre_stride + s * h) = v;
-                }
-        }
+                    for (int i = 0; i < STORES; ++i) {
+                        const u32x2 v = summed ? *(const lds_u32x2*)(out8 + uint32_t(s * PART8 + i * AT_ONCE * PITCH8)) : u32x2{0u, 0u};
+                        if (row + i * AT_ONCE < left && cols > 0) put_eight<WHOLE, PAST>(pre + i * AT_ONCE * gate.pre_stride + s * h, cols, v);
+                    }
+            }
+        });
         wave_sync();
         __builtin_amdgcn_sched_barrier(0);
     }
@@ -358,47 +377,65 @@ __device__ __forceinline__ void leave_pairs(const f32x16 (&acc)[S::FA][LIVE > 0 
 
 // Backward: dact goes through LDS in fp32, unrounded, and meets the kept pair where a lane has eight neighbouring features of a row.  A row has FA * 8 pieces of 16 bytes there,
 // piece j of row q at place j ^ q (of the places that there are), so that neither side's accesses meet in a bank.
-template <class S, int LIVE, int KEEP>
-__device__ __forceinline__ void leave_grads(const f32x16 (&acc)[S::FA][LIVE > 0 ? LIVE : 1], const Gate& gate, const Args& p, const Tile& now, lds_ptr room, int nchunk, int lane, int cg, int rg)
+template <class S, int LIVE, int KEEP, bool WHOLE, int ROOM>
+__device__ __forceinline__ void leave_grads(const f32x16 (&acc)[S::FA][LIVE > 0 ? LIVE : 1], const Gate& gate, const Args& p, const Tile& now, lds_ptr room, bool summed, int lane, int cg, int rg)
 {
     using lds_f32x4 = __attribute__((address_space(3))) f32x4;
     constexpr int FA = S::FA, PIECES = FA * 8, LANES = FA * 4, AT_ONCE = 64 / LANES, STORES = 32 / AT_ONCE;
-    static_assert(32 * PIECES * 16 <= int(BUF_BYTES<GRAD_INPUT, S> / S::WAVES), "room");
-    const int q = lane & 31, hk = lane >> 5, h = gate.h, col = lane % LANES * 8, row = lane / LANES, c = now.c0 + cg * (FA * 32) + col;
-    const bool on = c < h;
-    bf16_t* const out = static_cast<bf16_t*>(p.out);
+    static_assert(32 * PIECES * 16 <= ROOM, "room");
+    const int q = lane & 31, hk = lane >> 5, h = gate.h, col = lane % LANES * 8, row = lane / LANES, c = now.c0 + cg * (FA * 32) + col, cols = h - c;
+    auto put = [&](int64_t at, const u32x4& dg, const u32x4& du, const u32x4& f) {
+        put_past(WHOLE && gate.past, [&](auto past) {
+            constexpr bool PAST = decltype(past)::value;
+            bf16_t* const to = static_cast<bf16_t*>(p.out) + at * p.out_stride + c;
+            put_eight<WHOLE, PAST>(to, cols, dg);
+            put_eight<WHOLE, PAST>(to + h, cols, du);
+            if (gate.hidden) put_eight<WHOLE, PAST>(gate.hidden + at * gate.hidden_stride + c, cols, f);
+        });
+    };
+    if (!summed) {                                             // rows of no group: zeros, whatever was kept; the LDS is not this wave's
+        const u32x4 none = {0u, 0u, 0u, 0u};
+        for (int b = 0; b < LIVE; ++b)
+            for (int r = (b * S::RG + rg) * 32 + row, i = 0; i < 32; i += AT_ONCE)
+                if (r + i < now.rows && cols > 0) put(now.begin + r + i, none, none, none);
+        return;
+    }
 #pragma unroll
     for (int b = 0; b < LIVE; ++b) {
         const int64_t from = now.begin + (b * S::RG + rg) * 32 + row;
-        const int left = now.rows - (b * S::RG + rg) * 32 - row;
-        KeptEight<KEEP> kept[STORES];
+        const int left = cols > 0 ? now.rows - (b * S::RG + rg) * 32 - row : 0;              // a step's row is there if it is below this
+        KeptEight<KEEP, WHOLE> kept[STORES];
 #pragma unroll
-        for (int i = 0; i < STORES; ++i) kept[i].load(gate, from + (left > i * AT_ONCE ? i * AT_ONCE : -row - (b * S::RG + rg) * 32), on ? c : h - 8, 8);
-        if (nchunk > 0)
+        for (int i = 0; i < STORES; ++i)
+            // (behind the last row or feature one that is there, whose results go nowhere: no load waits for a branch)
+            if (WHOLE) kept[i].load(gate, i * AT_ONCE < left ? from + i * AT_ONCE : now.begin, cols > 0 ? c : h - 8, 8);
+            else if (i * AT_ONCE < left) kept[i].load(gate, from + i * AT_ONCE, c, cols);
 #pragma unroll
-            for (int a = 0; a < FA; ++a) {
+        for (int a = 0; a < FA; ++a) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    *(lds_f32x4*)(room + uint32_t((q * PIECES + ((a * 8 + hk * 4 + j) ^ (q & (PIECES - 1)))) * 16)) =
-                        f32x4{acc[a][b][4 * j], acc[a][b][4 * j + 1], acc[a][b][4 * j + 2], acc[a][b][4 * j + 3]};
-                __builtin_amdgcn_sched_barrier(0);
-            }
+            for (int j = 0; j < 4; ++j)
+                *(lds_f32x4*)(room + uint32_t((q * PIECES + ((a * 8 + hk * 4 + j) ^ (q & (PIECES - 1)))) * 16)) =
+                    f32x4{acc[a][b][4 * j], acc[a][b][4 * j + 1], acc[a][b][4 * j + 2], acc[a][b][4 * j + 3]};
+            __builtin_amdgcn_sched_barrier(0);
+        }
         wave_sync();
 #pragma unroll
         for (int i = 0; i < STORES; ++i) {
             const int r = row + i * AT_ONCE;
-            f32x4 d[2] = {};
-            if (nchunk > 0)
+            f32x4 d[2];
 #pragma unroll
-                for (int j = 0; j < 2; ++j) d[j] = *(const lds_f32x4*)(room + uint32_t((r * PIECES + ((col / 4 + j) ^ (r & (PIECES - 1)))) * 16));
+            for (int j = 0; j < 2; ++j) d[j] = *(const lds_f32x4*)(room + uint32_t((r * PIECES + ((col / 4 + j) ^ (r & (PIECES - 1)))) * 16));
+            if (i * AT_ONCE >= left) continue;
             float dg[8], du[8], f[8];
-            grad_of_eight<KEEP>(gate, kept[i], nchunk > 0, [&](int e) { return d[e >> 2][e & 3]; }, dg, du, f);
-            if (i * AT_ONCE < left && on) {
-                const int64_t at = from + i * AT_ONCE;
-                *reinterpret_cast<u32x4*>(out + at * p.out_stride + c) = pack_eight(dg);
-                *reinterpret_cast<u32x4*>(out + at * p.out_stride + h + c) = pack_eight(du);
-                if (gate.hidden) *reinterpret_cast<u32x4*>(gate.hidden + at * gate.hidden_stride + c) = pack_eight(f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float u = kept[i].up_at(e), dact = d[e >> 2][e & 3];
+                const GateValue v = gate_both(gate.form, kept[i].gate_at(e));
+                dg[e] = dact * u * v.slope;
+                du[e] = dact * v.f;
+                f[e] = v.f * u;
             }
+            put(from + i * AT_ONCE, pack_eight(dg), pack_eight(du), pack_eight(f));
         }
         wave_sync();
         __builtin_amdgcn_sched_barrier(0);
@@ -966,8 +1003,8 @@ __device__ __forceinline__ void product_tiles(Args p, G gate, int units, int ct,
                 }
             };
             const int first_col = now.c0 + cg * (FA * 32);
-            if constexpr (PAIRS) leave_pairs<S, LIVE, G::KEEP>(acc, gate, p, now, mine_at, nchunk, lane, cg, rg);
-            else if constexpr (G::ON) leave_grads<S, LIVE, G::KEEP>(acc, gate, p, now, mine_at, nchunk, lane, cg, rg);
+            if constexpr (PAIRS) leave_pairs<S, LIVE, G::KEEP, true, int(BUF / S::WAVES / 16 * 16)>(acc, gate, p, now, mine_at, nchunk > 0, lane, cg, rg);
+            else if constexpr (G::ON) leave_grads<S, LIVE, G::KEEP, true, int(BUF / S::WAVES / 16 * 16)>(acc, gate, p, now, mine_at, nchunk > 0, lane, cg, rg);
             else if constexpr (DIR == GRAD_WEIGHT) {
                 const size_t row = size_t(now.r0) * size_t(p.K) + size_t(first_col), all = size_t(p.N) * size_t(p.K);
                 float* const part = now.slot >= 0 ? partial + size_t(now.slot) * all + row : nullptr;
@@ -992,228 +1029,6 @@ __device__ __forceinline__ void product_tiles(Args p, G gate, int units, int ct,
         now = then;
     }
     answered_but<0>();                                         // (nothing is on its way to LDS that another workgroup may have next)
-}
-
-// ------------------------------------------------------------------------------------------ any size, stride and address
-// Mid's tiles and its places in LDS, by way of registers: pieces of 16 bytes are loaded from wherever they lie (rows of odd length lie between the borders that a copy
-// straight into LDS keeps to), the last of a row element by element, a chunk ahead.  65536 rows, 1001 -> 1501, one expert: 465 us forward, 485 the input's
-// gradient, 855 the weights', where 1000 -> 1504 takes 231, 207 and 241 through k_product, whose tiles
-// of 256 x 256 read either operand half as often and have their next chunk on its way without registers (what share each has was not taken apart).
-// A gated layer's results, each lane's where they belong: of every block b of 32 rows row q, of every block a of 32 columns gate and up of 8 features (forward) or
-// the gradients of 16 hidden features.
-template <int DIR>
-__device__ __forceinline__ void leave_any(const f32x16 (&acc)[2][2], const Gate& gate, const Args& p, const Tile& t, int h, int lane, int cg, int rg)
-{
-    const int q = lane & 31, hk = lane >> 5;
-    bf16_t* const out = static_cast<bf16_t*>(p.out);
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-        const int r = (b * 2 + rg) * 32 + q;
-        const bool there = r < t.rows;
-        const int64_t row = t.begin + r;
-        if constexpr (DIR == FORWARD) {
-            uint32_t largest[2] = {0u, 0u};
-            float v[2][2][8];
-#pragma unroll
-            for (int a = 0; a < 2; ++a) {
-                const int f = t.c0 + (cg * 2 + a) * 16 + 8 * hk;
-                float y[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float g = acc[a][b][i], u = acc[a][b][8 + i];
-                    y[i] = gate_f(gate.form, g) * u;
-                    v[0][a][i] = g;
-                    v[1][a][i] = u;
-                    largest[0] = max(largest[0], magnitude(g));
-                    largest[1] = max(largest[1], magnitude(u));
-                }
-                if (there && f < h) {
-                    store_piece<8>(out + row * p.out_stride + f, h - f, y);
-                    if (gate.keep == KEEP_BF16)
-#pragma unroll
-                        for (int s = 0; s < 2; ++s) store_piece<8>(static_cast<bf16_t*>(gate.pre) + row * gate.pre_stride + s * h + f, h - f, v[s][a]);
-                }
-            }
-            if (gate.keep == KEEP_8)
-#pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    const Scale8 c = scale8(max(largest[s], uint32_t(__shfl_xor(int(largest[s]), 32))));
-#pragma unroll
-                    for (int a = 0; a < 2; ++a) {
-                        const int f = t.c0 + (cg * 2 + a) * 16 + 8 * hk;
-                        const float* const x = v[s][a];
-                        if (there && f < h) store_eight(static_cast<int8_t*>(gate.pre) + row * gate.pre_stride + s * h + f, h - f, u32x2{pack8(x[0], x[1], x[2], x[3], c.inv), pack8(x[4], x[5], x[6], x[7], c.inv)});
-                        if (there && f < h && a == 0 && hk == 0) gate.scale[row * gate.scale_stride + s * gate.blocks() + f / BLOCK8] = scale8_bits(c);
-                    }
-                }
-        } else {
-#pragma unroll
-            for (int n = 0; n < 4; ++n) {
-                const int c = t.c0 + (cg * 2 + (n >> 1)) * 32 + 16 * hk + 8 * (n & 1), left = h - c;
-                if (!there || left <= 0) continue;
-                float dg[8], du[8], f[8];
-                auto both = [&](auto keep) {
-                    KeptEight<decltype(keep)::value> kept;
-                    kept.load(gate, row, c, left);
-                    grad_of_eight(gate, kept, t.depth > 0, [&](int i) { return acc[n >> 1][b][8 * (n & 1) + i]; }, dg, du, f);
-                };
-                if (gate.keep == KEEP_8) both(std::integral_constant<int, KEEP_8>{});
-                else both(std::integral_constant<int, KEEP_BF16>{});
-                store_piece<8>(out + row * p.out_stride + c, left, dg);
-                store_piece<8>(out + row * p.out_stride + h + c, left, du);
-                if (gate.hidden) store_piece<8>(gate.hidden + row * gate.hidden_stride + c, left, f);
-            }
-        }
-    }
-}
-
-template <int DIR, typename TO, class G>
-__device__ __forceinline__ void product_tiles_any(Args p, G gate, int units, int ct, int rt, Shares shares, float* __restrict__ partial)
-{
-    extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
-    using S = Mid;
-    constexpr bool A_ACROSS = DIR != FORWARD, B_ACROSS = DIR == GRAD_WEIGHT;
-    constexpr int U = 2, EACH = 2, UA = A_ACROSS ? YUNIT : XUNIT, UB = B_ACROSS ? YUNIT : XUNIT;
-    constexpr bool PAIRS = G::ON && DIR == FORWARD;
-    constexpr int WIDE = PAIRS ? S::COLS / 2 : S::COLS;
-    constexpr uint32_t BUF = BUF_BYTES<DIR, S>;
-    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, q = lane & 31, hk = lane >> 5, cg = wave % 2, rg = wave / 2;
-    const int cols = PAIRS ? p.N / 2 : DIR == FORWARD ? p.N : p.K;
-    const lds_ptr lds = (lds_ptr)lds_raw;
-    using lds_u32x4 = __attribute__((address_space(3))) u32x4;
-
-    u32x4 a_piece[U][EACH], b_piece[U][EACH];
-    auto load = [&](const Tile& t, int z0) {
-        const u32x4 none = {0u, 0u, 0u, 0u};
-        const size_t w = size_t(t.e) * size_t(p.N) * size_t(p.K);
-#pragma unroll
-        for (int j = 0; j < EACH; ++j) {
-            const int block = wave + j * S::WAVES, s_q = copied_row(block, lane), z = z0 + copied_place(block, lane), along = z0 + (lane & 7) * 8, rest = t.depth - along;
-#pragma unroll
-            for (int i = 0; i < U; ++i) {
-                const int a_col = t.c0 + i * 64 + (lane & 7) * 8, row = i * 64 + (lane >> 5) * 32 + s_q;
-                if constexpr (PAIRS) {
-                    const int feature = t.c0 + (i * 2 + (lane >> 5)) * 16 + pair_feature(s_q);
-                    a_piece[i][j] = feature < cols && rest > 0 ? load_piece(p.a + w + (size_t(s_q >> 4) * size_t(cols) + size_t(feature)) * size_t(p.K) + along, rest) : none;
-                    b_piece[i][j] = row < t.rows && rest > 0 ? load_piece(p.b + p.g.row(t.begin + row) * p.b_stride + along, rest) : none;
-                } else if constexpr (DIR == FORWARD) {         // (the features in the order that gives a lane 16 neighbours)
-                    const int feature = t.c0 + i * 64 + (lane >> 5) * 32 + (s_q >> 2 & 1) * 16 + (s_q >> 3) * 4 + (s_q & 3);
-                    a_piece[i][j] = feature < cols && rest > 0 ? load_piece(p.a + w + size_t(feature) * size_t(p.K) + along, rest) : none;
-                    b_piece[i][j] = row < t.rows && rest > 0 ? load_piece(p.b + p.g.row(t.begin + row) * p.b_stride + along, rest) : none;
-                } else if constexpr (DIR == GRAD_INPUT) {
-                    a_piece[i][j] = z < t.depth && a_col < cols ? load_piece(p.a + w + size_t(z) * size_t(p.K) + a_col, cols - a_col) : none;
-                    b_piece[i][j] = row < t.rows && rest > 0 ? load_piece(p.b + int64_t(t.begin + row) * p.b_stride + along, rest) : none;
-                } else {
-                    const int b_col = t.r0 + i * 64 + (lane & 7) * 8;
-                    a_piece[i][j] = z < t.depth && a_col < cols ? load_piece(p.a + p.g.row(t.begin + z) * p.a_stride + a_col, cols - a_col) : none;
-                    b_piece[i][j] = z < t.depth && b_col < p.N ? load_piece(p.b + int64_t(t.begin + z) * p.b_stride + b_col, p.N - b_col) : none;
-                }
-            }
-        }
-    };
-    auto write = [&](lds_ptr to) {
-#pragma unroll
-        for (int j = 0; j < EACH; ++j)
-#pragma unroll
-            for (int i = 0; i < U; ++i) {
-                const int block = wave + j * S::WAVES;
-                *(lds_u32x4*)(to + uint32_t(i * UA + block * (A_ACROSS ? YBLOCK : XBLOCK) + lane * 16)) = a_piece[i][j];
-                *(lds_u32x4*)(to + uint32_t(U * UA + i * UB + block * (B_ACROSS ? YBLOCK : XBLOCK) + lane * 16)) = b_piece[i][j];
-            }
-    };
-    const uint32_t a_slot = uint32_t(cg * UA) + (A_ACROSS ? places_at(lane, false) : fragment_at(q, hk));
-    const uint32_t b_slot = uint32_t(U * UA) + uint32_t(rg * (B_ACROSS ? 64 : 512)) + (B_ACROSS ? places_at(lane, true) : fragment_at(q, hk));
-
-    auto work = [&](const Tile& t) {
-        f32x16 acc[2][2];
-#pragma unroll
-        for (int i = 0; i < 64; ++i) acc[i >> 5][i >> 4 & 1][i & 15] = 0.f;
-        if (t.depth > 0) load(t, 0);
-        uint32_t at = 0;
-        for (int z0 = 0; z0 < t.depth; z0 += 64) {
-            write(lds + at);
-            __syncthreads();                                   // (who is still at the other place's chunk has not written this one's successor)
-            if (z0 + 64 < t.depth) load(t, z0 + 64);
-#pragma unroll
-            for (int ks = 0; ks < 4; ++ks) {
-                bf16x8 af[2], bf[2];
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    // (rows: block i of this wave is the i-th unit's fragment rg)
-                    if constexpr (A_ACROSS) af[i] = read_across(lds + at + a_slot + uint32_t(i * 64 + ks * 2 * YBLOCK));
-                    else af[i] = read_along(lds + at + a_slot + uint32_t(i * 512 + ks * 32));
-                    if constexpr (B_ACROSS) bf[i] = read_across(lds + at + b_slot + uint32_t(i * UB + ks * 2 * YBLOCK));
-                    else bf[i] = read_along(lds + at + b_slot + uint32_t(i * UB + ks * 32));
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[i & 1][i >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(af[i & 1], bf[i >> 1], acc[i & 1][i >> 1], 0, 0, 0);
-            }
-            at = BUF - at;
-        }
-        __syncthreads();
-        if constexpr (G::ON) {
-            leave_any<DIR>(acc, gate, p, t, cols, lane, cg, rg);
-            __syncthreads();
-            return;
-        }
-        const lds_ptr mine_at = lds + uint32_t(wave) * (2 * BUF / S::WAVES / 16 * 16);
-        auto put = [&](auto* to, int64_t pitch) {
-            using T = std::remove_pointer_t<decltype(to)>;
-            constexpr int P = PIECE<T>, LANES = 64 / P, AT_ONCE = 64 / LANES, PITCH = 64 * int(sizeof(T)) + 16;
-            static_assert(32 * PITCH <= int(2 * BUF / S::WAVES), "room");
-            const int col = lane % LANES * P, row = lane / LANES, first = t.c0 + cg * 64, left = cols - first - col;
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-#pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    float v = acc[i >> 4][b][i & 15];
-                    if (DIR == FORWARD && p.relu) v = v < 0.f ? 0.f : v;                                     // (a NaN stays one)
-                    const lds_ptr here = mine_at + uint32_t(q * PITCH + ((i >> 4) * 32 + 16 * hk + (i & 15)) * int(sizeof(T)));
-                    if constexpr (sizeof(T) == 4) *(__attribute__((address_space(3))) float*)here = v;
-                    else *(__attribute__((address_space(3))) bf16_t*)here = f32_to_bf16(v);
-                }
-                wave_sync();
-                for (int i = 0; i < 32; i += AT_ONCE) {
-                    const int r = (b * 2 + rg) * 32 + row + i;
-                    if (r >= t.rows || left <= 0) continue;
-                    const u32x4 v = *(const lds_u32x4*)(mine_at + uint32_t((row + i) * PITCH + col * int(sizeof(T))));
-                    u32x4 act;
-                    const bool masked = DIR == GRAD_INPUT && p.act;
-                    if (masked) act = load_piece(p.act + int64_t(t.begin + r) * p.act_stride + first + col, left);
-                    float w[P];
-#pragma unroll
-                    for (int j = 0; j < P; ++j) {
-                        w[j] = element<T>(v, j);
-                        if (masked && !(element<bf16_t>(act, j) > 0.f)) w[j] = 0.f;
-                    }
-                    store_piece<P>(to + int64_t(r) * pitch + first + col, left, w);
-                }
-                wave_sync();
-            }
-        };
-        if constexpr (DIR == GRAD_WEIGHT) {
-            const size_t all = size_t(p.N) * size_t(p.K), row = size_t(t.r0) * size_t(p.K);
-            if (t.slot >= 0) put(partial + size_t(t.slot) * all + row, p.K);
-            else put(static_cast<TO*>(p.out) + size_t(t.e) * all + row, p.K);
-        } else put(static_cast<TO*>(p.out) + int64_t(t.begin) * p.out_stride, p.out_stride);
-        __syncthreads();
-    };
-    if constexpr (DIR == GRAD_WEIGHT) {
-        const int w_lane = int(blockIdx.x) / (ct * rt);
-        const Place at = walk<4>(int(blockIdx.x) % (ct * rt), rt, ct);
-        const int64_t from = shares.each * w_lane, to = from + shares.each;
-        for (int e = group_at(p.g, shares, from); e < p.g.E && start_of(p.g, shares, e) < to; ++e) {
-            const int a = p.g.begin(e), n = max(p.g.begin(e + 1) - a, 0);
-            const int64_t s = start_of(p.g, shares, e), first = s + shares.extra;
-            const int lo = int(min(max(from - first, int64_t(0)), int64_t(n))), hi = int(min(max(to - first, int64_t(0)), int64_t(n)));
-            if (n == 0 ? s < from : hi <= lo) continue;
-            work(Tile{e, a + lo, min(p.N - at.row * S::ROWS, S::ROWS), at.col * S::COLS, at.row * S::ROWS, hi - lo, hi - lo == n ? -1 : 2 * w_lane + (lo > 0 ? 0 : 1)});
-        }
-    } else {
-        const Place w = walk<1>(int(blockIdx.x), units / ct, ct);
-        const Piece at = counted(p.g.M, p.g.E) ? count_pieces(p.g, S::ROWS, w.row, reinterpret_cast<int*>(lds_raw)) : find_piece(p.g, S::ROWS, w.row);
-        if (at.rows > 0) work(Tile{at.e, at.begin, at.rows, w.col * WIDE, 0, at.e < p.g.E ? (DIR == FORWARD ? p.K : p.N) : 0, -1});
-    }
 }
 
 int check_groups(const moe_product_shape* s, const moe_groups* g, bool gathers, const std::string& who)
