@@ -45,6 +45,7 @@ struct Gate {
     bf16_t* hidden;           // backward: f(gate) up, or null
     int64_t hidden_stride;
     bool past;                // results go past the caches
+    bool on_16;               // rows kept in 8 bits lie on borders of 16 bytes
     __device__ __forceinline__ int blocks() const { return (h + 31) / 32; }
 };
 template <int KEEP_> struct GateKeeping : Gate { static constexpr int KEEP = KEEP_; };         // ... in a kernel that is made for one way of keeping

@@ -170,6 +170,7 @@ Gate gate_of(const moe_gated_shape* s, const moe_gated_pre* p, void* hidden, int
         g.pre_stride = p->stride;
         g.scale = static_cast<bf16_t*>(p->scale);
         g.scale_stride = p->scale_stride;
+        g.on_16 = s->h % 16 == 0 && p->stride % 16 == 0 && on_16({p->rows});
     }
     g.hidden = static_cast<bf16_t*>(hidden);
     g.hidden_stride = hidden_stride;

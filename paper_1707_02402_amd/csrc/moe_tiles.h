@@ -282,7 +282,7 @@ __device__ __forceinline__ u32x4 pack_eight(const float* v) { return u32x4{pack_
 // Forward: a lane's sums are gate and up of the same eight features.  What is kept in 8 bits shares scales among the 32 features of two blocks of columns, which the
 // two halves of the wave have.  summed false: rows of no group, zeros, and the LDS is not this wave's.
 template <class S, int LIVE, int KEEP, bool WHOLE, int ROOM>
-__device__ __forceinline__ void leave_pairs(const f32x16 (&acc)[S::FA][LIVE > 0 ? LIVE : 1], const Gate& gate, const Args& p, const Tile& now, lds_ptr room, bool summed, int lane, int cg, int rg)
+__device__ __forceinline__ void leave_pairs(f32x16 (&acc)[S::FA][LIVE > 0 ? LIVE : 1], const Gate& gate, const Args& p, const Tile& now, lds_ptr room, bool summed, int lane, int cg, int rg)
 {
     using lds_u32x4 = __attribute__((address_space(3))) u32x4;
     using lds_u32x2 = __attribute__((address_space(3))) u32x2;
@@ -290,16 +290,24 @@ __device__ __forceinline__ void leave_pairs(const f32x16 (&acc)[S::FA][LIVE > 0 
     constexpr int LANES = FA * 2, AT_ONCE = 64 / LANES, STORES = 32 / AT_ONCE;
     static_assert(KEEP != KEEP_8 || FA % 2 == 0, "a block of 32 features");
     static_assert(PARTS * PART + (KEEP == KEEP_8 ? 2 * PART8 : 0) <= ROOM, "room");
-    const int q = lane & 31, hk = lane >> 5, h = gate.h, first = now.c0 + cg * (FA * 16), col = lane % LANES * 8, row = lane / LANES, cols = h - first - col;
+    // (what follows from a lane's number is made where it is used: kept in registers through the products, some of it was in scratch memory)
+    auto here = [&]() {
+        int l = lane;
+        if constexpr (KEEP == KEEP_8) asm volatile("" : "+v"(l));
+        return l;
+    };
+    const int h = gate.h, first = now.c0 + cg * (FA * 16);
     const int64_t from = now.begin + rg * 32;
-    const lds_ptr in = room + uint32_t(q * PITCH + hk * 16), in8 = room + uint32_t(PARTS * PART + q * PITCH8 + hk * 8);
-    const lds_ptr out = room + uint32_t(row * PITCH + col * 2), out8 = room + uint32_t(PARTS * PART + row * PITCH8 + col);
 #pragma unroll
     for (int b = 0; b < LIVE; ++b) {
         const int block = (b * S::RG) * 32, left = now.rows - block - rg * 32;
+        uint32_t scales = KEEP == KEEP_8 ? uint32_t(scale8_bits(scale8(0u))) * 0x10001u : 0u;  // of two blocks, of gate or of up
         if (summed) {
+            const int in_lane = here();
+            const lds_ptr in = room + uint32_t((in_lane & 31) * PITCH + (in_lane >> 5) * 16);
 #pragma unroll
             for (int a = 0; a < FA; ++a) {
+                if constexpr (S::BIG && KEEP == KEEP_8) asm volatile("" : "+a"(acc[a][b]));            // (read here, and not ahead of the block before)
                 float y[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) y[i] = gate_f(gate.form, acc[a][b][i]) * acc[a][b][8 + i];
@@ -312,37 +320,49 @@ __device__ __forceinline__ void leave_pairs(const f32x16 (&acc)[S::FA][LIVE > 0 
                         *(lds_u32x4*)(in + uint32_t((1 + s) * PART + a * 32)) = pack_eight(y);
                     }
                 __builtin_amdgcn_sched_barrier(0);             // (all accumulators at once in other registers would have no room)
-            }
-            if constexpr (KEEP == KEEP_8)
+                if constexpr (KEEP == KEEP_8)
+                    if (a % 2 == 1) {                          // (while the two blocks are in ordinary registers)
+                        const int l = here(), hk = l >> 5;
+                        const lds_ptr in8 = room + uint32_t(PARTS * PART + (l & 31) * PITCH8 + hk * 8 + (a - 1) * 16);
 #pragma unroll
-                for (int a = 0; a < FA; a += 2)
+                        for (int s = 0; s < 2; ++s) {
+                            uint32_t largest = 0u;
 #pragma unroll
-                    for (int s = 0; s < 2; ++s) {
-                        uint32_t largest = 0u;
+                            for (int i = 0; i < 16; ++i) largest = max(largest, magnitude(acc[a - 1 + (i >> 3)][b][8 * s + (i & 7)]));
+                            const Scale8 c = scale8(largest_of_halves(largest));
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) largest = max(largest, magnitude(acc[a + (i >> 3)][b][8 * s + (i & 7)]));
-                        const Scale8 c = scale8(max(largest, uint32_t(__shfl_xor(int(largest), 32))));
+                            for (int n = 0; n < 2; ++n) {
+                                float x[8];
 #pragma unroll
-                        for (int n = 0; n < 2; ++n) {
-                            float x[8];
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) x[i] = acc[a + n][b][8 * s + i];
-                            *(lds_u32x2*)(in8 + uint32_t(s * PART8 + (a + n) * 16)) = u32x2{pack8(x[0], x[1], x[2], x[3], c.inv), pack8(x[4], x[5], x[6], x[7], c.inv)};
+                                for (int i = 0; i < 8; ++i) x[i] = acc[a - 1 + n][b][8 * s + i];
+                                *(lds_u32x2*)(in8 + uint32_t(s * PART8 + n * 16)) = u32x2{pack8(x[0], x[1], x[2], x[3], c.inv), pack8(x[4], x[5], x[6], x[7], c.inv)};
+                            }
+                            // (without a branch: a half of the word is a block's, of gate in the lower half of the wave, of up in the upper)
+                            const uint32_t mine = (s == 0 ? ~0u : 0u - uint32_t(hk)) & (a == 1 ? 0x0000ffffu : 0xffff0000u);
+                            scales = (scales & ~mine) | (mine & (uint32_t(scale8_bits(c)) * 0x10001u));
+                            __builtin_amdgcn_sched_barrier(0);
                         }
-                        const int f = first + a * 16;
-                        if (hk == 0 && q < left && f < h) gate.scale[(from + block + q) * gate.scale_stride + s * gate.blocks() + f / BLOCK8] = scale8_bits(c);
-                        __builtin_amdgcn_sched_barrier(0);
                     }
+            }
             wave_sync();
-        } else if (KEEP == KEEP_8 && hk == 0 && q < left)
-#pragma unroll
-            for (int a = 0; a < FA; a += 2)
-                if (first + a * 16 < h)
-#pragma unroll
-                    for (int s = 0; s < 2; ++s) gate.scale[(from + block + q) * gate.scale_stride + s * gate.blocks() + (first + a * 16) / BLOCK8] = scale8_bits(scale8(0u));
+        }
+        // (one half of the wave has gate's scales, the other up's; two blocks' leave together)
+        if constexpr (KEEP == KEEP_8) {
+            const int l = here();
+            if ((l & 31) < left && first < h) {
+                using Offset = std::conditional_t<WHOLE, uint32_t, int64_t>;                   // (32 rows are within 32 bits)
+                bf16_t* const to = gate.scale + (from + block) * gate.scale_stride + first / BLOCK8 + (Offset(l & 31) * Offset(gate.scale_stride) + Offset(l >> 5) * Offset(gate.blocks()));
+                typedef uint32_t u32_at2 __attribute__((aligned(2)));
+                if (FA == 4 && first + BLOCK8 < h) *reinterpret_cast<u32_at2*>(to) = scales;
+                else *to = bf16_t(scales);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
         put_past(WHOLE && gate.past, [&](auto past) {
             constexpr bool PAST = decltype(past)::value;
             const u32x4 none = {0u, 0u, 0u, 0u};
+            const int l = here(), col = l % LANES * 8, row = l / LANES, cols = h - first - col;
+            const lds_ptr out = room + uint32_t(row * PITCH + col * 2);
             bf16_t* const to = static_cast<bf16_t*>(p.out) + (from + block + row) * p.out_stride + first + col;
 #pragma unroll
             for (int i = 0; i < STORES; ++i) {
@@ -360,14 +380,27 @@ __device__ __forceinline__ void leave_pairs(const f32x16 (&acc)[S::FA][LIVE > 0 
                     }
             }
             if constexpr (KEEP == KEEP_8) {
-                int8_t* const pre = static_cast<int8_t*>(gate.pre) + (from + block + row) * gate.pre_stride + first + col;
+                // 16 features a lane where rows allow it, or 8
+                auto eight = [&](auto wide) {
+                    constexpr int N = decltype(wide)::value, LANES8 = FA * 16 / N, AT_ONCE8 = 64 / LANES8;
+                    const int l8 = here(), row8 = l8 / LANES8, col8 = l8 % LANES8 * N, cols8 = h - first - col8;
+                    int8_t* to = static_cast<int8_t*>(gate.pre) + (from + block + row8) * gate.pre_stride + first + col8;
+                    lds_ptr at = room + uint32_t(PARTS * PART + row8 * PITCH8 + col8);
 #pragma unroll
-                for (int s = 0; s < 2; ++s)
+                    for (int s = 0; s < 2; ++s, to += h, at += PART8)
 #pragma unroll
-                    for (int i = 0; i < STORES; ++i) {
-                        const u32x2 v = summed ? *(const lds_u32x2*)(out8 + uint32_t(s * PART8 + i * AT_ONCE * PITCH8)) : u32x2{0u, 0u};
-                        if (row + i * AT_ONCE < left && cols > 0) put_eight<WHOLE, PAST>(pre + i * AT_ONCE * gate.pre_stride + s * h, cols, v);
-                    }
+                        for (int i = 0; i < 32; i += AT_ONCE8) {
+                            using V = std::conditional_t<N == 16, u32x4, u32x2>;
+                            V v = {};
+                            if (summed) v = *(const __attribute__((address_space(3))) V*)(at + uint32_t(i * PITCH8));
+                            if (row8 + i < left && cols8 > 0) {
+                                if constexpr (N == 16) put_eight<WHOLE, PAST>(reinterpret_cast<bf16_t*>(to + i * gate.pre_stride), 8, v);
+                                else put_eight<WHOLE, PAST>(to + i * gate.pre_stride, cols8, v);
+                            }
+                        }
+                };
+                if (WHOLE && gate.on_16) eight(std::integral_constant<int, 16>{});
+                else eight(std::integral_constant<int, 8>{});
             }
         });
         wave_sync();
@@ -378,11 +411,12 @@ __device__ __forceinline__ void leave_pairs(const f32x16 (&acc)[S::FA][LIVE > 0 
 // Backward: dact goes through LDS in fp32, unrounded, and meets the kept pair where a lane has eight neighbouring features of a row.  A row has FA * 8 pieces of 16 bytes there,
 // piece j of row q at place j ^ q (of the places that there are), so that neither side's accesses meet in a bank.
 template <class S, int LIVE, int KEEP, bool WHOLE, int ROOM>
-__device__ __forceinline__ void leave_grads(const f32x16 (&acc)[S::FA][LIVE > 0 ? LIVE : 1], const Gate& gate, const Args& p, const Tile& now, lds_ptr room, bool summed, int lane, int cg, int rg)
+__device__ __forceinline__ void leave_grads(f32x16 (&acc)[S::FA][LIVE > 0 ? LIVE : 1], const Gate& gate, const Args& p, const Tile& now, lds_ptr room, bool summed, int lane, int cg, int rg)
 {
     using lds_f32x4 = __attribute__((address_space(3))) f32x4;
     constexpr int FA = S::FA, PIECES = FA * 8, LANES = FA * 4, AT_ONCE = 64 / LANES, STORES = 32 / AT_ONCE;
     static_assert(32 * PIECES * 16 <= ROOM, "room");
+    asm volatile("" : "+v"(lane));                             // (as above)
     const int q = lane & 31, hk = lane >> 5, h = gate.h, col = lane % LANES * 8, row = lane / LANES, c = now.c0 + cg * (FA * 32) + col, cols = h - c;
     auto put = [&](int64_t at, const u32x4& dg, const u32x4& du, const u32x4& f) {
         put_past(WHOLE && gate.past, [&](auto past) {
@@ -635,7 +669,12 @@ __device__ __forceinline__ void product_tiles(Args p, G gate, int units, int ct,
 #pragma unroll
             for (int i = 0; i < AU; ++i) {
                 const uint32_t col = uint32_t(min(t.c0 + i * 64 + (lane & 7) * 8, cols - 8)) * 2u;
-                if constexpr (PAIRS) a_off[i][j] = (uint32_t(s_q >> 4) * uint32_t(cols) + uint32_t(min((i * 2 + (lane >> 5)) * 16 + pair_feature(s_q), cols - 1 - t.c0))) * uint32_t(p.K) * 2u + piece;
+                if constexpr (PAIRS) {
+                    int l = lane;                              // (made anew for every tile where registers are short)
+                    if constexpr (G::KEEP == KEEP_8) asm volatile("" : "+v"(l));
+                    const int row = copied_row(block, l);
+                    a_off[i][j] = (uint32_t(row >> 4) * uint32_t(cols) + uint32_t(min((i * 2 + (l >> 5)) * 16 + pair_feature(row), cols - 1 - t.c0))) * uint32_t(p.K) * 2u + piece;
+                }
                 else if constexpr (DIR == FORWARD)             // (the features in the order that gives a lane 16 neighbours)
                     a_off[i][j] = uint32_t(min(i * 64 + (lane >> 5) * 32 + (s_q >> 2 & 1) * 16 + (s_q >> 3) * 4 + (s_q & 3), cols - 1 - t.c0)) * uint32_t(p.K) * 2u + piece;
                 else if constexpr (DIR == GRAD_INPUT) a_off[i][j] = uint32_t(z) * uint32_t(p.K) * 2u + col;
@@ -1023,8 +1062,8 @@ __device__ __forceinline__ void product_tiles(Args p, G gate, int units, int ct,
         primed = nchunk > 0 && then.depth > 0;
         // (the fewest that there can have been: of the blocks that are whole)
         if constexpr (G::ON)
-            // (gated: out, and of the kept pair two in bfloat16 or two in 8 bits and scales; backwards three, or two without the hidden rows)
-            stores = now.c0 + (cg + 1) * WAVE_WIDE <= cols ? max(0, (now.rows / 32 - rg + S::RG - 1) / S::RG) * FA * (PAIRS ? (G::KEEP == KEEP_NOTHING ? 1 : 3) : 4) : 0;
+            // (gated: out, and of the kept pair two in bfloat16, or two halves in 8 bits and scales; backwards three, or two without the hidden rows)
+            stores = now.c0 + (cg + 1) * WAVE_WIDE <= cols ? max(0, (now.rows / 32 - rg + S::RG - 1) / S::RG) * FA * (PAIRS ? (G::KEEP == KEEP_NOTHING ? 1 : G::KEEP == KEEP_BF16 ? 3 : 2) : 4) : 0;
         else stores = now.c0 + cg * (FA * 32) + FA * 32 <= cols ? max(0, (now.rows / 32 - rg + S::RG - 1) / S::RG) * FA * (DIR == GRAD_WEIGHT ? int(sizeof(TO)) : 2) : 0;
         now = then;
     }

@@ -22,6 +22,12 @@ __device__ __forceinline__ Scale8 scale8(uint32_t largest)
     const float s = __uint_as_float(max(up, 0x00800000u));
     return Scale8{s, 1.f / s};
 }
+// of a lane's and that of the lane 32 further on or back
+__device__ __forceinline__ uint32_t largest_of_halves(uint32_t v)
+{
+    const auto both = __builtin_amdgcn_permlane32_swap(v, v, false, false);                // the lower half's twice, the upper half's twice
+    return max(both[0], both[1]);
+}
 __device__ __forceinline__ bf16_t scale8_bits(const Scale8& s) { return bf16_t(__float_as_uint(s.s) >> 16); }
 // four elements.  Added to 1.5 * 2^23 a number leaves its nearest whole number in the lowest bits of the sum; the product is rounded first, as the definition says.
 __device__ __forceinline__ uint32_t pack8(float x0, float x1, float x2, float x3, float inv)
