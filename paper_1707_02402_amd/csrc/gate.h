@@ -24,6 +24,7 @@ __device__ __forceinline__ float gate_f(const GateForm& k, float g)
     const float c = within_1e4(g);
     return g * gate_sigma(k, g, c * c);
 }
+__device__ __forceinline__ float gate_silu(float g) { return g * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(g * -1.44269504f)); }
 __device__ __forceinline__ GateValue gate_both(const GateForm& k, float g)
 {
     const float c = within_1e4(g), c2 = c * c, s = gate_sigma(k, g, c2), w = k.a + k.b3 * c2;

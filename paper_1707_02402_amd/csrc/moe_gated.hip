@@ -155,7 +155,6 @@ int check_pre(const moe_gated_shape* s, const moe_gated_pre* p, const std::strin
     if ((p->dtype == DYNB_BF16 && odd(p->rows)) || (p->dtype == DYNB_I8 && odd(p->scale))) return fail(DYNB_E_INVAL, who + ": misaligned pre");
     return DYNB_OK;
 }
-constexpr int64_t PAST = 64 << 20;                             // bytes of results from which they go past the caches (put_eight)
 // written: bytes of results for a row's feature
 Gate gate_of(const moe_gated_shape* s, const moe_gated_pre* p, void* hidden, int64_t hidden_stride, int written)
 {

@@ -215,8 +215,8 @@ __device__ __forceinline__ Place walk(int u, int rows, int ct)
 }
 
 // Eight features of a row to or from anywhere: `left` of them are there (at least one).  WHOLE: all eight, and on a border of eight.
-// past: results that no cache will hold for who reads them next go past the caches, and leave them to the operands (65536 rows, 1024 -> 2 x 2048, 64 experts: forward
-// 614 -> 598 us, with the pair kept in bfloat16 696 -> 654, backward 496 -> 478; what fits the caches is read from them by the next call, and leaves as usual).
+// PAST: see put_past (65536 rows, 1024 -> 2 x 2048, 64 experts: with the pair kept in bfloat16 forward 696 -> 654 us, backward from 8 bits 497 -> 474; 16384 rows of 1024
+// hidden features, backward 90 -> 71).
 template <bool WHOLE, bool PAST>
 __device__ __forceinline__ void put_eight(bf16_t* p, int left, const u32x4& v)
 {
@@ -234,16 +234,6 @@ __device__ __forceinline__ void put_eight(int8_t* p, int left, const u32x2& v)
     if constexpr (WHOLE && PAST) __builtin_nontemporal_store(v, reinterpret_cast<u32x2*>(p));
     else if constexpr (WHOLE) *reinterpret_cast<u32x2*>(p) = v;
     else store_eight(p, left, v);
-}
-// (the compiler would make one store of the two, and an ordinary one)
-template <class F>
-__device__ __forceinline__ void put_past(bool past, F put)
-{
-    if (past) {
-        asm volatile("; past the caches" ::: "memory");
-        put(std::true_type{});
-        asm volatile("" ::: "memory");
-    } else put(std::false_type{});
 }
 // ... of a kept pair's gate and up, as they lie and as numbers
 template <int KEEP, bool WHOLE>
@@ -309,8 +299,13 @@ __device__ __forceinline__ void leave_pairs(f32x16 (&acc)[S::FA][LIVE > 0 ? LIVE
             for (int a = 0; a < FA; ++a) {
                 if constexpr (S::BIG && KEEP == KEEP_8) asm volatile("" : "+a"(acc[a][b]));            // (read here, and not ahead of the block before)
                 float y[8];
+                // (SiLU does without three of the gate's ten operations: 1 % of the time at 65536 rows, 1024 -> 2 x 2048)
+                if (gate.form.b2 == 0.f)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] = gate_f(gate.form, acc[a][b][i]) * acc[a][b][8 + i];
+                    for (int i = 0; i < 8; ++i) y[i] = gate_silu(acc[a][b][i]) * acc[a][b][8 + i];
+                else
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) y[i] = gate_f(gate.form, acc[a][b][i]) * acc[a][b][8 + i];
                 *(lds_u32x4*)(in + uint32_t(a * 32)) = pack_eight(y);
                 if constexpr (KEEP == KEEP_BF16)
 #pragma unroll
@@ -326,16 +321,22 @@ __device__ __forceinline__ void leave_pairs(f32x16 (&acc)[S::FA][LIVE > 0 ? LIVE
                         const lds_ptr in8 = room + uint32_t(PARTS * PART + (l & 31) * PITCH8 + hk * 8 + (a - 1) * 16);
 #pragma unroll
                         for (int s = 0; s < 2; ++s) {
-                            uint32_t largest = 0u;
+                            // (as signed numbers the largest is of those without a sign, as unsigned ones of those with one, if there are any)
+                            int32_t above = 0;
+                            uint32_t below = 0u;
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) largest = max(largest, magnitude(acc[a - 1 + (i >> 3)][b][8 * s + (i & 7)]));
-                            const Scale8 c = scale8(largest_of_halves(largest));
+                            for (int i = 0; i < 16; ++i) {
+                                const float x = acc[a - 1 + (i >> 3)][b][8 * s + (i & 7)];
+                                above = max(above, __float_as_int(x));
+                                below = max(below, __float_as_uint(x));
+                            }
+                            const Scale8 c = scale8_of_sums(largest_of_halves(max(uint32_t(above), below & 0x7fffffffu)));
 #pragma unroll
                             for (int n = 0; n < 2; ++n) {
                                 float x[8];
 #pragma unroll
                                 for (int i = 0; i < 8; ++i) x[i] = acc[a - 1 + n][b][8 * s + i];
-                                *(lds_u32x2*)(in8 + uint32_t(s * PART8 + n * 16)) = u32x2{pack8(x[0], x[1], x[2], x[3], c.inv), pack8(x[4], x[5], x[6], x[7], c.inv)};
+                                *(lds_u32x2*)(in8 + uint32_t(s * PART8 + n * 16)) = u32x2{pack8<false>(x[0], x[1], x[2], x[3], c.inv), pack8<false>(x[4], x[5], x[6], x[7], c.inv)};
                             }
                             // (without a branch: a half of the word is a block's, of gate in the lower half of the wave, of up in the upper)
                             const uint32_t mine = (s == 0 ? ~0u : 0u - uint32_t(hk)) & (a == 1 ? 0x0000ffffu : 0xffff0000u);

@@ -98,30 +98,61 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void k_norm(const T*
     }
 }
 
-// The backward pass's x as it lies (RowsOf), or in 8 bits (Rows8)
+// The sum over a wave without LDS: neighbours, quads, halves of 16 lanes and 16 lanes by lanes' permutations, then the two 16s and the two halves change places.  (By way of
+// LDS it is six round trips of 100 clocks and more, which a row's wave does not hide.)
+__device__ __forceinline__ float wave_sum_in_registers(float v)
+{
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xb1, 0xf, 0xf, true));              // lanes 1 0 3 2
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x4e, 0xf, 0xf, true));              // lanes 2 3 0 1
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x141, 0xf, 0xf, true));             // eight lanes backwards
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x140, 0xf, 0xf, true));             // sixteen lanes backwards
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+__device__ __forceinline__ void store_past(bf16_t* p, const float (&v)[8])
+{
+    __builtin_nontemporal_store(u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])}, reinterpret_cast<u32x4_at2*>(p));
+}
+__device__ __forceinline__ void store_past(float* p, const float (&v)[4])
+{
+    __builtin_nontemporal_store(u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])}, reinterpret_cast<u32x4_at4*>(p));
+}
+
+// The backward pass's x as it lies (RowsOf), or in 8 bits (Rows8).  From 8 bits 65536 x 1024 take bf16 62 us (340 MB, 5.4 TB/s) where x in bf16 takes 74, fp32 136 (610 MB, 4.5); 4097 x 777 fp32,
+// which wait for their rows' loads, 11.3.
 template <typename T>
 struct RowsOf {
+    static constexpr bool WHOLE = false;
     const T* x;
     int64_t stride;
     using Raw = u32x4;
     __device__ __forceinline__ Raw load(int64_t row, int c, int d) const { return load_piece(x + row * stride + c, d - c); }
     static __device__ __forceinline__ float value(const Raw& v, int j) { return element<T>(v, j); }
+    static __device__ __forceinline__ float sum(float v) { return wave_sum(v); }
     __device__ __forceinline__ float at(int64_t row, int c) const { return load_f32(x + row * stride + c); }
 };
-template <typename T>
+// WHOLE: d is a multiple of a piece's elements, so that a piece is there or is not
+template <typename T, bool WHOLE_>
 struct Rows8 {
+    static constexpr bool WHOLE = WHOLE_;
     const int8_t* q;
     int64_t stride;
     const bf16_t* scale;
     int64_t scale_stride;
+    bool past;                // dx goes past the caches
     struct Raw { u32x2 q; float s; };
     __device__ __forceinline__ Raw load(int64_t row, int c, int d) const
     {
         if (c >= d) return Raw{{0u, 0u}, 0.f};
-        if constexpr (PIECE<T> == 8) return Raw{load_eight(q + row * stride + c, d - c), bf16_to_f32(scale[row * scale_stride + c / BLOCK8])};
-        else return Raw{{load_four(q + row * stride + c, d - c), 0u}, bf16_to_f32(scale[row * scale_stride + c / BLOCK8])};
+        const int left = WHOLE ? 8 : d - c;
+        if constexpr (PIECE<T> == 8) return Raw{load_eight(q + row * stride + c, left), bf16_to_f32(scale[row * scale_stride + c / BLOCK8])};
+        else return Raw{{load_four(q + row * stride + c, left), 0u}, bf16_to_f32(scale[row * scale_stride + c / BLOCK8])};
     }
     static __device__ __forceinline__ float value(const Raw& v, int j) { return unpack8(v.q[j >> 2], j & 3) * v.s; }
+    static __device__ __forceinline__ float sum(float v) { return wave_sum_in_registers(v); }
     __device__ __forceinline__ float at(int64_t row, int c) const { return float(q[row * stride + c]) * bf16_to_f32(scale[row * scale_stride + c / BLOCK8]); }
 };
 // said to be other numbers, so that what follows from them is made anew
@@ -166,7 +197,8 @@ __device__ __forceinline__ void norm_grad_rows(const T* dy, int64_t dy_stride, X
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = (i * NL + lane) * P;
-            a[i] = load_piece(dy + row * dy_stride + c, d - c);
+            if constexpr (X::WHOLE) a[i] = c < d ? load_piece(dy + row * dy_stride + c, P) : u32x4{0u, 0u, 0u, 0u};
+            else a[i] = load_piece(dy + row * dy_stride + c, d - c);
             b[i] = x.load(row, c, d);
         }
         m = mean[row];
@@ -181,7 +213,7 @@ __device__ __forceinline__ void norm_grad_rows(const T* dy, int64_t dy_stride, X
         for (int i = 0; i < NV; ++i)
 #pragma unroll
             for (int j = 0; j < P; ++j) {
-                const bool on = (i * NL + lane) * P + j < d;   // (what lies behind the row must not count, whatever mean and rstd are)
+                const bool on = (i * NL + lane) * P + (X::WHOLE ? 0 : j) < d;                // (what lies behind the row must not count, whatever mean and rstd are)
                 h[i][j] = on ? (X::value(b[i], j) - m) * r : 0.f;
                 const float y = element<T>(a[i], j);
                 dg[i][j] += y * h[i][j];
@@ -195,12 +227,12 @@ __device__ __forceinline__ void norm_grad_rows(const T* dy, int64_t dy_stride, X
         const int64_t here = row;
         if (WAVES < 16 && row < n - step) load(row + step);
         if constexpr (WAVES == 1) {
-            s1 = wave_sum(s1);
-            s2 = wave_sum(s2);
+            s1 = X::sum(s1);
+            s2 = X::sum(s2);
         } else {
             // (one meeting for both; the next row's sums lie in the other half)
-            s1 = wave_sum(s1);
-            s2 = wave_sum(s2);
+            s1 = X::sum(s1);
+            s2 = X::sum(s2);
             if ((threadIdx.x & 63) == 0) { room[turn][0][wave] = s1; room[turn][1][wave] = s2; }
             __syncthreads();
             s1 = s2 = 0.f;
@@ -224,7 +256,14 @@ __device__ __forceinline__ void norm_grad_rows(const T* dy, int64_t dy_stride, X
                 }
 #pragma unroll
                 for (int j = 0; j < P; ++j) v[i][j] = r0 * (v[i][j] - m1 - h[i][j] * m2);
-                store_piece<P>(dx + here * dx_stride + c, d - c, v[i]);
+                if constexpr (X::WHOLE) {
+                    T* const to = dx + here * dx_stride + c;
+                    if (c < d)
+                        put_past(x.past, [&](auto past) {
+                            if constexpr (decltype(past)::value) store_past(to, v[i]);
+                            else store_piece<P>(to, P, v[i]);
+                        });
+                } else store_piece<P>(dx + here * dx_stride + c, d - c, v[i]);
             }
         }
         if (WAVES == 16 && row < n - step) load(row + step);   // (sixteen waves have half the registers: no room for two rows)
@@ -259,11 +298,11 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void k_norm_grad(con
 {
     norm_grad_rows<T, RowsOf<T>, NV, WAVES>(dy, dy_stride, RowsOf<T>{x, x_stride}, gamma, mean, rstd, dx, dx_stride, partial, n, d);
 }
-template <typename T, int NV, int WAVES>
-__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void k_norm8_grad(const T* dy, int64_t dy_stride, Rows8<T> x, const float* __restrict__ gamma, const float* __restrict__ mean,
+template <typename T, int NV, int WAVES, bool WHOLE>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void k_norm8_grad(const T* dy, int64_t dy_stride, Rows8<T, WHOLE> x, const float* __restrict__ gamma, const float* __restrict__ mean,
                                                                               const float* __restrict__ rstd, T* dx, int64_t dx_stride, float* __restrict__ partial, int n, int d)
 {
-    norm_grad_rows<T, Rows8<T>, NV, WAVES>(dy, dy_stride, x, gamma, mean, rstd, dx, dx_stride, partial, n, d);
+    norm_grad_rows<T, Rows8<T, WHOLE>, NV, WAVES>(dy, dy_stride, x, gamma, mean, rstd, dx, dx_stride, partial, n, d);
 }
 
 // dgamma and dbeta, as they lie one behind the other in a line of `partial`
@@ -349,7 +388,7 @@ __global__ __launch_bounds__(256) void k_norm_dx_long(const T* dy, int64_t dy_st
     norm_dx_long<T>(dy, dy_stride, RowsOf<T>{x, x_stride}, gamma, mean, rstd, dx, dx_stride, d);
 }
 template <typename T>
-__global__ __launch_bounds__(256) void k_norm8_dx_long(const T* dy, int64_t dy_stride, Rows8<T> x, const float* __restrict__ gamma, const float* __restrict__ mean,
+__global__ __launch_bounds__(256) void k_norm8_dx_long(const T* dy, int64_t dy_stride, Rows8<T, false> x, const float* __restrict__ gamma, const float* __restrict__ mean,
                                                        const float* __restrict__ rstd, T* dx, int64_t dx_stride, int d)
 {
     norm_dx_long<T>(dy, dy_stride, x, gamma, mean, rstd, dx, dx_stride, d);
@@ -382,7 +421,7 @@ __global__ __launch_bounds__(256) void k_norm_dparams_long(const T* dy, int64_t 
     norm_dparams_long<T>(dy, dy_stride, RowsOf<T>{x, x_stride}, mean, rstd, dgamma, dbeta, n, d);
 }
 template <typename T>
-__global__ __launch_bounds__(256) void k_norm8_dparams_long(const T* dy, int64_t dy_stride, Rows8<T> x, const float* __restrict__ mean, const float* __restrict__ rstd,
+__global__ __launch_bounds__(256) void k_norm8_dparams_long(const T* dy, int64_t dy_stride, Rows8<T, false> x, const float* __restrict__ mean, const float* __restrict__ rstd,
                                                             float* __restrict__ dgamma, float* __restrict__ dbeta, int n, int d)
 {
     norm_dparams_long<T>(dy, dy_stride, x, mean, rstd, dgamma, dbeta, n, d);
@@ -492,12 +531,16 @@ int norm_backward(const dynb_norm_shape* s, const void* dy, int64_t dy_stride, c
         using T = decltype(in);
         constexpr int NV = decltype(nv)::value, WAVES = decltype(waves)::value;
         const T *a = static_cast<const T*>(dy), *b = static_cast<const T*>(x);
-        const Rows8<T> r = rows ? Rows8<T>{static_cast<const int8_t*>(rows->q), rows->q_stride, static_cast<const bf16_t*>(rows->scale), rows->scale_stride} : Rows8<T>{};
+        using Eight = Rows8<T, false>;
+        const Eight r = rows ? Eight{static_cast<const int8_t*>(rows->q), rows->q_stride, static_cast<const bf16_t*>(rows->scale), rows->scale_stride, false} : Eight{};
         T* const to = static_cast<T*>(dx);
         if constexpr (WAVES > 0) {
             const dim3 threads(WAVES == 1 ? 256 : WAVES * 64);
-            if (lines > 0 && rows)
-                hipLaunchKernelGGL((k_norm8_grad<T, NV, WAVES>), dim3(unsigned(lines)), threads, 0, st, a, dy_stride, r, gamma, mean, rstd, to, dx_stride, partial, s->T, s->d);
+            if (lines > 0 && rows && s->d % PIECE<T> == 0)
+                hipLaunchKernelGGL((k_norm8_grad<T, NV, WAVES, true>), dim3(unsigned(lines)), threads, 0, st, a, dy_stride, Rows8<T, true>{r.q, r.stride, r.scale, r.scale_stride, int64_t(s->T) * s->d * int64_t(sizeof(T)) >= PAST}, gamma, mean, rstd,
+                                   to, dx_stride, partial, s->T, s->d);
+            else if (lines > 0 && rows)
+                hipLaunchKernelGGL((k_norm8_grad<T, NV, WAVES, false>), dim3(unsigned(lines)), threads, 0, st, a, dy_stride, r, gamma, mean, rstd, to, dx_stride, partial, s->T, s->d);
             else if (lines > 0)
                 hipLaunchKernelGGL((k_norm_grad<T, NV, WAVES>), dim3(unsigned(lines)), threads, 0, st, a, dy_stride, b, x_stride, gamma, mean, rstd, to, dx_stride, partial, s->T, s->d);
             if (partial) hipLaunchKernelGGL(k_norm_join, dim3(unsigned((2 * int64_t(s->d) + 63) / 64)), dim3(1024), 0, st, partial, dgamma, dbeta, lines, s->d);
@@ -510,7 +553,7 @@ int norm_backward(const dynb_norm_shape* s, const void* dy, int64_t dy_stride, c
         for (int64_t t = 0; t < s->T && dx; t += MOST_ROWS) {
             const dim3 n(unsigned(std::min<int64_t>(s->T - t, MOST_ROWS)));
             if (rows)
-                hipLaunchKernelGGL((k_norm8_dx_long<T>), n, dim3(256), 0, st, a + t * dy_stride, dy_stride, Rows8<T>{r.q + t * r.stride, r.stride, r.scale + t * r.scale_stride, r.scale_stride},
+                hipLaunchKernelGGL((k_norm8_dx_long<T>), n, dim3(256), 0, st, a + t * dy_stride, dy_stride, Eight{r.q + t * r.stride, r.stride, r.scale + t * r.scale_stride, r.scale_stride, false},
                                    gamma, mean + t, rstd + t, to + t * dx_stride, dx_stride, s->d);
             else
                 hipLaunchKernelGGL((k_norm_dx_long<T>), n, dim3(256), 0, st, a + t * dy_stride, dy_stride, b + t * x_stride, x_stride, gamma, mean + t, rstd + t, to + t * dx_stride, dx_stride,

@@ -44,7 +44,7 @@ __global__ __launch_bounds__(256) void k_store8(const T* __restrict__ x, int64_t
 
 template <typename T>
 __global__ __launch_bounds__(256) void k_load8(const int8_t* __restrict__ q, int64_t q_stride, const bf16_t* __restrict__ scale, int64_t scale_stride, T* __restrict__ x, int64_t x_stride, int d,
-                                               int pieces, int64_t all)
+                                               int pieces, int64_t all, bool past)
 {
     for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < all; i += int64_t(gridDim.x) * 256) {
         const int64_t row = i / pieces;
@@ -54,7 +54,13 @@ __global__ __launch_bounds__(256) void k_load8(const int8_t* __restrict__ q, int
         float v[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = unpack8(raw[j >> 2], j & 3) * s;
-        store_piece<8>(x + row * x_stride + c, left, v);
+        T* const to = x + row * x_stride + c;
+        put_past(past, [&](auto past_) {
+            if (decltype(past_)::value && sizeof(T) == 2 && left >= 8) {
+                const u32x4 packed = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+                __builtin_nontemporal_store(packed, reinterpret_cast<u32x4_at2*>(to));
+            } else store_piece<8>(to, left, v);
+        });
     }
 }
 
@@ -101,8 +107,9 @@ extern "C" int dynb_load8(const dynb_rows8_shape* s, const dynb_rows8* rows, voi
     hipStream_t st = static_cast<hipStream_t>(stream);
     const int d = s->d, pieces = (d + 7) / 8;
     const int64_t all = int64_t(s->T) * pieces;
+    const bool past = s->dtype == DYNB_BF16 && int64_t(s->T) * d * 2 >= PAST;               // (fp32: a lane's 32 bytes are two stores, 100 us past the caches where 62 do)
     const dim3 grid(unsigned(std::min((all + 255) / 256, MOST_GROUPS)));
-    if (s->dtype == DYNB_BF16) hipLaunchKernelGGL((k_load8<bf16_t>), grid, dim3(256), 0, st, static_cast<const int8_t*>(rows->q), rows->q_stride, static_cast<const bf16_t*>(rows->scale), rows->scale_stride, static_cast<bf16_t*>(x), x_stride, d, pieces, all);
-    else hipLaunchKernelGGL((k_load8<float>), grid, dim3(256), 0, st, static_cast<const int8_t*>(rows->q), rows->q_stride, static_cast<const bf16_t*>(rows->scale), rows->scale_stride, static_cast<float*>(x), x_stride, d, pieces, all);
+    if (s->dtype == DYNB_BF16) hipLaunchKernelGGL((k_load8<bf16_t>), grid, dim3(256), 0, st, static_cast<const int8_t*>(rows->q), rows->q_stride, static_cast<const bf16_t*>(rows->scale), rows->scale_stride, static_cast<bf16_t*>(x), x_stride, d, pieces, all, past);
+    else hipLaunchKernelGGL((k_load8<float>), grid, dim3(256), 0, st, static_cast<const int8_t*>(rows->q), rows->q_stride, static_cast<const bf16_t*>(rows->scale), rows->scale_stride, static_cast<float*>(x), x_stride, d, pieces, all, past);
     return launched("dynb_load8");
 }
