@@ -213,7 +213,8 @@ def _stream(stream=None):
         return ct.c_void_p(stream.cuda_stream)
     import torch
     try:                                         # current_stream() builds an object: 2.6 us, more than the smallest kernels take
-        return ct.c_void_p(torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()))
+        c = torch._C
+        return ct.c_void_p(c._cuda_getCurrentRawStream(c._cuda_getDevice()))
     except AttributeError:                       # neither is torch's public interface: a torch without them is asked the slower way
         return ct.c_void_p(torch.cuda.current_stream().cuda_stream)
 
@@ -242,6 +243,8 @@ def _made(stream, make):
 def _scratch(nbytes: int, device, stream):
     """Device buffer the binding allocates on the caller's behalf."""
     import torch
+    if stream is None:                           # (the usual case, without the detour)
+        return torch.empty(max(int(nbytes), 1), dtype=torch.uint8, device=device)
     return _made(stream, lambda: torch.empty(max(int(nbytes), 1), dtype=torch.uint8, device=device))
 
 
@@ -560,12 +563,22 @@ def dynb_moe_kernels(T: int, d: int, h: int, E: int, k: int, noisy: bool = False
 MOE_PRODUCT_RELU = 1
 
 
-def _dtype_code(t) -> int:
+_F32 = _BF16 = _I8 = _I32 = None                 # torch's, once a tensor has been met
+
+
+def _meet_torch():
+    global _F32, _BF16, _I8, _I32
     import torch
+    _F32, _BF16, _I8, _I32 = torch.float32, torch.bfloat16, torch.int8, torch.int32
+
+
+def _dtype_code(t) -> int:
+    if _F32 is None:
+        _meet_torch()
     dtype = t.dtype
-    if dtype is torch.float32:
+    if dtype is _F32:
         return DYNB_F32
-    assert dtype is torch.bfloat16, dtype
+    assert dtype is _BF16, dtype
     return DYNB_BF16
 
 
@@ -592,10 +605,13 @@ def _twin(stream, t):
 
 
 def _groups_struct(offsets, perm, k: int, M: int, rows: int) -> _Groups:
-    import torch
-    assert offsets.is_cuda and offsets.is_contiguous() and offsets.dtype == torch.int32
-    assert perm is None or (perm.is_cuda and perm.is_contiguous() and perm.dtype == torch.int32 and perm.shape == (M,))
-    return _Groups(offsets.data_ptr(), None if perm is None else perm.data_ptr(), k, rows)
+    if _I32 is None:
+        _meet_torch()
+    assert offsets.is_cuda and offsets.is_contiguous() and offsets.dtype is _I32
+    if perm is None:
+        return _Groups(offsets.data_ptr(), None, k, rows)
+    assert perm.is_cuda and perm.is_contiguous() and perm.dtype is _I32 and perm.shape == (M,)
+    return _Groups(offsets.data_ptr(), perm.data_ptr(), k, rows)
 
 
 def moe_product(x, W, offsets, perm=None, k: int = 1, relu: bool = False, out=None, stream=None):
@@ -664,36 +680,37 @@ MOE_GATE_SILU, MOE_GATE_GELU = 0, 1
 
 
 def _pre_struct(pre, M: int, h: int) -> _GatedPre:
-    import torch
-    rows = pre.q if isinstance(pre, Rows8) else pre
-    stride = rows.stride()
-    assert rows.is_cuda and rows.shape == (M, 2, h) and stride[1] == h and (h == 1 or stride[2] == 1), (rows.shape, stride)
-    row = stride[0] if M > 1 else max(stride[0], 2 * h)
-    if rows is pre:
-        assert rows.dtype is torch.bfloat16
-        return _GatedPre(rows.data_ptr(), row, None, 0, DYNB_BF16)
+    eight = type(pre) is Rows8
+    rows = pre.q if eight else pre
+    s0, s1, s2 = rows.stride()
+    assert rows.is_cuda and rows.shape == (M, 2, h) and s1 == h and (s2 == 1 or h == 1), (rows.shape, rows.stride())
+    if M <= 1:
+        s0 = max(s0, 2 * h)
+    if _BF16 is None:
+        _meet_torch()
+    if not eight:
+        assert rows.dtype is _BF16
+        return _GatedPre(rows.data_ptr(), s0, None, 0, DYNB_BF16)
     scale, n = pre.scale, (h + 31) // 32
-    s = scale.stride()
-    assert rows.dtype is torch.int8 and scale.is_cuda and scale.dtype is torch.bfloat16 and scale.shape == (M, 2, n) and s[1] == n and (n == 1 or s[2] == 1), (scale.shape, s)
-    return _GatedPre(rows.data_ptr(), row, scale.data_ptr(), s[0] if M > 1 else max(s[0], 2 * n), DYNB_I8)
+    c0, c1, c2 = scale.stride()
+    assert rows.dtype is _I8 and scale.dtype is _BF16 and scale.is_cuda and scale.shape == (M, 2, n) and c1 == n and (c2 == 1 or n == 1), (scale.shape, scale.stride())
+    return _GatedPre(rows.data_ptr(), s0, scale.data_ptr(), c0 if M > 1 else max(c0, 2 * n), DYNB_I8)
 
 
 def moe_gated(x, W, offsets, perm=None, k: int = 1, gate: int = MOE_GATE_SILU, out=None, pre=None, stream=None):
     """out[r] = f(x[row(r)] Wg_e^T) (x[row(r)] Wu_e^T) for the rows r of every group e, f SiLU or GELU (tanh form).  x [rows,K], W [E,2,h,K] (Wg, Wu)
     bf16; offsets, perm and k as in moe_product.  pre: what to keep of gate and up for the backward pass, a bf16 tensor [M,2,h] or Rows8(q [M,2,h],
     scale [M,2,(h + 31) // 32]) to be written, or None.  Returns out [M,h] bf16."""
-    import torch
     E, two, h, K = W.shape
-    M = x.shape[0] if perm is None else perm.shape[0]
-    xs = _rows(x, x.shape[0], K)
-    assert two == 2 and W.is_cuda and W.is_contiguous() and W.dtype == x.dtype == torch.bfloat16 and offsets.shape == (E + 1,)
+    n = x.shape[0]
+    M = n if perm is None else perm.shape[0]
+    xs = _rows(x, n, K)
+    g = _groups_struct(offsets, perm, k, M, n)
+    assert two == 2 and W.is_cuda and W.is_contiguous() and W.dtype is x.dtype is _BF16 and len(offsets) == E + 1
     if out is None:
         out = _new(stream, M, h, like=x)
-    os_ = _rows(out, M, h, x)
-    g = _groups_struct(offsets, perm, k, M, x.shape[0])
-    shape = _GatedShape(M, K, h, E, DYNB_BF16, gate)
-    _check(lib.moe_gated(ct.byref(shape), ct.byref(g), x.data_ptr(), xs, W.data_ptr(), out.data_ptr(), os_, None if pre is None else ct.byref(_pre_struct(pre, M, h)),
-                         _stream(stream)))
+    _check(lib.moe_gated(_GatedShape(M, K, h, E, DYNB_BF16, gate), g, x.data_ptr(), xs, W.data_ptr(), out.data_ptr(), _rows(out, M, h, x),
+                         None if pre is None else _pre_struct(pre, M, h), _stream(stream)))
     return out
 
 
@@ -702,22 +719,19 @@ def moe_gated_grad(dout, W, offsets, pre, gate: int = MOE_GATE_SILU, dpre=None, 
     and f(gate) up again, which the second layer's weights' gradient wants.  dout [M,N], W [E,N,h] bf16 (moe_product's second layer), pre as moe_gated kept
     it.  Returns (dpre [M,2,h], hidden [M,h]) bf16, or dpre alone without want_hidden.  dpre.view(M, 2 * h) and W.view(E, 2 * h, K) of moe_gated are what
     moe_product_grad_input and moe_product_grad_weight take."""
-    import torch
     E, N, h = W.shape
     M = dout.shape[0]
     ds = _rows(dout, M, N)
-    assert W.is_cuda and W.is_contiguous() and W.dtype == dout.dtype == torch.bfloat16 and offsets.shape == (E + 1,)
+    g = _groups_struct(offsets, None, 1, M, M)
+    assert W.is_cuda and W.is_contiguous() and W.dtype is dout.dtype is _BF16 and len(offsets) == E + 1
     if dpre is None:
         dpre = _new(stream, M, 2, h, like=dout)
-    assert not isinstance(dpre, Rows8)
+    assert type(dpre) is not Rows8
     d = _pre_struct(dpre, M, h)
     if hidden is None and want_hidden:
         hidden = _new(stream, M, h, like=dout)
-    hs = 0 if hidden is None else _rows(hidden, M, h, dout)
-    g = _groups_struct(offsets, None, 1, M, M)
-    shape = _GatedShape(M, N, h, E, DYNB_BF16, gate)
-    _check(lib.moe_gated_grad(ct.byref(shape), ct.byref(g), dout.data_ptr(), ds, W.data_ptr(), ct.byref(_pre_struct(pre, M, h)), d.rows, d.stride,
-                              None if hidden is None else hidden.data_ptr(), hs, _stream(stream)))
+    to, hs = (None, 0) if hidden is None else (hidden.data_ptr(), _rows(hidden, M, h, dout))
+    _check(lib.moe_gated_grad(_GatedShape(M, N, h, E, DYNB_BF16, gate), g, dout.data_ptr(), ds, W.data_ptr(), _pre_struct(pre, M, h), d.rows, d.stride, to, hs, _stream(stream)))
     return dpre if hidden is None else (dpre, hidden)
 
 
@@ -729,33 +743,32 @@ class Rows8(NamedTuple):
 
 
 def _rows8_struct(r: Rows8, T: int, d: int) -> _Rows8:
-    import torch
-    assert r.q.dtype is torch.int8 and r.scale.dtype is torch.bfloat16
-    return _Rows8(r.q.data_ptr(), _rows(r.q, T, d), r.scale.data_ptr(), _rows(r.scale, T, (d + 31) // 32))
+    if _I8 is None:
+        _meet_torch()
+    q, scale = r
+    assert q.dtype is _I8 and scale.dtype is _BF16
+    return _Rows8(q.data_ptr(), _rows(q, T, d), scale.data_ptr(), _rows(scale, T, (d + 31) // 32))
 
 
 def dynb_store8(x, out=None, stream=None) -> Rows8:
     """Rows x [T,d] float32 or bfloat16 in 8 bits, (q [T,d] int8, scale [T,(d + 31) // 32] bfloat16): s = max|x| / 127 of 32 neighbours, rounded up to a
     bfloat16, q = x / s rounded (both in fp32).  A block with an infinity or a NaN comes back as NaN."""
-    import torch
     T, d = x.shape
     xs = _rows(x, T, d)
-    if out is None:
-        out = Rows8(_new(stream, T, d, like=x, dtype=torch.int8), _new(stream, T, (d + 31) // 32, like=x, dtype=torch.bfloat16))
     shape = _Rows8Shape(T, d, _dtype_code(x))
-    _check(lib.dynb_store8(ct.byref(shape), x.data_ptr(), xs, ct.byref(_rows8_struct(out, T, d)), _stream(stream)))
+    if out is None:
+        out = Rows8(_new(stream, T, d, like=x, dtype=_I8), _new(stream, T, (d + 31) // 32, like=x, dtype=_BF16))
+    _check(lib.dynb_store8(shape, x.data_ptr(), xs, _rows8_struct(out, T, d), _stream(stream)))
     return out
 
 
 def dynb_load8(rows: Rows8, out=None, dtype: int = DYNB_BF16, stream=None):
     """What rows in 8 bits stand for, q s.  Returns a tensor [T,d] of `dtype`, bfloat16 or float32 (`out`: such a tensor, to be overwritten)."""
-    import torch
     T, d = rows.q.shape
+    r = _rows8_struct(rows, T, d)
     if out is None:
-        out = _new(stream, T, d, like=rows.q, dtype=torch.float32 if dtype == DYNB_F32 else torch.bfloat16)
-    os_ = _rows(out, T, d)
-    shape = _Rows8Shape(T, d, _dtype_code(out))
-    _check(lib.dynb_load8(ct.byref(shape), ct.byref(_rows8_struct(rows, T, d)), out.data_ptr(), os_, _stream(stream)))
+        out = _new(stream, T, d, like=rows.q, dtype=_F32 if dtype == DYNB_F32 else _BF16)
+    _check(lib.dynb_load8(_Rows8Shape(T, d, _dtype_code(out)), r, out.data_ptr(), _rows(out, T, d), _stream(stream)))
     return out
 
 
@@ -801,8 +814,9 @@ def dynb_embed_backward(tokens, dout, V: int, scale: float = 1.0, dtable=None, g
 def _fp32(t, n: int):
     if t is None:
         return None
-    import torch
-    assert t.is_cuda and t.dtype is torch.float32 and t.shape == (n,) and t.is_contiguous()
+    if _F32 is None:
+        _meet_torch()
+    assert t.is_cuda and t.dtype is _F32 and t.shape == (n,) and t.is_contiguous()
     return t.data_ptr()
 
 
@@ -833,23 +847,22 @@ def dynb_layer_norm_backward_workspace_bytes(T: int, d: int, dtype: int) -> int:
 def dynb_layer_norm_backward(dy, x, gamma, mean, rstd, dx=None, workspace=None, stream=None):
     """Gradients of dynb_layer_norm: dy, x [T,d], mean and rstd what it returned; x may be Rows8, the layer's input in 8 bits.  Returns (dx [T,d] in the dtype of
     dy, dgamma [d], dbeta [d] float32)."""
-    import torch
     T, d = dy.shape
-    eight = isinstance(x, Rows8)
+    eight = type(x) is Rows8
     ds, xs = _rows(dy, T, d), 0 if eight else _rows(x, T, d, dy)
     if dx is None:
         dx = _new(stream, T, d, like=dy)
     dxs = _rows(dx, T, d, dy)
-    dgamma = _new(stream, d, like=dy, dtype=torch.float32)
-    dbeta = _twin(stream, dgamma)
     shape = _NormShape(T, d, _dtype_code(dy), 0.0)
+    dgamma = _new(stream, d, like=dy, dtype=_F32)
+    dbeta = _twin(stream, dgamma)
     if workspace is None:
-        workspace = _scratch(lib.dynb_layer_norm_backward_workspace_bytes(ct.byref(shape)), dy.device, stream)
+        workspace = _scratch(lib.dynb_layer_norm_backward_workspace_bytes(shape), dy.device, stream)
     rest = (_fp32(gamma, d), _fp32(mean, T), _fp32(rstd, T), dx.data_ptr(), dxs, dgamma.data_ptr(), dbeta.data_ptr(), workspace.data_ptr(), workspace.nbytes, _stream(stream))
     if eight:
-        _check(lib.dynb_layer_norm_backward8(ct.byref(shape), dy.data_ptr(), ds, ct.byref(_rows8_struct(x, T, d)), *rest))
+        _check(lib.dynb_layer_norm_backward8(shape, dy.data_ptr(), ds, _rows8_struct(x, T, d), *rest))
     else:
-        _check(lib.dynb_layer_norm_backward(ct.byref(shape), dy.data_ptr(), ds, x.data_ptr(), xs, *rest))
+        _check(lib.dynb_layer_norm_backward(shape, dy.data_ptr(), ds, x.data_ptr(), xs, *rest))
     return dx, dgamma, dbeta
 
 
