@@ -56,6 +56,29 @@ __device__ __forceinline__ void gated_any(const Args& p, const Gate& gate, const
             return;
         }
         const int rest = t.depth - int(z) - along;
+        if (t.depth >= 8 && (!A_ACROSS || h >= 8)) {
+            // Whole pieces all the same: one that would reach over its row's end is the row's last eight elements, without those that another lane has
+            const int gone = min(max(8 - rest, 0), 8);
+            const int64_t from = gone > 0 ? int64_t(t.depth) - 8 - along : int64_t(z);
+#pragma unroll
+            for (int j = 0; j < EACH; ++j) {
+                const int place = int(z) + copied_place(wave + j * S::WAVES, lane), last = t.depth - 1;
+#pragma unroll
+                for (int i = 0; i < AU; ++i) {
+                    if constexpr (!A_ACROSS) to.a[i][j] = without_first(load_piece(a_at[i][j] + from, 8), gone);
+                    else {
+                        // (over its end is the next row's beginning, in columns that go nowhere, but behind the last row)
+                        const int left = max(a_left[i], 1);
+                        const bool over = place >= last && left < 8;
+                        const u32x4 v = load_piece(w + size_t(min(place, last)) * size_t(p.K) + (h - (over ? 8 : left)), 8);
+                        to.a[i][j] = without_first(v, place > last ? 8 : over ? 8 - left : 0);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < BU; ++i) to.b[i][j] = without_first(load_piece(b_at[i][j] + from, 8), gone);
+            }
+            return;
+        }
 #pragma unroll
         for (int j = 0; j < EACH; ++j) {
             const int place = int(z) + copied_place(wave + j * S::WAVES, lane);

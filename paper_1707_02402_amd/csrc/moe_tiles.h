@@ -260,9 +260,17 @@ struct KeptEight<KEEP_8, WHOLE> {
         u = load_eight(from + gate.h, WHOLE ? 8 : left);
         sg = scale[0];
         su = scale[gate.blocks()];
+        if constexpr (!WHOLE) {                                // (eight features that begin anywhere are of two blocks)
+            within = BLOCK8 - c % BLOCK8;
+            const int next = (c + min(left, 8) - 1) / BLOCK8 - c / BLOCK8;
+            sg2 = scale[next];
+            su2 = scale[next + gate.blocks()];
+        }
     }
-    __device__ __forceinline__ float gate_at(int i) const { return unpack8(g[i >> 2], i & 3) * bf16_to_f32(sg); }
-    __device__ __forceinline__ float up_at(int i) const { return unpack8(u[i >> 2], i & 3) * bf16_to_f32(su); }
+    __device__ __forceinline__ float gate_at(int i) const { return unpack8(g[i >> 2], i & 3) * bf16_to_f32(WHOLE || i < within ? sg : sg2); }
+    __device__ __forceinline__ float up_at(int i) const { return unpack8(u[i >> 2], i & 3) * bf16_to_f32(WHOLE || i < within ? su : su2); }
+    bf16_t sg2, su2;
+    int within;
 };
 __device__ __forceinline__ u32x4 pack_eight(const float* v) { return u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])}; }
 
@@ -418,7 +426,10 @@ __device__ __forceinline__ void leave_grads(f32x16 (&acc)[S::FA][LIVE > 0 ? LIVE
     constexpr int FA = S::FA, PIECES = FA * 8, LANES = FA * 4, AT_ONCE = 64 / LANES, STORES = 32 / AT_ONCE;
     static_assert(32 * PIECES * 16 <= ROOM, "room");
     asm volatile("" : "+v"(lane));                             // (as above)
-    const int q = lane & 31, hk = lane >> 5, h = gate.h, col = lane % LANES * 8, row = lane / LANES, c = now.c0 + cg * (FA * 32) + col, cols = h - c;
+    const int q = lane & 31, hk = lane >> 5, h = gate.h, row = lane / LANES, first = now.c0 + cg * (FA * 32);
+    // a lane's eight columns of the wave's: where the row ends among them, the row's last eight (some of which another lane makes and stores, too, the same)
+    const bool ends = !WHOLE && first + FA * 32 > h && first + 8 <= h;
+    const int col = ends ? min(lane % LANES * 8, h - 8 - first) : lane % LANES * 8, c = first + col, cols = first + lane % LANES * 8 < h ? h - c : 0;
     auto put = [&](int64_t at, const u32x4& dg, const u32x4& du, const u32x4& f) {
         put_past(WHOLE && gate.past, [&](auto past) {
             constexpr bool PAST = decltype(past)::value;
@@ -458,8 +469,13 @@ __device__ __forceinline__ void leave_grads(f32x16 (&acc)[S::FA][LIVE > 0 ? LIVE
         for (int i = 0; i < STORES; ++i) {
             const int r = row + i * AT_ONCE;
             f32x4 d[2];
+            if (WHOLE || !ends)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) d[j] = *(const lds_f32x4*)(room + uint32_t((r * PIECES + ((col / 4 + j) ^ (r & (PIECES - 1)))) * 16));
+                for (int j = 0; j < 2; ++j) d[j] = *(const lds_f32x4*)(room + uint32_t((r * PIECES + ((col / 4 + j) ^ (r & (PIECES - 1)))) * 16));
+            else
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    d[e >> 2][e & 3] = *(const __attribute__((address_space(3))) float*)(room + uint32_t((r * PIECES + (((col + e) / 4) ^ (r & (PIECES - 1)))) * 16 + (col + e) % 4 * 4));
             if (i * AT_ONCE >= left) continue;
             float dg[8], du[8], f[8];
 #pragma unroll

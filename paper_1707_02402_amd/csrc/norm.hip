@@ -129,12 +129,13 @@ struct RowsOf {
     const T* x;
     int64_t stride;
     using Raw = u32x4;
-    __device__ __forceinline__ Raw load(int64_t row, int c, int d) const { return load_piece(x + row * stride + c, d - c); }
+    __device__ __forceinline__ Raw load(int64_t row, int c, int, int d) const { return load_piece(x + row * stride + c, d - c); }
     static __device__ __forceinline__ float value(const Raw& v, int j) { return element<T>(v, j); }
     static __device__ __forceinline__ float sum(float v) { return wave_sum(v); }
     __device__ __forceinline__ float at(int64_t row, int c) const { return load_f32(x + row * stride + c); }
 };
-// WHOLE: d is a multiple of a piece's elements, so that a piece is there or is not
+// WHOLE: d is a piece's elements or more, and every load is a whole piece: a lane whose piece would reach over the row's end takes the row's last one instead, and of that only the
+// elements that no other lane has (65536 x 1001 bf16: 131 us element by element, 61 so)
 template <typename T, bool WHOLE_>
 struct Rows8 {
     static constexpr bool WHOLE = WHOLE_;
@@ -144,12 +145,14 @@ struct Rows8 {
     int64_t scale_stride;
     bool past;                // dx goes past the caches
     struct Raw { u32x2 q; float s; };
-    __device__ __forceinline__ Raw load(int64_t row, int c, int d) const
+    // the piece from c, in its own place the one from `own`
+    __device__ __forceinline__ Raw load(int64_t row, int c, int own, int d) const
     {
-        if (c >= d) return Raw{{0u, 0u}, 0.f};
+        if (!WHOLE && c >= d) return Raw{{0u, 0u}, 0.f};
         const int left = WHOLE ? 8 : d - c;
-        if constexpr (PIECE<T> == 8) return Raw{load_eight(q + row * stride + c, left), bf16_to_f32(scale[row * scale_stride + c / BLOCK8])};
-        else return Raw{{load_four(q + row * stride + c, left), 0u}, bf16_to_f32(scale[row * scale_stride + c / BLOCK8])};
+        const float s = bf16_to_f32(scale[row * scale_stride + min(own, d - 1) / BLOCK8]);
+        if constexpr (PIECE<T> == 8) return Raw{load_eight(q + row * stride + c, left), s};
+        else return Raw{{load_four(q + row * stride + c, left), 0u}, s};
     }
     static __device__ __forceinline__ float value(const Raw& v, int j) { return unpack8(v.q[j >> 2], j & 3) * v.s; }
     static __device__ __forceinline__ float sum(float v) { return wave_sum_in_registers(v); }
@@ -176,12 +179,24 @@ __device__ __forceinline__ void norm_grad_rows(const T* dy, int64_t dy_stride, X
     __shared__ float room[2][2][WAVES > 1 ? WAVES : 1];
     __shared__ float share[WAVES == 1 ? 3 : 1][WAVES == 1 ? 64 * NV * P : 1];
     const int lane = threadIdx.x & (NL - 1), wave = threadIdx.x >> 6;
+    // a lane's columns of piece i; WHOLE: where they begin, and which of them are its own
+    auto own = [&](int i) { return (i * NL + lane) * P; };
+    auto at = [&](int i) { return X::WHOLE ? min(own(i), d - P) : own(i); };
+    u32x4 mine_of[X::WHOLE ? NV : 1];
+    if constexpr (X::WHOLE)
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const int skip = own(i) < d ? own(i) - at(i) : P;
+                mine_of[i][w] = P == 4 ? (w >= skip ? ~0u : 0u) : (2 * w >= skip ? 0xffffu : 0u) | (2 * w + 1 >= skip ? 0xffff0000u : 0u);
+            }
     float g_[NV][P], dg[NV][P], db[NV][P];
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
         for (int h = 0; h < P; h += 4) {
-            const int c = (i * NL + lane) * P + h;
+            const int c = at(i) + h;
             const u32x4 g = gamma ? load_piece(gamma + c, d - c) : u32x4{0x3f800000u, 0x3f800000u, 0x3f800000u, 0x3f800000u};
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -196,10 +211,9 @@ __device__ __forceinline__ void norm_grad_rows(const T* dy, int64_t dy_stride, X
     auto load = [&](int64_t row) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int c = (i * NL + lane) * P;
-            if constexpr (X::WHOLE) a[i] = c < d ? load_piece(dy + row * dy_stride + c, P) : u32x4{0u, 0u, 0u, 0u};
-            else a[i] = load_piece(dy + row * dy_stride + c, d - c);
-            b[i] = x.load(row, c, d);
+            const int c = at(i);
+            a[i] = load_piece(dy + row * dy_stride + c, X::WHOLE ? P : d - c);
+            b[i] = x.load(row, c, own(i), d);
         }
         m = mean[row];
         r = rstd[row];
@@ -209,11 +223,15 @@ __device__ __forceinline__ void norm_grad_rows(const T* dy, int64_t dy_stride, X
     int turn = 0;
     for (; row < n; row += step) {
         float v[NV][P], h[NV][P], s1 = 0.f, s2 = 0.f;
+        if constexpr (X::WHOLE)
+#pragma unroll
+            for (int i = 0; i < NV; ++i) a[i] &= mine_of[i];
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
             for (int j = 0; j < P; ++j) {
-                const bool on = (i * NL + lane) * P + (X::WHOLE ? 0 : j) < d;                // (what lies behind the row must not count, whatever mean and rstd are)
+                // (what lies behind the row must not count, whatever mean and rstd are.  WHOLE: it is another column of the row, and its dy is taken for 0)
+                const bool on = X::WHOLE || (i * NL + lane) * P + j < d;
                 h[i][j] = on ? (X::value(b[i], j) - m) * r : 0.f;
                 const float y = element<T>(a[i], j);
                 dg[i][j] += y * h[i][j];
@@ -257,12 +275,16 @@ __device__ __forceinline__ void norm_grad_rows(const T* dy, int64_t dy_stride, X
 #pragma unroll
                 for (int j = 0; j < P; ++j) v[i][j] = r0 * (v[i][j] - m1 - h[i][j] * m2);
                 if constexpr (X::WHOLE) {
-                    T* const to = dx + here * dx_stride + c;
-                    if (c < d)
+                    T* const to = dx + here * dx_stride + at(i);
+                    if (own(i) <= d - P)
                         put_past(x.past, [&](auto past) {
                             if constexpr (decltype(past)::value) store_past(to, v[i]);
                             else store_piece<P>(to, P, v[i]);
                         });
+                    else
+#pragma unroll
+                        for (int j = 1; j < P; ++j)
+                            if (at(i) + j >= own(i)) store_f32(to + j, v[i][j]);
                 } else store_piece<P>(dx + here * dx_stride + c, d - c, v[i]);
             }
         }
@@ -286,7 +308,11 @@ __device__ __forceinline__ void norm_grad_rows(const T* dy, int64_t dy_stride, X
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = (i * NL + lane) * P;
-            store_piece<P>(mine + size_t(which) * size_t(d) + c, d - c, sum[i]);
+            if constexpr (X::WHOLE) {
+#pragma unroll
+                for (int j = 0; j < P; ++j)
+                    if (own(i) < d && at(i) + j >= own(i)) mine[size_t(which) * size_t(d) + size_t(at(i) + j)] = sum[i][j];
+            } else store_piece<P>(mine + size_t(which) * size_t(d) + c, d - c, sum[i]);
         }
     }
 }
@@ -536,8 +562,9 @@ int norm_backward(const dynb_norm_shape* s, const void* dy, int64_t dy_stride, c
         T* const to = static_cast<T*>(dx);
         if constexpr (WAVES > 0) {
             const dim3 threads(WAVES == 1 ? 256 : WAVES * 64);
-            if (lines > 0 && rows && s->d % PIECE<T> == 0)
-                hipLaunchKernelGGL((k_norm8_grad<T, NV, WAVES, true>), dim3(unsigned(lines)), threads, 0, st, a, dy_stride, Rows8<T, true>{r.q, r.stride, r.scale, r.scale_stride, int64_t(s->T) * s->d * int64_t(sizeof(T)) >= PAST}, gamma, mean, rstd,
+            constexpr bool WHOLE = !(WAVES == 16 && NV * PIECE<T> == LANE);                  // (there is no room for the masks there)
+            if (lines > 0 && rows && WHOLE && s->d >= PIECE<T>)
+                hipLaunchKernelGGL((k_norm8_grad<T, NV, WAVES, WHOLE>), dim3(unsigned(lines)), threads, 0, st, a, dy_stride, Rows8<T, WHOLE>{r.q, r.stride, r.scale, r.scale_stride, int64_t(s->T) * s->d * int64_t(sizeof(T)) >= PAST}, gamma, mean, rstd,
                                    to, dx_stride, partial, s->T, s->d);
             else if (lines > 0 && rows)
                 hipLaunchKernelGGL((k_norm8_grad<T, NV, WAVES, false>), dim3(unsigned(lines)), threads, 0, st, a, dy_stride, r, gamma, mean, rstd, to, dx_stride, partial, s->T, s->d);

@@ -32,6 +32,18 @@ template <> __device__ __forceinline__ u32x4 load_piece<float>(const float* p, i
     return v;
 }
 
+// a piece without its first n elements of bfloat16 (0 to 8), zeros behind the others
+__device__ __forceinline__ u32x4 without_first(const u32x4& v, int n)
+{
+    uint64_t lo = uint64_t(v[1]) << 32 | v[0], hi = uint64_t(v[3]) << 32 | v[2];
+    lo = n >= 4 ? hi : lo;
+    hi = n >= 4 ? 0 : hi;
+    const int bits = (n & 3) * 16;
+    lo = lo >> bits | hi << 1 << (63 - bits);
+    hi >>= bits;
+    return n >= 8 ? u32x4{0u, 0u, 0u, 0u} : u32x4{uint32_t(lo), uint32_t(lo >> 32), uint32_t(hi), uint32_t(hi >> 32)};
+}
+
 // the same in pieces of E elements: 8 bytes of bfloat16 (E = 4), or 16
 template <typename T, int E> using Piece = std::conditional_t<(E * sizeof(T) == 8), u32x2, u32x4>;
 template <int E, typename T> __device__ __forceinline__ Piece<T, E> load_some(const T* p, int left)
