@@ -230,6 +230,8 @@ int launch_kind(const moe_product_shape* s, const Args& p, const Gate& gate, hip
     else return launch_with(k_gated<DIR, S, KEEP>, asked, LDS_BYTES<DIR, S>, grid, S::THREADS, st, who, p, g, int(units), ct);
 }
 
+// Few with waves of 64 columns and 32 rows: what is kept in 8 bits shares a scale among 32 features, and they have to be a wave's
+using FewWide = Kind<2, 1, 2, 2, 3, 2>;
 using AnyMid = Kind<2, 2, 2, 2, 2, 2>;   // 128 x 128
 using AnyFew = Kind<2, 1, 2, 2, 2, 2>;   // 128 columns x 64 rows
 
@@ -239,11 +241,7 @@ int launch_gated(const moe_product_shape* s, const Args& p, const Gate& gate, bo
     auto keeping = [&](auto kind, auto any) {
         using S = decltype(kind);
         constexpr bool ANY = decltype(any)::value;
-        if (gate.keep == KEEP_8) {
-            // (8 bits: 32 features have to be a wave's)
-            if constexpr (DIR == FORWARD && S::FA < 2) return launch_kind<DIR, Mid, KEEP_8, ANY>(s, p, gate, st, who);
-            else return launch_kind<DIR, S, KEEP_8, ANY>(s, p, gate, st, who);
-        }
+        if (gate.keep == KEEP_8) return launch_kind<DIR, std::conditional_t<DIR == FORWARD && S::FA == 1, FewWide, S>, KEEP_8, ANY>(s, p, gate, st, who);
         if constexpr (DIR == FORWARD)
             if (gate.keep == KEEP_NOTHING) return launch_kind<DIR, S, KEEP_NOTHING, ANY>(s, p, gate, st, who);
         return launch_kind<DIR, S, KEEP_BF16, ANY>(s, p, gate, st, who);
