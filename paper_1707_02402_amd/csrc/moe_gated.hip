@@ -232,6 +232,8 @@ int launch_kind(const moe_product_shape* s, const Args& p, const Gate& gate, hip
 
 // Few with waves of 64 columns and 32 rows: what is kept in 8 bits shares a scale among 32 features, and they have to be a wave's
 using FewWide = Kind<2, 1, 2, 2, 3, 2>;
+// Half of Few's columns: twice the workgroups where Few's leave half of the CUs without work
+using Narrow = Kind<1, 1, 2, 2, 3, 2>;
 using AnyMid = Kind<2, 2, 2, 2, 2, 2>;   // 128 x 128
 using AnyFew = Kind<2, 1, 2, 2, 2, 2>;   // 128 columns x 64 rows
 
@@ -251,7 +253,10 @@ int launch_gated(const moe_product_shape* s, const Args& p, const Gate& gate, bo
     switch (kind) {
     case BIG: return keeping(Big{}, std::false_type{});
     case MID: return keeping(Mid{}, std::false_type{});
-    default: return keeping(Few{}, std::false_type{});
+    default: {
+        const int wide = DIR == FORWARD ? Few::COLS / 2 : Few::COLS;
+        return most_pieces(s->M, s->E, Few::ROWS) * ((gate.h + wide - 1) / wide) <= CUS / 2 ? keeping(Narrow{}, std::false_type{}) : keeping(Few{}, std::false_type{});
+    }
     }
 }
 

@@ -284,7 +284,7 @@ __device__ __forceinline__ void leave_pairs(f32x16 (&acc)[S::FA][LIVE > 0 ? LIVE
 {
     using lds_u32x4 = __attribute__((address_space(3))) u32x4;
     using lds_u32x2 = __attribute__((address_space(3))) u32x2;
-    constexpr int FA = S::FA, PARTS = KEEP == KEEP_BF16 ? 3 : 1, PITCH = FA * 32 + 16, PART = 32 * PITCH, PITCH8 = FA * 16 + 16, PART8 = 32 * PITCH8;
+    constexpr int FA = S::FA, PARTS = KEEP == KEEP_BF16 ? 3 : 1, PITCH = FA * 32 + (FA > 1 ? 16 : 0), PART = 32 * PITCH, PITCH8 = FA * 16 + 16, PART8 = 32 * PITCH8;
     constexpr int LANES = FA * 2, AT_ONCE = 64 / LANES, STORES = 32 / AT_ONCE;
     static_assert(KEEP != KEEP_8 || FA % 2 == 0, "a block of 32 features");
     static_assert(PARTS * PART + (KEEP == KEEP_8 ? 2 * PART8 : 0) <= ROOM, "room");
