@@ -571,8 +571,8 @@ typedef struct {
 } dynb_rows8_shape;
 
 /* x, device [T][d] dtype, rows x_stride elements apart, into 8 bits; and what they stand for, rounded to dtype, back into x.
- * Errors: DYNB_E_INVAL (NULL, sizes <= 0, strides below a row's length, misaligned), DYNB_E_UNSUPPORTED (dtype, more than 2^28
- * columns), DYNB_E_HIP.                                                                          */
+ * x and rows may not overlap.  Errors: DYNB_E_INVAL (NULL, sizes <= 0, strides below a row's length, misaligned),
+ * DYNB_E_UNSUPPORTED (dtype, more than 2^28 columns), DYNB_E_HIP.                                */
 int dynb_store8(const dynb_rows8_shape* shape, const void* x, int64_t x_stride, const dynb_rows8* rows, void* stream);
 int dynb_load8(const dynb_rows8_shape* shape, const dynb_rows8* rows, void* x, int64_t x_stride, void* stream);
 

@@ -260,12 +260,12 @@ int launch_gated(const moe_product_shape* s, const Args& p, const Gate& gate, bo
     }
 }
 
-// whether what is kept lies on borders of 8 elements
+// whether what is kept lies on borders of 8 elements, and 32 rows of scales within 32 bits
 bool kept_on_8(const moe_gated_pre* p)
 {
     if (!p) return true;
     if (p->dtype == DYNB_BF16) return p->stride % 8 == 0 && on_16({p->rows});
-    return p->stride % 8 == 0 && (reinterpret_cast<uintptr_t>(p->rows) & 7) == 0;
+    return p->stride % 8 == 0 && (reinterpret_cast<uintptr_t>(p->rows) & 7) == 0 && p->scale_stride <= 1 << 27;
 }
 
 }  // namespace
