@@ -112,17 +112,8 @@ __device__ __forceinline__ float wave_sum_in_registers(float v)
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-__device__ __forceinline__ void store_past(bf16_t* p, const float (&v)[8])
-{
-    __builtin_nontemporal_store(u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])}, reinterpret_cast<u32x4_at2*>(p));
-}
-__device__ __forceinline__ void store_past(float* p, const float (&v)[4])
-{
-    __builtin_nontemporal_store(u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])}, reinterpret_cast<u32x4_at4*>(p));
-}
-
-// The backward pass's x as it lies (RowsOf), or in 8 bits (Rows8).  From 8 bits 65536 x 1024 take bf16 62 us (340 MB, 5.4 TB/s) where x in bf16 takes 74, fp32 136 (610 MB, 4.5); 4097 x 777 fp32,
-// which wait for their rows' loads, 11.3.
+// The backward pass's x as it lies (RowsOf), or in 8 bits (Rows8).  From 8 bits 65536 x 1024 bf16 take 57 us (340 MB, 6.0 TB/s) where x in bf16 takes 74, 65536 x 1000 fp32 111 (595 MB, 5.3; 152);
+// 4097 x 777 fp32, which wait for their rows' loads, 11.
 template <typename T>
 struct RowsOf {
     static constexpr bool WHOLE = false;

@@ -111,6 +111,16 @@ __device__ __forceinline__ void put_past(bool past, F put)
     } else put(std::false_type{});
 }
 
+// a piece of 16 bytes past the caches, at any element's address
+__device__ __forceinline__ void store_past(bf16_t* p, const float (&v)[8])
+{
+    __builtin_nontemporal_store(u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])}, reinterpret_cast<u32x4_at2*>(p));
+}
+__device__ __forceinline__ void store_past(float* p, const float (&v)[4])
+{
+    __builtin_nontemporal_store(u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])}, reinterpret_cast<u32x4_at4*>(p));
+}
+
 __device__ __forceinline__ float wave_sum(float v)
 {
 #pragma unroll

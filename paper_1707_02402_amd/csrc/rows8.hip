@@ -13,7 +13,8 @@ using dynb::fail;
 
 namespace {
 
-// A lane has 8 elements of a block, four neighbouring lanes a block.
+// A lane has 8 elements of a block, four neighbouring lanes a block, who exchange their largest.  A row is read once and what is written is half of it or a quarter: memory bounds it
+// (65536 x 1024: bf16 35 us, 200 MB at 5.9 TB/s, fp32 57, 338 MB at 5.8).
 template <typename T>
 __global__ __launch_bounds__(256) void k_store8(const T* __restrict__ x, int64_t x_stride, int8_t* __restrict__ q, int64_t q_stride, bf16_t* __restrict__ scale, int64_t scale_stride, int d,
                                                 int pieces, int64_t all)
@@ -42,24 +43,28 @@ __global__ __launch_bounds__(256) void k_store8(const T* __restrict__ x, int64_t
     }
 }
 
+// A lane has what one store of 16 bytes takes, so that the stores of a wave lie side by side; large results go past the caches (65536 x 1024: bf16 31 us, 6.6 TB/s; fp32 47, 7.2, where 8
+// elements a lane, in two stores, took 62, and past the caches 100; rows of 1001: 33 and 52).
 template <typename T>
 __global__ __launch_bounds__(256) void k_load8(const int8_t* __restrict__ q, int64_t q_stride, const bf16_t* __restrict__ scale, int64_t scale_stride, T* __restrict__ x, int64_t x_stride, int d,
                                                int pieces, int64_t all, bool past)
 {
+    constexpr int P = PIECE<T>;
     for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < all; i += int64_t(gridDim.x) * 256) {
         const int64_t row = i / pieces;
-        const int c = int(i - row * pieces) * 8, left = d - c;
-        const u32x2 raw = load_eight(q + row * q_stride + c, left);
+        const int c = int(i - row * pieces) * P, left = d - c;
+        const int8_t* const from = q + row * q_stride + c;
+        u32x2 raw;
+        if constexpr (P == 8) raw = load_eight(from, left);
+        else raw = u32x2{load_four(from, left), 0u};
         const float s = bf16_to_f32(scale[row * scale_stride + c / BLOCK8]);
-        float v[8];
+        float v[P];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = unpack8(raw[j >> 2], j & 3) * s;
+        for (int j = 0; j < P; ++j) v[j] = unpack8(raw[j >> 2], j & 3) * s;
         T* const to = x + row * x_stride + c;
         put_past(past, [&](auto past_) {
-            if (decltype(past_)::value && sizeof(T) == 2 && left >= 8) {
-                const u32x4 packed = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
-                __builtin_nontemporal_store(packed, reinterpret_cast<u32x4_at2*>(to));
-            } else store_piece<8>(to, left, v);
+            if (decltype(past_)::value && left >= P) store_past(to, v);
+            else store_piece<P>(to, left, v);
         });
     }
 }
@@ -105,9 +110,9 @@ extern "C" int dynb_load8(const dynb_rows8_shape* s, const dynb_rows8* rows, voi
     const int rc = check(s, x, x_stride, rows, "dynb_load8");
     if (rc != DYNB_OK || s->T == 0) return rc;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const int d = s->d, pieces = (d + 7) / 8;
+    const int d = s->d, piece = s->dtype == DYNB_BF16 ? 8 : 4, pieces = (d + piece - 1) / piece;
     const int64_t all = int64_t(s->T) * pieces;
-    const bool past = s->dtype == DYNB_BF16 && int64_t(s->T) * d * 2 >= PAST;               // (fp32: a lane's 32 bytes are two stores, 100 us past the caches where 62 do)
+    const bool past = int64_t(s->T) * d * (s->dtype == DYNB_BF16 ? 2 : 4) >= PAST;
     const dim3 grid(unsigned(std::min((all + 255) / 256, MOST_GROUPS)));
     if (s->dtype == DYNB_BF16) hipLaunchKernelGGL((k_load8<bf16_t>), grid, dim3(256), 0, st, static_cast<const int8_t*>(rows->q), rows->q_stride, static_cast<const bf16_t*>(rows->scale), rows->scale_stride, static_cast<bf16_t*>(x), x_stride, d, pieces, all, past);
     else hipLaunchKernelGGL((k_load8<float>), grid, dim3(256), 0, st, static_cast<const int8_t*>(rows->q), rows->q_stride, static_cast<const bf16_t*>(rows->scale), rows->scale_stride, static_cast<float*>(x), x_stride, d, pieces, all, past);
