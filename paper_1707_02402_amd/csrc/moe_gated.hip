@@ -1,5 +1,16 @@
 // The first half of a gated feed-forward layer of experts, out = f(in Wg_e^T) (in Wu_e^T), and the gradients of its gate and up through the second layer's product:
 // dact = dout W_e, dgate = dact up f'(gate), dup = dact f(gate).  W is [E][2][h][K], so that [dgate, dup] and W are an ordinary layer's (N = 2 h) for the products that remain.
+//
+// Either is one launch: the products are the tiles of moe_tiles.h, and the gate is where a tile leaves, on sums in fp32.  A wave has gate and up of the same features in the same lane
+// (pair_feature), so the forward pass writes h numbers a row where a product and a gate of its own would write 2 h, read them and write h; what the backward pass needs is written
+// beside, in bfloat16 or 8 bits.  Backward a tile's dact never leaves the CU.
+// Bounds: products where a group has hundreds of rows, the weights' bytes where it has few.  us on this card (products by hipBLASLt reach 1.36 PFLOP/s, copies 4.8 TB/s):
+//   forward, 8192 rows, 2048 -> 2 x 4096, one expert       224 (1.23 PFLOP/s), with the pair in bf16 236, in 8 bits 243.  206 of them are the tiles' loop
+//   forward, 65536 rows, 1024 -> 2 x 2048, 64 experts      585 (0.94 PFLOP/s), 640, 685.  505 are the loop: 16 chunks a tile, and one wave a SIMD, which multiplies nothing while a
+//                                                          tile leaves; of the rest the stores are 15 without a pair, the arithmetic in 8 bits 40
+//   backward, 65536 rows, 1024 x 2048, 64 experts          490 from bf16, 467 from 8 bits: 275 GFLOP and 1.4 GB; without the stores 340
+//   forward, 148 rows, 256 experts, 1024 -> 2 x 2048       91 (504 MB of weights at 5.5 TB/s)
+//   backward, 16384 rows, 256 experts, 512 x 1024          78 to 82 (360 MB at 4.5 TB/s)
 #include "moe_tiles.h"
 
 namespace {
@@ -7,7 +18,8 @@ namespace {
 // ------------------------------------------------------------------------------------------ any size, stride and address
 // 128 columns (64 features' gate and up) by 128 or 64 rows, by way of registers: pieces of 16 bytes are loaded from wherever they lie and wait there, DEPTH chunks of 64 places of the sum
 // ahead, then go where a copy would have put them.  Places of rows and features are found once a tile; behind a tile's last row or feature the last one is loaded again, and the
-// results that it gives go nowhere.  Only the last chunk looks where its rows end.
+// results that it gives go nowhere.  Only the last chunk looks where its rows end.  A chunk's arithmetic (16 products a wave) covers a fraction of
+// memory's latency: with one chunk ahead 3001 rows, 777 -> 2 x 1001, 8 experts take 47 us, with three 28 (776 -> 2 x 1000 by the kernels below: 19).
 template <int DIR, class S, int KEEP, int DEPTH>
 __device__ __forceinline__ void gated_any(const Args& p, const Gate& gate, const Tile& t, lds_ptr lds)
 {
@@ -230,9 +242,11 @@ int launch_kind(const moe_product_shape* s, const Args& p, const Gate& gate, hip
     else return launch_with(k_gated<DIR, S, KEEP>, asked, LDS_BYTES<DIR, S>, grid, S::THREADS, st, who, p, g, int(units), ct);
 }
 
-// Few with waves of 64 columns and 32 rows: what is kept in 8 bits shares a scale among 32 features, and they have to be a wave's
+// Few with waves of 64 columns and 32 rows: what is kept in 8 bits shares a scale among 32 features, which have to be a wave's (148 rows, 256 experts, 1024 -> 2 x 2048: 94 us, by
+// Mid 104, Few without a pair 91)
 using FewWide = Kind<2, 1, 2, 2, 3, 2>;
-// Half of Few's columns: twice the workgroups where Few's leave half of the CUs without work
+// Half of Few's columns: twice the workgroups where Few's leave half of the CUs without work.  What bounds those is the way of a workgroup's stream of weights into its CU (one row,
+// 2048 -> 2 x 4096: 13.4 us by Few, 11.9 so; backward 14.8, 12.2; 64 rows, 1024 -> 2 x 2048: 8.9, 7.7; backward 11.0, 8.6; five chunks ahead instead of two: 12.8)
 using Narrow = Kind<1, 1, 2, 2, 3, 2>;
 using AnyMid = Kind<2, 2, 2, 2, 2, 2>;   // 128 x 128
 using AnyFew = Kind<2, 1, 2, 2, 2, 2>;   // 128 columns x 64 rows
@@ -248,6 +262,19 @@ int launch_gated(const moe_product_shape* s, const Args& p, const Gate& gate, bo
             if (gate.keep == KEEP_NOTHING) return launch_kind<DIR, S, KEEP_NOTHING, ANY>(s, p, gate, st, who);
         return launch_kind<DIR, S, KEEP_BF16, ANY>(s, p, gate, st, who);
     };
+    // The products' rule.  us of the gated layer, forward without a pair / backward from bf16, by rows, K, h, experts, Zipf exponent:
+    //                                   Big          Mid          Few
+    //   1000 x 1024 x 512, 8, 0.5       29 / 42      14 / 14      10 / 9
+    //   3000 x 2048 x 1024, 1           47 / 61      30 / 30      37 / 25
+    //   4096 x 2048 x 1024, 16, 0.6     58 / 63      55 / 33      64 / 41
+    //   8192 x 512 x 1024, 64, 0.8      52 / 57      39 / 33      42 / 32
+    //   16384 x 512 x 1024, 256, 0.8   160 / 126    146 / 96     133 / 98
+    //   16384 x 1024 x 1024, 64, 0.8   120 / 84     108 / 69     124 / 77
+    //   32768 x 1024 x 1024, 32, 0.6   149 / 130    162 / 112    204 / 133
+    //   65536 x 512 x 512, 64, 0.6      92 / 100     92 / 80     117 / 93
+    //   65536 x 1024 x 1024, 256, 0.6  412 / 315    461 / 314    521 / 362
+    //   65536 x 1024 x 2048, 64, 0.6   586 / 489    845 / 541   1207 / 679
+    // (the rule takes the best of a line or one within 5 %; with the pair in 8 bits 16384 rows of 2048 -> 2 x 1024 take 170 by Big, 159 by Mid)
     const KindOf kind = kind_of(s, DIR == FORWARD ? s->N : s->K, DIR == FORWARD ? s->K : s->N);
     if (!fast) return kind == FEW ? keeping(AnyFew{}, std::true_type{}) : keeping(AnyMid{}, std::true_type{});
     switch (kind) {

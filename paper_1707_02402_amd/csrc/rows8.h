@@ -23,8 +23,8 @@ __device__ __forceinline__ Scale8 scale8(uint32_t largest)
     return Scale8{s, 1.f / s};
 }
 // For numbers that are sums in fp32 themselves: the quotients as products with 1 / 127 and a reciprocal to 1 ulp, and the product and its rounding in one step.  s may then be the
-// next number where a / 127 is one of 8 bits, and q the other neighbour where x / s is within 2^-16 of the middle between two.  (The two divisions and the steps that fall away are a
-// fifth of a gated layer's instructions behind its products: 65536 rows, 1024 -> 2 x 2048, 695 -> 670 us.)
+// next number where a / 127 is one of 8 bits, and q the other neighbour where x / s is within 2^-16 of the middle between two.  (A gated
+// layer's forward pass makes 8192 elements a wave between two tiles' products, while the matrix pipes wait: 65536 rows, 1024 -> 2 x 2048, 695 -> 690 us.)
 __device__ __forceinline__ Scale8 scale8_of_sums(uint32_t largest)
 {
     if (largest >= 0x7f800000u) return Scale8{__uint_as_float(0x7fc00000u), 0.f};
