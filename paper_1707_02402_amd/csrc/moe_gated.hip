@@ -10,7 +10,7 @@
 //                                                          tile leaves; of the rest the stores are 15 without a pair, the arithmetic in 8 bits 40
 //   backward, 65536 rows, 1024 x 2048, 64 experts          490 from bf16, 467 from 8 bits: 275 GFLOP and 1.4 GB; without the stores 340
 //   forward, 148 rows, 256 experts, 1024 -> 2 x 2048       91 (504 MB of weights at 5.5 TB/s)
-//   backward, 16384 rows, 256 experts, 512 x 1024          78 to 82 (360 MB at 4.5 TB/s)
+//   backward, 8192 rows, 256 experts, 512 x 1024           78 to 82 (360 MB at 4.5 TB/s)
 #include "moe_tiles.h"
 
 namespace {
@@ -19,7 +19,7 @@ namespace {
 // 128 columns (64 features' gate and up) by 128 or 64 rows, by way of registers: pieces of 16 bytes are loaded from wherever they lie and wait there, DEPTH chunks of 64 places of the sum
 // ahead, then go where a copy would have put them.  Places of rows and features are found once a tile; behind a tile's last row or feature the last one is loaded again, and the
 // results that it gives go nowhere.  Only the last chunk looks where its rows end.  A chunk's arithmetic (16 products a wave) covers a fraction of
-// memory's latency: with one chunk ahead 3001 rows, 777 -> 2 x 1001, 8 experts take 47 us, with three 28 (776 -> 2 x 1000 by the kernels below: 19).
+// memory's latency: with one chunk ahead 3001 rows, 777 -> 2 x 1001, 8 experts take 47 us, with three 28 (776 -> 2 x 1000 by the kernels below: 20).
 template <int DIR, class S, int KEEP, int DEPTH>
 __device__ __forceinline__ void gated_any(const Args& p, const Gate& gate, const Tile& t, lds_ptr lds)
 {
