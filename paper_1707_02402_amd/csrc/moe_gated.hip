@@ -172,6 +172,63 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_gated(Args p, GateKeepi
     product_tiles<DIR, bf16_t, S, false>(p, gate, units, ct, 1, Shares{}, nullptr);
 }
 
+// ------------------------------------------------------------------------------------------ few rows, nothing kept
+// Tokens that are being answered: their experts' weights are read once, and that is all there is to do.  A workgroup takes NA blocks of 8 features, each 16 rows of weights (of four
+// neighbours: gate's of two features, up's of the same, which are a lane's four sums), and up to 16 rows of one group: the matrix instructions take 16 rows in the time of one.  Its waves take every
+// WAVES-th 64 channels each, straight into registers with DEPTH of them on their way at once, and their sums meet in LDS and are added up in order.  A lane has 32 neighbouring bytes of a
+// row's 64 channels, half of them in either product.
+constexpr int ROWS_FEW = 16;
+template <int NA, int DEPTH>
+__global__ __launch_bounds__(256) void k_gated_few(Args p, Gate gate, int ct)
+{
+    constexpr int WAVES = 4;
+    __shared__ __attribute__((aligned(16))) float sums[WAVES * NA * 256];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane & 15, h = gate.h;
+    const Place place = walk<1>(int(blockIdx.x), int(gridDim.x) / ct, ct);
+    const Piece at = counted(p.g.M, p.g.E) ? count_pieces(p.g, ROWS_FEW, place.row, reinterpret_cast<int*>(sums)) : find_piece(p.g, ROWS_FEW, place.row);
+    if (at.rows <= 0) return;
+    const int f0 = place.col * NA * 8;
+    f32x4 acc[NA] = {};
+    if (at.e < p.g.E) {
+        const bf16_t* w[NA];
+#pragma unroll
+        for (int n = 0; n < NA; ++n) w[n] = p.a + (size_t(at.e) * 2 * size_t(h) + (q & 2 ? size_t(h) : 0) + size_t(min(f0 + n * 8 + (q >> 2) * 2 + (q & 1), h - 1))) * size_t(p.K);
+        const bf16_t* const x = p.b + p.g.row(at.begin + min(q, at.rows - 1)) * p.b_stride;
+        for (int k0 = wave * 64; k0 < p.K; k0 += DEPTH * WAVES * 64) {
+            u32x4 a[DEPTH][2][NA] = {}, b[DEPTH][2] = {};
+#pragma unroll
+            for (int d = 0; d < DEPTH; ++d)
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    const int k = k0 + d * WAVES * 64 + (lane >> 4) * 16 + s * 8;
+                    if (k >= p.K) continue;
+#pragma unroll
+                    for (int n = 0; n < NA; ++n) a[d][s][n] = *reinterpret_cast<const u32x4*>(w[n] + k);
+                    b[d][s] = *reinterpret_cast<const u32x4*>(x + k);
+                }
+#pragma unroll
+            for (int d = 0; d < DEPTH; ++d)
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int n = 0; n < NA; ++n)
+                        acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a[d][s][n]), __builtin_bit_cast(bf16x8, b[d][s]), acc[n], 0, 0, 0);
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < NA; ++n) *reinterpret_cast<f32x4*>(sums + (n * WAVES * 64 + tid) * 4) = acc[n];
+    __syncthreads();
+    if (wave >= NA || q >= at.rows) return;                    // (wave n leaves with block n of features)
+    f32x4 sum = *reinterpret_cast<const f32x4*>(sums + (wave * WAVES * 64 + lane) * 4);
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) sum += *reinterpret_cast<const f32x4*>(sums + ((wave * WAVES + w) * 64 + lane) * 4);
+    const int f = f0 + wave * 8 + (lane >> 4) * 2;
+    bf16_t* const to = static_cast<bf16_t*>(p.out) + int64_t(at.begin + q) * p.out_stride + f;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        if (f + i < h) to[i] = f32_to_bf16((gate.form.b2 == 0.f ? gate_silu(sum[i]) : gate_f(gate.form, sum[i])) * sum[2 + i]);
+}
+
 int check(const moe_gated_shape* s, const std::string& who)
 {
     if (!s) return fail(DYNB_E_INVAL, who + ": NULL shape");
@@ -287,6 +344,27 @@ int launch_gated(const moe_product_shape* s, const Args& p, const Gate& gate, bo
     }
 }
 
+// Where this layer's tiles would leave CUs without work, and give the others one stream of weights after the other: up to 16 rows, and as many blocks of 8 features as start at once.  us, by rows, K, h,
+// experts and the blocks that are launched:
+//                                      tiles   1 block   2 blocks a workgroup
+//   1 x 512 x 1024, 1           128      4.9     3.2       3.7
+//   2 x 512 x 1024, 256         256      6.2     4.4       4.9
+//   1 x 2048 x 4096, 1          512     11.9     7.5       7.6
+//   16 x 2048 x 512, 1          128     11.1     6.1       7.9
+//   8 x 4096 x 1024, 1          128     19.8     9.1      12.5
+//   16 x 2048 x 4096, 1        1024     12.0    10.3       8.9
+//   4 x 1024 x 2048, 64        1024      9.3     9.5       8.1
+//   1 x 8192 x 8192, 1         1024     58.8    45.0      41.8
+//   8 x 4096 x 1536, 128       1536     30.9    34.4      34.0
+//   16 x 512 x 1024, 256       2048      6.9    12.2       7.3
+template <int NA, int DEPTH>
+int launch_few(const moe_product_shape* s, const Args& p, const Gate& gate, hipStream_t st)
+{
+    const int ct = (gate.h + NA * 8 - 1) / (NA * 8);
+    hipLaunchKernelGGL((k_gated_few<NA, DEPTH>), dim3(unsigned(most_pieces(s->M, s->E, ROWS_FEW) * ct)), dim3(256), 0, st, p, gate, ct);
+    return launched("moe_gated");
+}
+
 // whether what is kept lies on borders of 8 elements, and 32 rows of scales within 32 bits
 bool kept_on_8(const moe_gated_pre* p)
 {
@@ -309,10 +387,17 @@ extern "C" int moe_gated(const moe_gated_shape* s, const moe_groups* g, const vo
     if (in_stride < s->K || out_stride < s->h) return fail(DYNB_E_INVAL, "moe_gated: rows overlap (stride below their length)");
     if (odd(in) || odd(W) || odd(out)) return fail(DYNB_E_INVAL, "moe_gated: misaligned pointer");
     const Args p = {groups_of(&as, g), static_cast<const bf16_t*>(W), static_cast<const bf16_t*>(in), 0, in_stride, nullptr, 0, out, out_stride, as.K, as.N, 0};
+    const Gate gate = gate_of(s, pre, nullptr, 0, !pre ? 2 : pre->dtype == DYNB_BF16 ? 6 : 4);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (!pre && s->M <= ROWS_FEW && s->K % 8 == 0 && in_stride % 8 == 0 && on_16({in, W})) {
+        const int64_t blocks = (most_pieces(s->M, s->E, ROWS_FEW) - 1) * ((s->h + 7) / 8);
+        if (blocks <= 2 * CUS) return launch_few<1, 8>(&as, p, gate, st);
+        if (blocks <= 4 * CUS) return launch_few<2, 4>(&as, p, gate, st);
+    }
     // (32-bit offsets within an expert's two matrices: up's rows lie h rows behind gate's)
     const bool fast = s->K % 8 == 0 && s->h % 8 == 0 && in_stride % 8 == 0 && out_stride % 8 == 0 && on_16({in, W, out}) && kept_on_8(pre) && reached(g, in_stride, 0) &&
                       (int64_t(s->h) + 256) * s->K * 2 < int64_t(1) << 32;
-    return launch_gated<FORWARD>(&as, p, gate_of(s, pre, nullptr, 0, !pre ? 2 : pre->dtype == DYNB_BF16 ? 6 : 4), fast, static_cast<hipStream_t>(stream), "moe_gated");
+    return launch_gated<FORWARD>(&as, p, gate, fast, st, "moe_gated");
 }
 
 extern "C" int moe_gated_grad(const moe_gated_shape* s, const moe_groups* g, const void* dout, int64_t dout_stride, const void* W, const moe_gated_pre* pre, void* dpre, int64_t dpre_stride,

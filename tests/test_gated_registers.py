@@ -10,7 +10,7 @@ from tests.test_handover import OBJDUMP, code_objects
 pytestmark = pytest.mark.skipif(not os.path.exists(OBJDUMP), reason="needs llvm-objdump")
 
 
-@pytest.mark.parametrize("name,variants", [("7k_gatedI", 19), ("11k_gated_anyI", 10), ("8k_store8I", 2), ("7k_load8I", 2), ("12k_norm8_gradI", 28), ("15k_norm8_dx_longI", 2), ("20k_norm8_dparams_longI", 2)])
+@pytest.mark.parametrize("name,variants", [("7k_gatedI", 19), ("11k_gated_anyI", 10), ("11k_gated_fewI", 2), ("8k_store8I", 2), ("7k_load8I", 2), ("12k_norm8_gradI", 28), ("15k_norm8_dx_longI", 2), ("20k_norm8_dparams_longI", 2)])
 def test_no_variant_has_scratch_memory(tmp_path, name, variants):
     found = {}
     for path in code_objects(tmp_path):
