@@ -10,6 +10,7 @@
 //                                                          tile leaves; of the rest the stores are 15 without a pair, the arithmetic in 8 bits 40
 //   backward, 65536 rows, 1024 x 2048, 64 experts          490 from bf16, 467 from 8 bits: 275 GFLOP and 1.4 GB; without the stores 340
 //   forward, 148 rows, 256 experts, 1024 -> 2 x 2048       91 (504 MB of weights at 5.5 TB/s)
+//   forward, one row, 2048 -> 2 x 4096                     7.4 (33.6 MB), 8192 -> 2 x 8192 42 (6.4 TB/s)
 //   backward, 8192 rows, 256 experts, 512 x 1024           78 to 82 (360 MB at 4.5 TB/s)
 #include "moe_tiles.h"
 
@@ -303,7 +304,7 @@ int launch_kind(const moe_product_shape* s, const Args& p, const Gate& gate, hip
 // Mid 104, Few without a pair 91)
 using FewWide = Kind<2, 1, 2, 2, 3, 2>;
 // Half of Few's columns: twice the workgroups where Few's leave half of the CUs without work.  What bounds those is the way of a workgroup's stream of weights into its CU (one row,
-// 2048 -> 2 x 4096: 13.4 us by Few, 11.9 so; backward 14.8, 12.2; 64 rows, 1024 -> 2 x 2048: 8.9, 7.7; backward 11.0, 8.6; five chunks ahead instead of two: 12.8)
+// 2048 -> 2 x 4096, the pair in bf16: 13.4 us by Few, 12.0 so; backward 14.8, 12.2; 64 rows, 1024 -> 2 x 2048: 8.9, 7.7; backward 11.0, 8.6; five chunks ahead instead of two: 12.8)
 using Narrow = Kind<1, 1, 2, 2, 3, 2>;
 using AnyMid = Kind<2, 2, 2, 2, 2, 2>;   // 128 x 128
 using AnyFew = Kind<2, 1, 2, 2, 2, 2>;   // 128 columns x 64 rows
