@@ -338,13 +338,13 @@ __device__ __forceinline__ void leave_pairs(f32x16 (&acc)[S::FA][LIVE > 0 ? LIVE
                                 above = max(above, __float_as_int(x));
                                 below = max(below, __float_as_uint(x));
                             }
-                            const Scale8 c = scale8_of_sums(largest_of_halves(max(uint32_t(above), below & 0x7fffffffu)));
+                            const Scale8 c = scale8(largest_of_halves(max(uint32_t(above), below & 0x7fffffffu)));
 #pragma unroll
                             for (int n = 0; n < 2; ++n) {
                                 float x[8];
 #pragma unroll
                                 for (int i = 0; i < 8; ++i) x[i] = acc[a - 1 + n][b][8 * s + i];
-                                *(lds_u32x2*)(in8 + uint32_t(s * PART8 + n * 16)) = u32x2{pack8<false>(x[0], x[1], x[2], x[3], c.inv), pack8<false>(x[4], x[5], x[6], x[7], c.inv)};
+                                *(lds_u32x2*)(in8 + uint32_t(s * PART8 + n * 16)) = u32x2{pack8(x[0], x[1], x[2], x[3], c.inv), pack8(x[4], x[5], x[6], x[7], c.inv)};
                             }
                             // (without a branch: a half of the word is a block's, of gate in the lower half of the wave, of up in the upper)
                             const uint32_t mine = (s == 0 ? ~0u : 0u - uint32_t(hk)) & (a == 1 ? 0x0000ffffu : 0xffff0000u);
