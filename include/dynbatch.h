@@ -556,7 +556,8 @@ int dynb_layer_norm_backward(const dynb_norm_shape* shape, const void* dy, int64
 
 /* Rows of activations in 8 bits, for what a backward pass has to keep.  Every 32 neighbours of a row (the last ones may be fewer)
  * share a scale: with a = max |x|, s = a / 127 rounded up to a bfloat16, at least 2^-126, and q = the whole number nearest to
- * x * (1 / s), ties to even; both in fp32, step by step.  The row stands for q s: an element is off by at most s / 2, a / 252.
+ * x * (1 / s), ties to even; both in fp32, step by step.  The row stands for q s: an element is off by at most s / 2 and 2^-15 of
+ * that (fp32's roundings), which is below a / 252, or is 2^-127 where a is below 127 * 2^-126.
  * A block with an infinity or a NaN is NaN altogether; numbers next to the largest of fp32 may come back as infinities. */
 typedef struct {
     void* q;                  /* device [T][d] int8, rows q_stride elements apart                */

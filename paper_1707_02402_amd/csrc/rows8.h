@@ -1,7 +1,8 @@
 // Rows of activations in 8 bits.  Every 32 neighbours of a row (the last block of a row may be shorter) share a scale s: with a = max |x|
 //     s = a / 127, rounded up to a bfloat16, at least 2^-126        q = the whole number nearest to x * (1 / s), ties to even
 // in fp32, each step rounded once; what comes back is q s.  |q| <= 127 follows from s >= a / 127.  An element is off by at most s / 2 (and fp32's rounding of
-// x * (1 / s)), so by (1/254) (1 + 2^-7) of its block's largest.  Rounded up in 8 bits of significand a scale takes 2 bytes of 32 elements, costs at most 2^-7 of the step
+// x * (1 / s)): by at most a / 252, (1/254) (1 + 2^-7) of its block's largest, where a >= 127 * 2^-126, and by 2^-127 in a block of smaller numbers, whose s is held at 2^-126.
+// Rounded up in 8 bits of significand a scale takes 2 bytes of 32 elements, costs at most 2^-7 of the step
 // and keeps q s exact in fp32 (7 bits times 8).  Whole numbers rather than 8-bit floats: their step is the same for all elements of a block, so the error of
 // a sum of many of them is s / sqrt(12) an element, some 0.6 % of a normal block's standard deviation, where e4m3's 2^-4 half a step gives 2.6 %.
 // A block with an infinity or a NaN has s = NaN and q = 0: all of it comes back as NaN.
@@ -16,7 +17,8 @@ struct Scale8 { float s, inv; };                               // inv 0: not fin
 
 __device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }   // as a whole number: a NaN is above infinity
 // Both quotients are rounded as fp32 rounds: a product with the rounded 1 / 127, or a reciprocal to 1 ulp, and one correction by what it leaves over.  (The remainders are exact.  All 2^23
-// significands of a, and the 128 of s with a reciprocal up to 2 ulp off, come to what a division gives; below 2^-126, where a quotient loses bits, s does not depend on it.  A gated layer's tile takes no longer than without the corrections: 65536 rows, 1024 -> 2 x 2048, 728 us either way.)
+// significands of a, and the 128 of s with a reciprocal up to 2 ulp off, come to what a division gives; below 2^-126, where a quotient loses bits, s does not depend on it.
+// A gated layer's tile takes no longer than without the corrections: 65536 rows, 1024 -> 2 x 2048, 728 us either way.)
 __device__ __forceinline__ Scale8 scale8(uint32_t largest)
 {
     if (largest >= 0x7f800000u) return Scale8{__uint_as_float(0x7fc00000u), 0.f};
