@@ -21,11 +21,11 @@ namespace {
 // ahead, then go where a copy would have put them.  Places of rows and features are found once a tile; behind a tile's last row or feature the last one is loaded again, and the
 // results that it gives go nowhere.  Only the last chunk looks where its rows end.  A chunk's arithmetic (16 products a wave) covers a fraction of
 // memory's latency: with one chunk ahead 3001 rows, 777 -> 2 x 1001, 8 experts take 47 us, with three 28 (776 -> 2 x 1000 by the kernels below: 20).
-template <int DIR, class S, int KEEP, int DEPTH>
+template <int DIR, class S, int KEEP>
 __device__ __forceinline__ void gated_any(const Args& p, const Gate& gate, const Tile& t, lds_ptr lds)
 {
     constexpr bool A_ACROSS = DIR != FORWARD;
-    constexpr int AU = S::COLS / 64, BU = S::ROWS / 64, EACH = 8 / S::WAVES, UA = A_ACROSS ? YUNIT : XUNIT, UB = XUNIT, FA = S::FA, NB = S::NB;
+    constexpr int DEPTH = 3, AU = S::COLS / 64, BU = S::ROWS / 64, EACH = 8 / S::WAVES, UA = A_ACROSS ? YUNIT : XUNIT, UB = XUNIT, FA = S::FA, NB = S::NB;
     constexpr uint32_t BUF = BUF_BYTES<DIR, S>;
     using lds_u32x4 = __attribute__((address_space(3))) u32x4;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, q = lane & 31, hk = lane >> 5, cg = wave % S::CG, rg = wave / S::CG;
@@ -163,7 +163,7 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD) void k_gated_any(Args p, GateK
     const Place w = walk<1>(int(blockIdx.x), units / ct, ct);
     const Piece at = counted(p.g.M, p.g.E) ? count_pieces(p.g, S::ROWS, w.row, reinterpret_cast<int*>(lds_raw)) : find_piece(p.g, S::ROWS, w.row);
     if (at.rows > 0)
-        gated_any<DIR, S, KEEP, 3>(p, gate, Tile{at.e, at.begin, at.rows, w.col * (DIR == FORWARD ? S::COLS / 2 : S::COLS), 0, at.e < p.g.E ? (DIR == FORWARD ? p.K : p.N) : 0, -1}, (lds_ptr)lds_raw);
+        gated_any<DIR, S, KEEP>(p, gate, Tile{at.e, at.begin, at.rows, w.col * (DIR == FORWARD ? S::COLS / 2 : S::COLS), 0, at.e < p.g.E ? (DIR == FORWARD ? p.K : p.N) : 0, -1}, (lds_ptr)lds_raw);
 }
 
 // ------------------------------------------------------------------------------------------ K and h multiples of 8, rows on 16-byte borders

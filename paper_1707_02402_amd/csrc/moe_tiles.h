@@ -220,7 +220,8 @@ __device__ __forceinline__ Place walk(int u, int rows, int ct)
 template <bool WHOLE, bool PAST>
 __device__ __forceinline__ void put_eight(bf16_t* p, int left, const u32x4& v)
 {
-    if constexpr (WHOLE && PAST) __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(p));
+    static_assert(WHOLE || !PAST, "past the caches from borders only");
+    if constexpr (PAST) __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(p));
     else if constexpr (WHOLE) *reinterpret_cast<u32x4*>(p) = v;
     else if (left >= 8) *reinterpret_cast<u32x4_at2*>(p) = v;
     else
@@ -231,7 +232,8 @@ __device__ __forceinline__ void put_eight(bf16_t* p, int left, const u32x4& v)
 template <bool WHOLE, bool PAST>
 __device__ __forceinline__ void put_eight(int8_t* p, int left, const u32x2& v)
 {
-    if constexpr (WHOLE && PAST) __builtin_nontemporal_store(v, reinterpret_cast<u32x2*>(p));
+    static_assert(WHOLE || !PAST, "past the caches from borders only");
+    if constexpr (PAST) __builtin_nontemporal_store(v, reinterpret_cast<u32x2*>(p));
     else if constexpr (WHOLE) *reinterpret_cast<u32x2*>(p) = v;
     else store_eight(p, left, v);
 }
@@ -367,7 +369,7 @@ __device__ __forceinline__ void leave_pairs(f32x16 (&acc)[S::FA][LIVE > 0 ? LIVE
             }
         }
         __builtin_amdgcn_sched_barrier(0);
-        put_past(WHOLE && gate.past, [&](auto past) {
+        put_past<WHOLE>(gate.past, [&](auto past) {
             constexpr bool PAST = decltype(past)::value;
             const u32x4 none = {0u, 0u, 0u, 0u};
             const int l = here(), col = l % LANES * 8, row = l / LANES, cols = h - first - col;
@@ -431,7 +433,7 @@ __device__ __forceinline__ void leave_grads(f32x16 (&acc)[S::FA][LIVE > 0 ? LIVE
     const bool ends = !WHOLE && first + FA * 32 > h && first + 8 <= h;
     const int col = ends ? min(lane % LANES * 8, h - 8 - first) : lane % LANES * 8, c = first + col, cols = first + lane % LANES * 8 < h ? h - c : 0;
     auto put = [&](int64_t at, const u32x4& dg, const u32x4& du, const u32x4& f) {
-        put_past(WHOLE && gate.past, [&](auto past) {
+        put_past<WHOLE>(gate.past, [&](auto past) {
             constexpr bool PAST = decltype(past)::value;
             bf16_t* const to = static_cast<bf16_t*>(p.out) + at * p.out_stride + c;
             put_eight<WHOLE, PAST>(to, cols, dg);

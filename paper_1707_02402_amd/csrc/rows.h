@@ -99,12 +99,13 @@ template <int N> __device__ __forceinline__ void store_piece(bf16_t* p, int left
 
 // Results that no cache will hold until somebody reads them go past the caches, and leave those to what is read meanwhile: from PAST bytes on, half of what the
 // 256 MB of the memory's own cache take beside the operands.  What fits is read from there by the next call, and leaves as usual.
-// put(std::true_type) stores past them, put(std::false_type) does not; `past` is the same for all lanes.  (The compiler would make one store of the two, and an ordinary one.)
+// put(std::true_type) stores past them, put(std::false_type) does not; `past` is the same for all lanes, MAY false: it never is.  (The compiler would make one store of the two, and an ordinary one.)
 constexpr int64_t PAST = 64 << 20;
-template <class F>
+template <bool MAY = true, class F>
 __device__ __forceinline__ void put_past(bool past, F put)
 {
-    if (past) {
+    if constexpr (!MAY) put(std::false_type{});
+    else if (past) {
         asm volatile("; past the caches" ::: "memory");
         put(std::true_type{});
         asm volatile("" ::: "memory");
