@@ -706,7 +706,7 @@ def moe_gated(x, W, offsets, perm=None, k: int = 1, gate: int = MOE_GATE_SILU, o
     M = n if perm is None else perm.shape[0]
     xs = _rows(x, n, K)
     g = _groups_struct(offsets, perm, k, M, n)
-    assert two == 2 and W.is_cuda and W.is_contiguous() and W.dtype is x.dtype is _BF16 and len(offsets) == E + 1
+    assert two == 2 and W.is_cuda and W.is_contiguous() and W.dtype is x.dtype is _BF16 and offsets.shape == (E + 1,)
     if out is None:
         out = _new(stream, M, h, like=x)
     _check(lib.moe_gated(_GatedShape(M, K, h, E, DYNB_BF16, gate), g, x.data_ptr(), xs, W.data_ptr(), out.data_ptr(), _rows(out, M, h, x),
@@ -723,7 +723,7 @@ def moe_gated_grad(dout, W, offsets, pre, gate: int = MOE_GATE_SILU, dpre=None, 
     M = dout.shape[0]
     ds = _rows(dout, M, N)
     g = _groups_struct(offsets, None, 1, M, M)
-    assert W.is_cuda and W.is_contiguous() and W.dtype is dout.dtype is _BF16 and len(offsets) == E + 1
+    assert W.is_cuda and W.is_contiguous() and W.dtype is dout.dtype is _BF16 and offsets.shape == (E + 1,)
     if dpre is None:
         dpre = _new(stream, M, 2, h, like=dout)
     assert type(dpre) is not Rows8
