@@ -767,6 +767,7 @@ def dynb_load8(rows: Rows8, out=None, dtype: int = DYNB_BF16, stream=None):
     T, d = rows.q.shape
     r = _rows8_struct(rows, T, d)
     if out is None:
+        assert dtype in (DYNB_F32, DYNB_BF16), dtype
         out = _new(stream, T, d, like=rows.q, dtype=_F32 if dtype == DYNB_F32 else _BF16)
     _check(lib.dynb_load8(_Rows8Shape(T, d, _dtype_code(out)), r, out.data_ptr(), _rows(out, T, d), _stream(stream)))
     return out

@@ -14,3 +14,9 @@ def test_offsets_are_one_row_of_borders(dyn, shape):  # noqa: F811
         dyn.moe_gated(x, W, off)
     with pytest.raises(AssertionError):
         dyn.moe_gated_grad(x, torch.ones(3, 16, 8, dtype=BF, device="cuda"), off, torch.ones(6, 2, 8, dtype=BF, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", [2, -1])
+def test_rows_are_restored_in_bfloat16_or_float32(dyn, dtype):  # noqa: F811
+    with pytest.raises(AssertionError):
+        dyn.dynb_load8(dyn.dynb_store8(torch.ones(3, 40, device="cuda")), dtype=dtype)
