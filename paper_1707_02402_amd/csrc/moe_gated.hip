@@ -20,7 +20,7 @@ namespace {
 // 128 columns (64 features' gate and up) by 128 or 64 rows, by way of registers: pieces of 16 bytes are loaded from wherever they lie and wait there, DEPTH chunks of 64 places of the sum
 // ahead, then go where a copy would have put them.  Places of rows and features are found once a tile; behind a tile's last row or feature the last one is loaded again, and the
 // results that it gives go nowhere.  Only the last chunk looks where its rows end.  A chunk's arithmetic (16 products a wave) covers a fraction of
-// memory's latency: with one chunk ahead 3001 rows, 777 -> 2 x 1001, 8 experts take 47 us, with three 28 (776 -> 2 x 1000 by the kernels below: 20).
+// memory's latency: with one chunk ahead 3001 rows, 777 -> 2 x 1001, 8 experts, the pair in bf16 take 47 us, with three 28 (776 -> 2 x 1000 by the kernels below: 22).
 template <int DIR, class S, int KEEP>
 __device__ __forceinline__ void gated_any(const Args& p, const Gate& gate, const Tile& t, lds_ptr lds)
 {
